@@ -71,6 +71,7 @@ typedef enum { ACES_F32 = 0, ACES_BF16 = 1 } aces_dtype;
 #define ACES_ROW_BAD_Q 2     /* invalid draft probability or draft token   */
 #define ACES_ROW_TIMEOUT 4   /* reserved for a kernel that gives up a bounded
                                 wait; no current kernel waits on another */
+#define ACES_ROW_RANGE 8     /* positions outside the cache (aces_kv4_*)   */
 
 /* The CUDA runtime's cudaStream_t (NULL = legacy default stream). */
 typedef struct CUstream_st *aces_stream_t;
@@ -361,6 +362,98 @@ aces_status aces_tree_budget(const double *draft_latency_s, int n, double rtt_s,
  * 1 <= gamma <= ACES_MAX_K.  Host-only; launches nothing.
  */
 aces_status aces_branch_alloc(int B_alloc, int gamma, double alpha, double beta, int32_t *F_out);
+
+/*
+ * A KV cache in 4 bits.  The edge of Sec. III-C keeps the prefix, the main
+ * chain and every branch in its cache and has the least memory; the paper
+ * leaves the cache's numbers open, so the format is this library's own.
+ *
+ *   cache [planes, B, H, S, R]  device bytes, 16-byte aligned; planes =
+ *         layers x {K, V} (a layer's keys, then its values), H key heads, S
+ *         positions, R = aces_kv4_row_bytes(D) = D / 2 + 16 for D = 64 or 128
+ *
+ * aces_compact_kv moves its rows as they are (elem_bytes = 1, its D = R), and
+ * the tree's layout is aces_compact_kv's and aces_tree_mask's.
+ * A row has eight groups of D / 8 channels.  With a the first number of
+ * largest magnitude of a group (NaN as 0, magnitudes above 1015808 as that),
+ * t = -a / 2^19 rounded to five significant bits (ties to even), 0 when |a| <
+ * 2^-90, and the step s = t * 2^16, a number x becomes the code clamp(rint(x
+ * / s), -8, 7) + 8 (ties to even) and stands for (code - 8) * s: at most half
+ * a step off (1.25, for those beyond 7.5 steps on a's other side), where a
+ * step is |a| / 8 to 3%.  Channels 8 i + 2 j and 8 i + 2 j + 1 lie at bits 4 j
+ * and 4 j + 16 of the row's 32-bit word i < D / 8; the groups' t follow as
+ * bfloat16.  Any bytes stand for finite numbers.
+ */
+int aces_kv4_row_bytes(int D); /* -1 for another D */
+
+/*
+ * Quantises the keys and values of new positions as it writes them.
+ *   k, v          [B, n, H, D] float32 or bfloat16 (dt), the last dimension
+ *                 dense; k_strides, v_strides: host arrays of the strides of
+ *                 the first three in elements (any; multiples of 16 bytes on
+ *                 16-byte aligned arrays are read in vectors)
+ *   start         [B] int32: token i goes to position start[b] + i
+ *   count         [B] int32 or NULL: tokens i >= count[b] are padding
+ * Output:
+ *   row_status    [B, n] int32: ACES_ROW_NONFINITE where a NaN or infinity
+ *                 was written (as 0, and as the largest magnitude);
+ *                 ACES_ROW_RANGE where the position is outside the cache (the
+ *                 token is not written); 0 for padding
+ * Two sequences never touch one another's rows; no position is written twice.
+ */
+aces_status aces_kv4_append(void *cache, int planes, int layer, int B, int H, int S, int D, const void *k,
+                            const void *v, aces_dtype dt, const int64_t *k_strides, const int64_t *v_strides,
+                            const int32_t *start, const int32_t *count, int n, int32_t *row_status,
+                            aces_stream_t stream);
+
+/*
+ * Reads positions start[b] .. start[b] + n - 1 back as numbers (exact in both
+ * types): k, v [B, n, H, D] dense, 16-byte aligned.  Positions outside the
+ * cache read as zeros.
+ */
+aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H, int S, int D,
+                          const int32_t *start, int n, void *k, void *v, aces_dtype dt, aces_stream_t stream);
+
+/*
+ * Attention of n new tokens of every sequence over a cache in 4 bits (Sec.
+ * III-C: the packed branch forward; n = 1: one token; any n: a prompt, in one
+ * piece or several).  The new tokens' keys and values are in the cache
+ * already (aces_kv4_append at prefix_len).
+ *   q             [B, n, Hq, D] float32 or bfloat16 (dt), the last dimension
+ *                 dense; q_strides as above; Hq a multiple of H: query heads
+ *                 h * Hq / H .. read key head h
+ *   prefix_len    [B] int32: cached positions before the new tokens, all of
+ *                 them visible
+ *   count         [B] int32 or NULL: tokens i >= count[b] are padding
+ *   mask, depth   NULL: new token i sees new tokens 0 .. i and has position
+ *                 prefix + i.  Else aces_tree_mask's: bit j of mask's row i
+ *                 lets it see new token j, and its position is prefix +
+ *                 depth[i].  mask_stride (words) and depth_stride (entries)
+ *                 between two sequences' arrays; 0: shared
+ *   scale > 0     of q . k (1 / sqrt(D) as a rule)
+ *   window, sinks window > 0: of what it sees otherwise a token at position p
+ *                 sees positions above p - window and those below sinks
+ * Outputs:
+ *   out           [B, n, Hq, D] of q's type, dense, 16-byte aligned: softmax(
+ *                 scale q . k) v; zeros for padding and tokens that see nothing
+ *   lse           [B, n, Hq] float32 or NULL: ln of the sum of exp(scale q .
+ *                 k); -inf for those
+ *   seq_status    [B] int32: ACES_ROW_RANGE where prefix_len or count is
+ *                 negative, count above n, or prefix + count above S (the
+ *                 sequence's tokens count as padding)
+ * Products are those of the cache's numbers and q's as they are, sums float32.
+ * Weights are rounded to bfloat16 before they meet the values when q is
+ * bfloat16, and are float32 when it is.
+ * workspace: aces_kv4_workspace_bytes(B, n, Hq, H, D) bytes, 16-byte aligned,
+ * not initialised, unused by others while the call's work is in flight.
+ */
+size_t aces_kv4_workspace_bytes(int B, int n, int Hq, int H, int D); /* 0 for invalid sizes */
+aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_strides, const void *cache, int planes,
+                               int layer, int B, int n, int Hq, int H, int S, int D, const int32_t *prefix_len,
+                               const int32_t *count, const uint32_t *mask, int64_t mask_stride,
+                               const int32_t *depth, int64_t depth_stride, float scale, int window, int sinks,
+                               void *out, float *lse, int32_t *seq_status, void *workspace,
+                               size_t workspace_bytes, aces_stream_t stream);
 
 #ifdef ACES_CHECKED
 /*

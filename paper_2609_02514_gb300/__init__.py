@@ -12,6 +12,8 @@ without the built library, or with host tensors, raises.
     sparsify(z, T, top_p, k)              Sec. III-B / V-C downlink payload
     cache_build(q, xt, F)                 Sec. III-C branch cache
     cache_lookup(branch_tok, F, pi, tok)  Algorithm 1 state recovery
+    kv4_cache, kv4_append, kv4_read       a KV cache in 4 bits
+    kv4_attention(q, cache, ...)          tokens, trees and prompts against it
 """
 from __future__ import annotations
 
@@ -22,7 +24,8 @@ import threading
 import torch
 
 __all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
-           "ROW_NONFINITE", "ROW_BAD_Q", "COUNTERS_OFFSET", "AcespecError"]
+           "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
+           "ROW_NONFINITE", "ROW_BAD_Q", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libacespec.so")
@@ -37,6 +40,7 @@ COUNTERS_OFFSET = 256
 
 ROW_NONFINITE = 1
 ROW_BAD_Q = 2
+ROW_RANGE = 8
 ACES_F32 = 0
 ACES_BF16 = 1
 _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported argument", 3: "CUDA launch error"}
@@ -118,11 +122,19 @@ def _open(path):
     lib.aces_tree_mask.argtypes = [P, I, I, P, P, P]
     lib.aces_tree_budget.argtypes = [P, I, ctypes.c_double, ctypes.c_double, I, P]
     lib.aces_branch_alloc.argtypes = [I, I, ctypes.c_double, ctypes.c_double, P]
+    L = ctypes.c_int64
+    lib.aces_kv4_row_bytes.argtypes = [I]
+    lib.aces_kv4_row_bytes.restype = I
+    lib.aces_kv4_workspace_bytes.argtypes = [I, I, I, I, I]
+    lib.aces_kv4_workspace_bytes.restype = S
+    lib.aces_kv4_append.argtypes = [P, I, I, I, I, I, I, P, P, I, P, P, P, P, I, P, P]
+    lib.aces_kv4_read.argtypes = [P, I, I, I, I, I, I, P, I, P, P, I, P]
+    lib.aces_kv4_attention.argtypes = [P, I, P, P, I, I, I, I, I, I, I, I, P, P, P, L, P, L, F, I, I, P, P, P, P, S, P]
     lib.aces_status_string.argtypes = [I]
     lib.aces_status_string.restype = ctypes.c_char_p
     for f in (lib.aces_verify, lib.aces_verify_exact, lib.aces_sparsify, lib.aces_cache_build,
               lib.aces_cache_lookup, lib.aces_resample_sparse, lib.aces_tree_budget, lib.aces_branch_alloc,
-              lib.aces_compact_kv, lib.aces_tree_mask):
+              lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention):
         f.restype = I
     if hasattr(lib, "aces_checked_violation"):
         lib.aces_checked_violation.argtypes = [P]
@@ -420,3 +432,144 @@ def tree_mask(F, branch_len: int, device=None):
     _check("aces_tree_mask", lib.aces_tree_mask(Fh, K, int(branch_len), mask.data_ptr(), depth.data_ptr(),
                                                 _stream(mask.device)))
     return mask, depth
+
+
+def _kv4_cache(cache):
+    """(planes, B, H, S, D) of a 4-bit cache."""
+    c = _cuda(cache, "cache")
+    if c.dtype != torch.uint8 or c.dim() != 5:
+        raise ValueError("cache must be uint8 [planes, B, H, S, row]")
+    planes, B, H, S, R = c.shape
+    return planes, B, H, S, 2 * (R - 16)
+
+
+def _dense_rows(t, name, shape=None, dtype=None, like=None):
+    """A [B, n, H, D] CUDA tensor whose last dimension is dense, and its strides."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 4 or (t.shape[3] != 1 and t.stride(3) != 1):
+        raise ValueError(f"{name} must be [B, n, heads, D] with a dense last dimension")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if shape is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype} {list(shape)}")
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _ints(t, name, *shape):
+    t = _cuda(t, name)
+    if t.dtype != _I32 or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be int32 {list(shape)}")
+    return t.data_ptr()
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}")
+
+
+def kv4_cache(layers: int, B: int, H: int, S: int, D: int, device=None):
+    """An empty 4-bit KV cache: uint8 [2 * layers, B, H, S, D / 2 + 16].
+    Moved rows and all, it is what compact_kv() takes."""
+    R = int(load().aces_kv4_row_bytes(int(D)))
+    if R < 0:
+        raise ValueError("D must be 64 or 128")
+    return torch.zeros(2 * layers, B, H, S, R, dtype=torch.uint8, device="cuda" if device is None else device)
+
+
+def kv4_append(cache, layer: int, k, v, start, count=None, out: torch.Tensor | None = None):
+    """Quantise k, v [B, n, H, D] into the cache at positions start[b] + i (in
+    place; tokens i >= count[b] are padding); returns row_status [B, n] int32.
+    k and v may be strided views with a dense last dimension."""
+    lib = load()
+    planes, B, H, S, D = _kv4_cache(cache)
+    ks = _dense_rows(k, "k")
+    n = k.shape[1]
+    if tuple(k.shape) != (B, n, H, D):
+        raise ValueError(f"k must be [{B}, n, {H}, {D}]")
+    vs = _dense_rows(v, "v", tuple(k.shape), k.dtype)
+    dev = cache.device
+    _same_device(dev, k=k, v=v, start=start, count=count, out=out)
+    st = out if out is not None else torch.empty(B, n, dtype=_I32, device=dev)
+    code = lib.aces_kv4_append(cache.data_ptr(), planes, int(layer), B, H, S, D, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype],
+                               ks, vs, _ints(start, "start", B), None if count is None else _ints(count, "count", B), n,
+                               _ints(st, "out", B, n), _stream(dev))
+    if code != 0:
+        _check("aces_kv4_append", code)
+    return st
+
+
+def kv4_read(cache, layer: int, start, n: int, dtype=torch.bfloat16, out: dict | None = None):
+    """Positions start[b] .. start[b] + n - 1 of the cache as numbers: a dict of
+    k, v [B, n, H, D] (zeros outside the cache)."""
+    lib = load()
+    planes, B, H, S, D = _kv4_cache(cache)
+    if dtype not in _DTYPES:
+        raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
+    dev = cache.device
+    o = _outputs(out, dev, ("k", (B, n, H, D), dtype), ("v", (B, n, H, D), dtype))
+    for key in ("k", "v"):
+        if _cuda(o[key], key).dtype != dtype or tuple(o[key].shape) != (B, n, H, D):
+            raise ValueError(f"{key} must be {dtype} {[B, n, H, D]}")
+    _same_device(dev, start=start, k=o["k"], v=o["v"])
+    code = lib.aces_kv4_read(cache.data_ptr(), planes, int(layer), B, H, S, D, _ints(start, "start", B), int(n),
+                             o["k"].data_ptr(), o["v"].data_ptr(), _DTYPES[dtype], _stream(dev))
+    if code != 0:
+        _check("aces_kv4_read", code)
+    return o
+
+
+def kv4_workspace_bytes(B: int, n: int, Hq: int, H: int, D: int) -> int:
+    return int(load().aces_kv4_workspace_bytes(int(B), int(n), int(Hq), int(H), int(D)))
+
+
+def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count=None, scale: float | None = None,
+                  window: int = 0, sinks: int = 0, out: dict | None = None, workspace: torch.Tensor | None = None):
+    """Attention of q [B, n, Hq, D] over the layer's cache, whose positions
+    prefix_len[b] .. hold the new tokens already (kv4_append).
+
+    Without a mask new token i sees the prefix and the new tokens up to itself;
+    with tree_mask()'s mask and depth ([n, words] and [n], or one a sequence:
+    [B, n, words] and [B, n]) what the tree lets it.  window > 0: only positions
+    above its own minus window, and those below sinks.  Tokens i >= count[b]
+    are padding.  scale: 1 / sqrt(D) unless given.  Returns a dict of out
+    [B, n, Hq, D], lse [B, n, Hq] and status [B] (ROW_RANGE: a sequence whose
+    tokens do not lie in the cache).
+    """
+    lib = load()
+    planes, B, H, S, D = _kv4_cache(cache)
+    qs = _dense_rows(q, "q")
+    n, Hq = q.shape[1], q.shape[2]
+    if q.shape[0] != B or q.shape[3] != D:
+        raise ValueError(f"q must be [{B}, n, Hq, {D}]")
+    if (mask is None) != (depth is None):
+        raise ValueError("mask and depth go together")
+    dev = cache.device
+    mp = dp = None
+    ms = ds = 0
+    if mask is not None:
+        words = (n + 31) // 32
+        each = mask.dim() == 3
+        mp = _ints(mask, "mask", *((B, n, words) if each else (n, words)))
+        ms = n * words if each else 0
+        each = depth.dim() == 2
+        dp = _ints(depth, "depth", *((B, n) if each else (n,)))
+        ds = n if each else 0
+    o = _outputs(out, dev, ("out", (B, n, Hq, D), q.dtype), ("lse", (B, n, Hq), _F32), ("status", (B,), _I32))
+    for key, shape, dtype in (("out", (B, n, Hq, D), q.dtype), ("lse", (B, n, Hq), _F32), ("status", (B,), _I32)):
+        if _cuda(o[key], key).dtype != dtype or tuple(o[key].shape) != shape:
+            raise ValueError(f"{key} must be {dtype} {list(shape)}")
+    ws = workspace
+    if ws is None:
+        ws = _empty(max(kv4_workspace_bytes(B, n, Hq, H, D), 16), dtype=torch.uint8, device=dev)
+    _same_device(dev, q=q, prefix_len=prefix_len, count=count, mask=mask, depth=depth, workspace=ws, out=o["out"], lse=o["lse"],
+                 status=o["status"])
+    code = lib.aces_kv4_attention(q.data_ptr(), _DTYPES[q.dtype], qs, cache.data_ptr(), planes, int(layer), B, n, Hq, H, S, D,
+                                  _ints(prefix_len, "prefix_len", B), None if count is None else _ints(count, "count", B),
+                                  mp, ms, dp, ds, D ** -0.5 if scale is None else float(scale), int(window), int(sinks),
+                                  o["out"].data_ptr(), o["lse"].data_ptr(), o["status"].data_ptr(), ws.data_ptr(),
+                                  ws.numel() * ws.element_size(), _stream(dev))
+    if code != 0:
+        _check("aces_kv4_attention", code)
+    return o

@@ -10,12 +10,8 @@
 
 using namespace aces;
 
-namespace {
-
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
 // SMs of the current device (asked once per device)
-int sm_count() {
+int aces::sm_count() {
     static std::atomic<int> of[64];
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 132;
@@ -24,6 +20,10 @@ int sm_count() {
     if (dev < 64) of[dev].store(n, std::memory_order_relaxed);
     return n;
 }
+
+namespace {
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
 size_t elem_size(aces_dtype dt) { return dt == ACES_BF16 ? 2 : 4; }
 
@@ -410,7 +410,7 @@ extern "C" aces_status aces_checked_violation(unsigned long long out[3]) {
     if (cudaDeviceSynchronize() != cudaSuccess) return ACES_ERR_CUDA;
     cudaError_t (*take[])(unsigned long long *) = {check_take_rows_cap, check_take_rows_general,
                                                    check_take_cache, check_take_resample, check_take_kv,
-                                                   check_take_mask};
+                                                   check_take_mask, check_take_kv4_rows, check_take_kv4_attend};
     out[0] = out[1] = out[2] = 0ull;
     for (auto f : take) {
         unsigned long long w[3];

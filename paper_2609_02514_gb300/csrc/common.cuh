@@ -47,6 +47,8 @@ cudaError_t check_take_selects(unsigned int *n);
 cudaError_t check_take_resample(unsigned long long out[3]);
 cudaError_t check_take_kv(unsigned long long out[3]);
 cudaError_t check_take_mask(unsigned long long out[3]);
+cudaError_t check_take_kv4_rows(unsigned long long out[3]);
+cudaError_t check_take_kv4_attend(unsigned long long out[3]);
 #else
 #define ACES_IN(i, n) true
 #endif
@@ -522,6 +524,8 @@ __device__ void nonfinite_row(const RowArgs &a, int r) {
     }
 }
 
+// SMs of the current device
+int sm_count();
 // host launchers (defined next to their kernels)
 void rows_cap_layout(RowArgs &a, int dt, bool ragged);
 cudaError_t launch_rows_cap(const RowArgs &a, int dt, bool ragged, cudaStream_t s);
