@@ -1,0 +1,526 @@
+// Attention over a 4-bit KV cache for few query rows (the format: kv4.cuh, the
+// shares: kv4_plan.cuh): single tokens, and everything in float32.
+#define ACES_FILE 8  // site numbers of the checked build
+#include <cuda_bf16.h>
+
+#include "kv4_plan.cuh"
+
+namespace aces {
+
+constexpr int FW = 8;            // warps
+constexpr int FT = FW * 32;
+constexpr int FKT = 32;          // keys of a tile: one warp's step
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
+}
+
+template <int D, bool F32, int NT>
+struct Few {
+    static constexpr int RB = kv4_row_bytes(D), R = 8 * NT, KS = D / 16, JT = D / 16, WPT = D / 32;
+    static constexpr int SPL = F32 ? 3 : 1;                 // bfloat16 parts of a query number and of a weight
+    static constexpr int MINB = !F32 && NT == 1 ? 2 : 1;    // CTAs an SM
+    static constexpr int ST = MINB == 2 ? 2 : 4;            // stages of a warp's ring
+    static constexpr bool QREG = !F32 && NT == 1;
+    static constexpr int STAGE = 2 * FKT * RB, RING = FW * ST * STAGE;
+    static constexpr int MERGE = FW * JT * 4 * 32 * 4;
+    static constexpr int QS = QREG ? 0 : NT * SPL * KS * 32 * 8;
+    static constexpr int SMEM = RING + MERGE + QS;
+};
+
+// The tiles stay in registers and shared memory: a warp takes 32 keys at a
+// time through a ring of its own (one bulk copy of the keys' rows, one of the
+// values'), dequantises them straight into the first operand of the tensor
+// products and keeps 8 NT query rows as the second, so no query row is padded
+// beyond eight:
+//   S' [16 keys x 8 rows] = K [16 x 16 channels] Q',
+//   O' [16 channels x 8 rows] += V' [16 x 16 keys] P'.
+// A thread's key words are neighbours of one row, its value words the same
+// channels of neighbouring keys: channels and keys come in whatever order the
+// words have, the same in both operands.  P' needs its pairs along the keys,
+// where S' has them along the rows: movmatrix turns the 8 x 8 blocks.
+template <int D, bool F32, int NT>
+__global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT) {
+    using C = Few<D, F32, NT>;
+    constexpr int RB = C::RB, R = C::R, KS = C::KS, JT = C::JT, WPT = C::WPT, ST = C::ST, SPL = C::SPL;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) unsigned long long bars[FW * ST];
+    __shared__ float sm_m[FW][R], sm_l[FW][R];
+    __shared__ int2 rowinfo[R];                 // token and position of a row
+    __shared__ int any_timeout;
+    float *merge = reinterpret_cast<float *>(smem + C::RING);
+    uint2 *qs = reinterpret_cast<uint2 *>(smem + C::RING + C::MERGE);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const uint32_t ring = smem_u32(smem) + warp * ST * C::STAGE;
+    const uint8_t *ringp = smem + warp * ST * C::STAGE;
+    const uint32_t bar0 = smem_u32(bars) + warp * ST * 8;
+    if (lane == 0)
+        for (int s = 0; s < ST; ++s) mbar_init(bar0 + 8 * s, 1);
+    if (tid == 0) any_timeout = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+
+    Kv4Start at = kv4_start<FKT, R, FW, FT>(a, RT);  // has a __syncthreads after the barriers' start
+    int e = at.e, h = at.h, x0 = at.off;
+    if (tid == 0) {
+        Kv4Info in;
+        in.valid = at.left > 0;
+        in.timeout = 0;
+        in.quantum = at.quantum;
+        in.b = in.rt = in.h = in.off = in.units = 0;
+        if (in.valid) {
+            in.b = e / RT, in.rt = e % RT, in.h = h, in.off = x0;
+            in.units = kv4_keys<FKT, R, FW>(a, in.b, in.rt).units;
+        }
+        ws.info[blockIdx.x] = in;
+    }
+    if (at.left == 0) return;
+    unsigned long long left = at.left;
+    Kv4Keys key = kv4_keys<FKT, R, FW>(a, e / RT, e % RT);
+    int x1 = (int)min((unsigned long long)key.units, x0 + left);
+
+    int seq = 0;       // tiles this warp has taken, of all segments
+    bool bad = false;  // a wait gave up
+    // this warp's y-th tile of the segment, into the ring's next place
+    auto issue = [&](const Kv4Keys &k, int b, int hh, int tile, int place) {
+        if (lane != 0) return;
+        const int j0 = kv4_tile<FKT>(k, tile), rows = min(FKT, k.P + k.cnt - j0);
+        if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
+        const int s = place % ST;
+        const uint32_t bytes = rows * RB, dst = ring + s * C::STAGE;
+        const size_t off = ((size_t)((size_t)b * a.H + hh) * a.S + j0) * RB;
+        mbar_expect(bar0 + 8 * s, 2 * bytes);
+        bulk_load(dst, a.k + off, bytes, bar0 + 8 * s);
+        bulk_load(dst + FKT * RB, a.v + off, bytes, bar0 + 8 * s);
+    };
+    auto my_tiles = [&](const Kv4Keys &k, int u0, int u1) {
+        const int top = min(u1 * FW, k.tiles) - u0 * FW - warp;
+        return top > 0 ? (top + FW - 1) / FW : 0;
+    };
+    int mine = my_tiles(key, x0, x1);
+    for (int y = 0; y < min(ST, mine); ++y) issue(key, e / RT, h, (x0 + y) * FW + warp, seq + y);
+
+    bool first = true;
+    while (true) {
+        const int b = e / RT, rt = e % RT, P = key.P, end = P + key.cnt;
+        // the segment's query rows
+        if (tid < R) {
+            const int r = rt * R + tid, i = r / a.G;
+            const bool ok = r < a.n * a.G && key.live && i < key.cnt;
+            rowinfo[tid] = ok ? make_int2(i, kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i)) : make_int2(-1, 0);
+        }
+        uint32_t q[C::QREG ? 2 * KS : 1];
+        auto q_words = [&](int row, int word, int sp, uint32_t (&o)[4]) {  // eight channels of a query row
+            const int r = rt * R + row;
+            o[0] = o[1] = o[2] = o[3] = 0u;
+            const int i = r / a.G;
+            if (!(r < a.n * a.G && key.live && i < key.cnt)) return;
+            const long long p = b * a.qb + i * a.qi + (long long)(h * a.G + r % a.G) * a.qh + 8 * word;
+            if (F32) {
+                const float *f = reinterpret_cast<const float *>(a.q) + p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float v0 = __ldg(f + 2 * j), v1 = __ldg(f + 2 * j + 1);
+                    uint32_t w = bf2_pack(v0, v1);
+                    for (int s = 0; s < sp; ++s) {
+                        v0 -= bf_lo(w), v1 -= bf_hi(w);
+                        w = bf2_pack(v0, v1);
+                    }
+                    o[j] = bf2_poison(w);
+                }
+            } else {
+                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + p;
+                if (((uintptr_t)f & 15) == 0) {
+                    const uint4 w = ldg16(f);
+                    o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = (uint32_t)__ldg(f + 2 * j) | (uint32_t)__ldg(f + 2 * j + 1) << 16;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = bf2_poison(o[j]);
+            }
+        };
+        if (C::QREG) {
+#pragma unroll
+            for (int w = 0; w < WPT; ++w) {
+                uint32_t o[4];
+                q_words(g, WPT * t + w, 0, o);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[C::QREG ? 4 * w + j : 0] = o[j];
+            }
+        } else {
+            for (int x = tid; x < NT * SPL * (KS / 2) * 32; x += FT) {  // one word: two steps of a lane
+                const int l = x & 31, w = (x >> 5) % WPT, sp = (x >> 5) / WPT % SPL, nt = (x >> 5) / WPT / SPL;
+                uint32_t o[4];
+                q_words(nt * 8 + (l >> 2), WPT * (l & 3) + w, sp, o);
+                qs[((nt * SPL + sp) * KS + 2 * w) * 32 + l] = make_uint2(o[0], o[1]);
+                qs[((nt * SPL + sp) * KS + 2 * w + 1) * 32 + l] = make_uint2(o[2], o[3]);
+            }
+        }
+        __syncthreads();
+        int posmax = 0;
+        if (a.window)
+            for (int r = 0; r < R; ++r) posmax = max(posmax, rowinfo[r].y);
+        const int all_see = P + (a.mask ? 0 : key.i0 + 1);  // positions below it are new to no row
+
+        float O[NT][JT][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < JT; ++j) O[nt][j][0] = O[nt][j][1] = O[nt][j][2] = O[nt][j][3] = 0.0f;
+        }
+        for (int y = 0; y < mine; ++y, ++seq) {
+            const int s = seq % ST;
+            if (!bad && !mbar_wait(bar0 + 8 * s, (seq / ST) & 1)) bad = true;
+            const uint8_t *kt = ringp + s * C::STAGE, *vt = kt + FKT * RB;
+            const int j0 = kv4_tile<FKT>(key, (x0 + y) * FW + warp);
+            float S[NT][2][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) S[nt][mt][0] = S[nt][mt][1] = S[nt][mt][2] = S[nt][mt][3] = 0.0f;
+                uint32_t w[2][WPT], t2[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint8_t *row = kt + (mt * 16 + x * 8 + g) * RB;
+                    if (WPT == 4) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(row + 16 * t);
+                        w[x][0] = v.x, w[x][1] = v.y, w[x][WPT / 2] = v.z, w[x][WPT - 1] = v.w;
+                    } else {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(row + 8 * t);
+                        w[x][0] = v.x, w[x][1] = v.y;
+                    }
+                    t2[x] = *reinterpret_cast<const uint32_t *>(row + D / 2 + 4 * t) & KV4_T_MASK;
+                }
+#pragma unroll
+                for (int i = 0; i < WPT; ++i) {
+                    uint32_t p[2][4];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t tt = __byte_perm(t2[x], 0, i < WPT / 2 ? 0x1010 : 0x3232);
+                        kv4_pairs(w[x][i], tt, kv4_offset(tt), p[x]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t A[4] = {p[0][2 * u], p[1][2 * u], p[0][2 * u + 1], p[1][2 * u + 1]};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (C::QREG) {
+                                mma16816(S[nt][mt], A, q[C::QREG ? 4 * i + 2 * u : 0], q[C::QREG ? 4 * i + 2 * u + 1 : 0]);
+                            } else {
+#pragma unroll
+                                for (int sp = SPL - 1; sp >= 0; --sp) {
+                                    const uint2 qq = qs[((nt * SPL + sp) * KS + 2 * i + u) * 32 + lane];
+                                    mma16816(S[nt][mt], A, qq.x, qq.y);
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+            // scores to weights
+            const bool masked = j0 + FKT > all_see || (a.window && j0 <= posmax - a.window && j0 + FKT > a.sinks);
+            uint32_t pk[NT][2][SPL][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int2 ri = rowinfo[nt * 8 + 2 * t + c];
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)
+                                if (ri.x < 0 || !kv4_sees(a, b, P, end, j0 + mt * 16 + x * 8 + g, ri.x, ri.y))
+                                    S[nt][mt][2 * x + c] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float mx = fmaxf(fmaxf(S[nt][0][c], S[nt][0][2 + c]), fmaxf(S[nt][1][c], S[nt][1][2 + c])) * a.scale;
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    const float mn = fmaxf(m[nt][c], mx);
+                    if (__any_sync(0xffffffffu, mn > m[nt][c])) {
+                        const float f = mn == -INFINITY ? 1.0f : ex2(m[nt][c] - mn);
+                        m[nt][c] = mn;
+                        l[nt][c] *= f;
+#pragma unroll
+                        for (int j = 0; j < JT; ++j) O[nt][j][c] *= f, O[nt][j][2 + c] *= f;
+                    }
+                    const float ref = mn == -INFINITY ? 0.0f : mn;
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float p = ex2(fmaf(S[nt][mt][2 * x + c], a.scale, -ref));
+                            S[nt][mt][2 * x + c] = p;
+                            l[nt][c] += p;
+                        }
+                }
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        float p0 = S[nt][mt][2 * x], p1 = S[nt][mt][2 * x + 1];
+#pragma unroll
+                        for (int sp = 0; sp < SPL; ++sp) {
+                            const uint32_t w = bf2_pack(p0, p1);
+                            pk[nt][mt][sp][x] = movmatrix(w);
+                            p0 -= bf_lo(w), p1 -= bf_hi(w);
+                        }
+                    }
+            }
+            // values
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                uint32_t w[4][WPT / 2], t1[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint8_t *row = vt + (mt * 16 + 2 * t + (x & 1) + (x >> 1) * 8) * RB;
+                    if (WPT == 4) {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(row + 8 * g);
+                        w[x][0] = v.x, w[x][WPT / 2 - 1] = v.y;
+                    } else {
+                        w[x][0] = *reinterpret_cast<const uint32_t *>(row + 4 * g);
+                    }
+                    t1[x] = *reinterpret_cast<const unsigned short *>(row + D / 2 + 2 * g);
+                }
+                // pairs of neighbouring keys: lo[u] of keys 2t, 2t + 1, then of 2t + 8, 2t + 9
+                uint32_t tt[2], off[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    tt[u] = __byte_perm(t1[2 * u], t1[2 * u + 1], 0x5410) & KV4_T_MASK;
+                    off[u] = kv4_offset(tt[u]);
+                }
+                // even and odd channels of a word: pv[word][odd][u][j]
+                uint32_t pv[WPT / 2][2][2][4];
+#pragma unroll
+                for (int i = 0; i < WPT / 2; ++i)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        kv4_pairs(__byte_perm(w[2 * u][i], w[2 * u + 1][i], 0x5410), tt[u], off[u], pv[i][0][u]);
+                        kv4_pairs(__byte_perm(w[2 * u][i], w[2 * u + 1][i], 0x7632), tt[u], off[u], pv[i][1][u]);
+                    }
+                // D = 128: rows g are word 2g, rows g + 8 word 2g + 1; D = 64: channels j and j + 4 of word g
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    constexpr int I1 = WPT / 2 - 1;
+                    const int ja = j, jb = WPT == 4 ? j : j + 4;
+                    const uint32_t A[4] = {pv[0][ja & 1][0][ja >> 1], pv[I1][jb & 1][0][jb >> 1], pv[0][ja & 1][1][ja >> 1],
+                                           pv[I1][jb & 1][1][jb >> 1]};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (F32) {  // the products of 16 keys are summed apart: the tensor cores' sums do not round to nearest
+                            float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                            for (int sp = SPL - 1; sp >= 0; --sp) mma16816(c, A, pk[nt][mt][sp][0], pk[nt][mt][sp][1]);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) O[nt][j][x] += c[x];
+                        } else {
+                            mma16816(O[nt][j], A, pk[nt][mt][0][0], pk[nt][mt][0][1]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (y + ST < mine) issue(key, b, h, (x0 + y + ST) * FW + warp, seq + ST);
+        }
+        // the next segment, whose first tiles are on their way while this one is merged
+        const bool whole = x0 == 0 && x1 == key.units;
+        left -= x1 - x0;
+        int ne = e, nh = h + 1, nx1 = 0, nmine = 0;
+        Kv4Keys nkey = key;
+        if (left > 0) {
+            if (nh == a.H) {
+                nh = 0, ++ne;
+                nkey = kv4_keys<FKT, R, FW>(a, ne / RT, ne % RT);
+            }
+            nx1 = (int)min((unsigned long long)nkey.units, left);
+            nmine = my_tiles(nkey, 0, nx1);
+            for (int y = 0; y < min(ST, nmine); ++y) issue(nkey, ne / RT, nh, y * FW + warp, seq + y);
+        }
+        // merge the warps
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 4);
+                l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 8);
+                l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
+                if (g == 0) sm_m[warp][nt * 8 + 2 * t + c] = m[nt][c], sm_l[warp][nt * 8 + 2 * t + c] = l[nt][c];
+            }
+        if (bad && lane == 0) any_timeout = 1;
+        __syncthreads();
+        float *slot = ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float M[2], L[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                M[c] = sm_m[0][nt * 8 + 2 * t + c];
+                for (int w = 1; w < FW; ++w) M[c] = fmaxf(M[c], sm_m[w][nt * 8 + 2 * t + c]);
+                const float ref = M[c] == -INFINITY ? 0.0f : M[c];
+                L[c] = 0.0f;
+                for (int w = 0; w < FW; ++w) L[c] += sm_l[w][nt * 8 + 2 * t + c] * ex2(sm_m[w][nt * 8 + 2 * t + c] - ref);
+                const float f = ex2(m[nt][c] - ref);
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    merge[((warp * JT + j) * 4 + c) * 32 + lane] = O[nt][j][c] * f;
+                    merge[((warp * JT + j) * 4 + 2 + c) * 32 + lane] = O[nt][j][2 + c] * f;
+                }
+            }
+            __syncthreads();
+            if (warp < JT) {  // warp j adds up the j-th tile of channels
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float o = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < FW; ++w) o += merge[((w * JT + warp) * 4 + x) * 32 + lane];
+                    const int c = x & 1, row = nt * 8 + 2 * t + c, r = rt * R + row;
+                    const int d = WPT == 4 ? 16 * g + (x >> 1) * 8 + warp : 8 * g + (x >> 1) * 4 + warp;
+                    const int i = r / a.G;
+                    if (!whole) {
+                        slot[row * D + d] = o;
+                    } else if (r < a.n * a.G) {
+                        const float v = L[c] == 0.0f || rowinfo[row].x < 0 ? 0.0f : o * KV4_STEP / L[c];
+                        const size_t at_o = (((size_t)b * a.n + i) * a.Hq + h * a.G + r % a.G) * D + d;
+                        if (F32)
+                            reinterpret_cast<float *>(a.out)[at_o] = v;
+                        else
+                            reinterpret_cast<__nv_bfloat16 *>(a.out)[at_o] = __float2bfloat16_rn(v);
+                    }
+                }
+            }
+            if (warp == 0 && g == 0) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int row = nt * 8 + 2 * t + c, r = rt * R + row, i = r / a.G;
+                    if (!whole) {
+                        slot[R * D + row] = M[c];
+                        slot[R * D + R + row] = L[c];
+                    } else if (a.lse && r < a.n * a.G) {
+                        a.lse[((size_t)b * a.n + i) * a.Hq + h * a.G + r % a.G] =
+                            L[c] == 0.0f || rowinfo[row].x < 0 ? -INFINITY : (M[c] + log2f(L[c])) * 0.6931471805599453f;
+                    }
+                }
+            }
+            __syncthreads();  // before the next rows' sums, the next segment's row infos and its maxima
+        }
+        first = false;
+        if (left == 0) break;
+        e = ne, h = nh, x0 = 0, x1 = nx1, mine = nmine, key = nkey;
+    }
+    if (tid == 0 && any_timeout) ws.info[blockIdx.x].timeout = 1;
+}
+
+// Adds the pieces of an item that several CTAs share, in their order: block c
+// takes the item in which the range of CTA c starts, when c is the first to
+// start inside it.  Block 0 writes the sequences' status.
+constexpr int JT_THREADS = 256;
+template <bool F32>
+__global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R) {
+    __shared__ int late;
+    const int tid = threadIdx.x, c = blockIdx.x, D = a.D;
+    pdl_wait();
+    if (c == 0) {
+        if (tid == 0) late = 0;
+        __syncthreads();
+        for (int x = tid; x < C; x += JT_THREADS)
+            if (ws.info[x].timeout) late = 1;
+        __syncthreads();
+        for (int b = tid; b < a.B; b += JT_THREADS)
+            a.status[b] = (kv4_seq(a.prefix, a.count, b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE) | (late ? ACES_ROW_TIMEOUT : 0);
+        return;
+    }
+    const Kv4Info in = ws.info[c];
+    if (!in.valid || in.off == 0 || in.off > in.quantum) return;
+    const int pieces = 1 + (in.units - in.off + in.quantum - 1) / in.quantum;
+    const int s0 = 2 * (c - 1) + (in.off == in.quantum ? 0 : 1);
+    const size_t stride = (size_t)R * (D + 2);
+    auto piece = [&](int p) { return ws.piece + (p == 0 ? s0 : 2 * (c - 1 + p)) * stride; };
+    const int D4 = D / 4;
+    const Kv4Seq sq = kv4_seq(a.prefix, a.count, in.b, a.n, a.S);
+    for (int x = blockIdx.y * JT_THREADS + tid; x < R * D4; x += JT_THREADS * gridDim.y) {
+        const int row = x / D4, d4 = x % D4;
+        const long long r = (long long)in.rt * R + row;
+        if (r >= (long long)a.n * a.G) break;
+        const int i = (int)(r / a.G);
+        float M = -INFINITY;
+        for (int p = 0; p < pieces; ++p) M = fmaxf(M, piece(p)[R * D + row]);
+        const float ref = M == -INFINITY ? 0.0f : M;
+        float L = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int p = 0; p < pieces; ++p) {
+            const float *pc = piece(p);
+            const float f = ex2(pc[R * D + row] - ref);
+            const float4 v = *reinterpret_cast<const float4 *>(pc + row * D + 4 * d4);
+            L = fmaf(pc[R * D + R + row], f, L);
+            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+        }
+        const bool none = L == 0.0f || !sq.ok || i >= sq.cnt;
+        const float k = none ? 0.0f : KV4_STEP / L;
+        if (none) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const size_t orow = ((size_t)in.b * a.n + i) * a.Hq + in.h * a.G + r % a.G;
+        if (F32) {
+            reinterpret_cast<float4 *>(a.out)[orow * D4 + d4] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
+        } else {
+            reinterpret_cast<uint2 *>(a.out)[orow * D4 + d4] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
+        }
+        if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+}
+
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
+    return a.f32 ? launch_after(k_kv4_join<true>, C, JT_THREADS, 1, s, a, ws, C, R)
+                 : launch_after(k_kv4_join<false>, C, JT_THREADS, 1, s, a, ws, C, R);
+}
+
+template <int D, bool F32, int NT>
+static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
+    using C = Few<D, F32, NT>;
+    const int grid = nsm * C::MINB;
+    const Kv4Ws ws = kv4_ws_carve(workspace, grid);
+    cudaError_t e = cudaFuncSetAttribute(k_kv4_few<D, F32, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
+    k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT);
+    e = cudaGetLastError();
+    return e != cudaSuccess ? e : launch_kv4_join(a, ws, grid, C::R, s);
+}
+
+// Rows of a tile: 8 when a head's rows fit (or float32 has few), else 16.
+static int few_tiles(int n, int G) { return (long long)n * G <= 8 ? 1 : 2; }
+
+size_t kv4_few_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(2 * nsm, 8 * few_tiles(n, G), D); }
+
+cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
+    const bool one = few_tiles(a.n, a.G) == 1;
+    if (a.D == 64)
+        return a.f32 ? (one ? run_few<64, true, 1>(a, workspace, nsm, s) : run_few<64, true, 2>(a, workspace, nsm, s))
+                     : (one ? run_few<64, false, 1>(a, workspace, nsm, s) : run_few<64, false, 2>(a, workspace, nsm, s));
+    return a.f32 ? (one ? run_few<128, true, 1>(a, workspace, nsm, s) : run_few<128, true, 2>(a, workspace, nsm, s))
+                 : (one ? run_few<128, false, 1>(a, workspace, nsm, s) : run_few<128, false, 2>(a, workspace, nsm, s));
+}
+
+size_t kv4_attention_ws(int B, int n, int Hq, int H, int D) { return kv4_few_ws(n, Hq / H, D, sm_count()); }
+cudaError_t launch_kv4_attention(const Kv4Att &a, void *workspace, cudaStream_t s) {
+    return launch_kv4_few(a, workspace, sm_count(), s);
+}
+
+#ifdef ACES_CHECKED
+cudaError_t check_take_kv4_attend(unsigned long long out[3]) { return check_take(out); }
+#endif
+
+}  // namespace aces

@@ -1,0 +1,207 @@
+// How the attention kernels share their work out (both read kv4.cuh's arguments).
+//
+// An item is one tile of R query rows (row r = token r / G, head r % G of the
+// group) of one sequence and key head; its keys are cut into tiles, and some
+// tiles are a unit.  The sequences' lengths lie on the device, so every CTA
+// counts the units of all items itself (one thread an entry (b, row tile), all
+// of whose heads have the same) and takes the units [c Q, (c + 1) Q), Q the
+// whole number that spreads them over the grid: CTAs are equally long whatever
+// the lengths.  An item inside one CTA's range is written out by it; the pieces
+// of one that several share go to the workspace as sums not yet divided,
+// with their reference maximum, and k_kv4_join adds them in the CTAs' order.
+#pragma once
+#include "kv4.cuh"
+
+namespace aces {
+
+struct Kv4Info {  // of the item in which a CTA's range starts
+    int b, rt, h, off, units, quantum;
+    int valid, timeout;
+};
+static_assert(sizeof(Kv4Info) == 32, "Kv4Info layout");
+
+// Workspace: Kv4Info[C], then 2 C pieces of R * (D + 2) floats (a CTA's first
+// piece and its last).
+struct Kv4Ws {
+    Kv4Info *info;
+    float *piece;
+};
+inline size_t kv4_ws_bytes(int C, int R, int D) { return sizeof(Kv4Info) * (size_t)C + (size_t)2 * C * R * (D + 2) * 4; }
+inline Kv4Ws kv4_ws_carve(void *p, int C) {
+    Kv4Ws w;
+    w.info = reinterpret_cast<Kv4Info *>(p);
+    w.piece = reinterpret_cast<float *>(w.info + C);
+    return w;
+}
+
+// Keys of one row tile of one sequence: those below s_hi (the first tokens
+// that stay visible) and [lo, hi), in tiles of KT.
+struct Kv4Keys {
+    int P, cnt, i0, i1;    // tokens [i0, i1]
+    int lo, hi, s_hi;
+    int st, mt0, tiles, units;
+    bool live;
+};
+
+template <int KT, int R, int TPU>
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int b, int rt) {
+    Kv4Keys k;
+    const Kv4Seq sq = kv4_seq(a.prefix, a.count, b, a.n, a.S);
+    k.P = sq.P, k.cnt = sq.cnt;
+    const long long r0 = (long long)rt * R, r1 = min(r0 + R, (long long)a.n * a.G);
+    k.i0 = (int)(r0 / a.G);
+    k.i1 = min((int)((r1 - 1) / a.G), sq.cnt - 1);
+    k.live = sq.ok && k.i0 < sq.cnt;
+    k.lo = k.hi = k.s_hi = k.st = k.mt0 = k.tiles = 0;
+    if (k.live) {
+        k.hi = k.P + (a.mask ? k.cnt : k.i1 + 1);
+        k.lo = a.window ? max(0, k.P + (a.mask ? 0 : k.i0) - a.window + 1) : 0;
+        k.s_hi = min(a.sinks, k.lo);
+        k.st = (k.s_hi + KT - 1) / KT;
+        k.mt0 = max(k.lo / KT, k.st);
+        k.tiles = k.st + max(0, (k.hi + KT - 1) / KT - k.mt0);
+    }
+    k.units = max(1, (k.tiles + TPU - 1) / TPU);
+    return k;
+}
+// first key of the x-th tile
+template <int KT>
+__device__ __forceinline__ int kv4_tile(const Kv4Keys &k, int x) {
+    return (x < k.st ? x : k.mt0 + x - k.st) * KT;
+}
+
+// Whether new or old position j is seen by token i at position pos.
+__device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end, int j, int i, int pos) {
+    if (j >= end) return false;
+    int kp = j;
+    if (j >= P) {
+        const int t = j - P;
+        if (a.mask) {
+            if (!((__ldg(a.mask + b * a.mask_b + (size_t)i * a.words + (t >> 5)) >> (t & 31)) & 1u)) return false;
+            kp = kv4_pos(P, a.depth + b * a.depth_b, t);
+        } else if (t > i) {
+            return false;
+        }
+    }
+    return !a.window || kp > pos - a.window || kp < a.sinks;
+}
+
+// A CTA's range and the item it starts in, by all NTH threads.
+struct Kv4Start {
+    unsigned long long left;  // units to do
+    int quantum, e, h, off;
+};
+template <int KT, int R, int TPU, int NTH>
+__device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int RT) {
+    __shared__ unsigned long long red[NTH / 32];
+    __shared__ int found[3];
+    const int E = a.B * RT, per = (E + NTH - 1) / NTH;
+    const int e0 = min(E, (int)threadIdx.x * per), e1 = min(E, e0 + per);
+    unsigned long long sum = 0, total;
+    for (int e = e0; e < e1; ++e) sum += (unsigned long long)kv4_keys<KT, R, TPU>(a, e / RT, e % RT).units * a.H;
+    unsigned long long at = block_exscan_n<NTH>(sum, red, &total);
+    const unsigned long long Q = (total + gridDim.x - 1) / gridDim.x, w0 = Q * blockIdx.x;
+    if (w0 >= at && w0 < at + sum) {
+        for (int e = e0; e < e1; ++e) {
+            const unsigned u = (unsigned)kv4_keys<KT, R, TPU>(a, e / RT, e % RT).units;
+            if (w0 < at + (unsigned long long)u * a.H) {
+                const unsigned x = (unsigned)(w0 - at);
+                found[0] = e;
+                found[1] = (int)(x / u);
+                found[2] = (int)(x % u);
+                break;
+            }
+            at += (unsigned long long)u * a.H;
+        }
+    }
+    __syncthreads();
+    Kv4Start s;
+    s.left = w0 < total ? min(Q, total - w0) : 0;
+    s.quantum = (int)Q;
+    s.e = found[0], s.h = found[1], s.off = found[2];
+    return s;
+}
+
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
+int kv4_few_grid(const Kv4Att &a, int nsm);
+cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
+
+// ---------------------------------------------------------------------------
+// mbarriers and bulk copies
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
+}
+// Waits for a phase; gives up after two seconds (nothing it waits for takes a
+// thousandth of that), so a mistake ends as a status and not as a hang.
+constexpr unsigned long long KV4_WAIT_NS = 2000000000ull;
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+    const unsigned long long t0 = globaltimer_ns();
+    while (!mbar_try(bar, parity))
+        if (globaltimer_ns() - t0 > KV4_WAIT_NS) return false;
+    return true;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 16; ++i)
+        if (mbar_try(bar, parity)) return true;
+    return mbar_wait_slow(bar, parity);
+}
+// global -> shared, 16-byte aligned, a multiple of 16 bytes
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// codes -> bfloat16 pairs
+__device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+// -24 t of two t's (exact: two and five significant bits)
+__device__ __forceinline__ uint32_t kv4_offset(uint32_t t2) { return bf2_fma(t2, 0xC1C0C1C0u, 0x80008000u); }
+// Four pairs of values from a word whose halves hold four codes each, pair j
+// the codes at bits 4 j: a code at bits 3..6 of 16.0 makes 16 + c, and (16 + c)
+// t - 24 t = (c - 8) t is exact.
+__device__ __forceinline__ void kv4_pairs(uint32_t w, uint32_t t2, uint32_t off, uint32_t (&p)[4]) {
+    p[0] = bf2_fma(((w << 3) & 0x00780078u) | 0x41804180u, t2, off);
+    p[1] = bf2_fma(((w >> 1) & 0x00780078u) | 0x41804180u, t2, off);
+    p[2] = bf2_fma(((w >> 5) & 0x00780078u) | 0x41804180u, t2, off);
+    p[3] = bf2_fma(((w >> 9) & 0x00780078u) | 0x41804180u, t2, off);
+}
+// bfloat16 pair with infinities made NaN, so a query that is not finite spoils
+// its row whatever the keys' signs
+__device__ __forceinline__ uint32_t bf2_poison(uint32_t x) {
+    if ((x & 0x7F80u) == 0x7F80u) x |= 0x40u;
+    if ((x & 0x7F800000u) == 0x7F800000u) x |= 0x400000u;
+    return x;
+}
+// low half from a, high half from b, rounded to nearest even
+__device__ __forceinline__ uint32_t bf2_pack(float a, float b) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+    return d;
+}
+__device__ __forceinline__ float bf_lo(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+
+}  // namespace aces

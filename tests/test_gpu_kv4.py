@@ -7,7 +7,8 @@ attention every product with a cache value is exact and what rounds is:
     scale * sum |q| |k| (some 2^-23 for each of the sum's partial sums);
     twice that, relative, in a weight and in the sum of the weights;
   - the weights' exponentials and sums, and their products' sums: 2^-17;
-  - bfloat16 queries: the weights' rounding, 2^-9, and the result's, 2^-9.
+  - bfloat16 queries: the weights' rounding, 2^-8, and the result's, 2^-8 (half
+    a unit of eight significant bits is up to 2^-8 of the number).
 All are relative to A = sum of the weights times |v| of the output's channel.
 """
 import numpy as np
@@ -183,7 +184,7 @@ def _compare(r, q, K, V, P, cnt, dtype, scale, mask=None, depth=None, window=0, 
         for hq in range(Hq):
             h = hq // (Hq // H)
             w, z, mag, M = O.attend(q[b, :, hq], K[b, h, :top], V[b, h, :top], ok, scale)
-            rel = 4 * 2.0 ** -20 * (M + 1) + 2.0 ** -17 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+            rel = 4 * 2.0 ** -20 * (M + 1) + 2.0 ** -17 + (2.0 ** -7 if dtype == "bf16" else 0.0)
             off = np.abs(out[b, :, hq] - w)
             assert (off <= rel[:, None] * mag + 1e-30).all(), (b, hq, float((off / (rel[:, None] * mag + 1e-30)).max()))
             seen = np.isfinite(z)
