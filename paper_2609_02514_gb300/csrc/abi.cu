@@ -410,7 +410,7 @@ extern "C" aces_status aces_checked_violation(unsigned long long out[3]) {
     if (cudaDeviceSynchronize() != cudaSuccess) return ACES_ERR_CUDA;
     cudaError_t (*take[])(unsigned long long *) = {check_take_rows_cap, check_take_rows_general,
                                                    check_take_cache, check_take_resample, check_take_kv,
-                                                   check_take_mask, check_take_kv4_rows, check_take_kv4_attend};
+                                                   check_take_mask, check_take_kv4_rows, check_take_kv4_few, check_take_kv4_many};
     out[0] = out[1] = out[2] = 0ull;
     for (auto f : take) {
         unsigned long long w[3];

@@ -48,7 +48,8 @@ cudaError_t check_take_resample(unsigned long long out[3]);
 cudaError_t check_take_kv(unsigned long long out[3]);
 cudaError_t check_take_mask(unsigned long long out[3]);
 cudaError_t check_take_kv4_rows(unsigned long long out[3]);
-cudaError_t check_take_kv4_attend(unsigned long long out[3]);
+cudaError_t check_take_kv4_few(unsigned long long out[3]);
+cudaError_t check_take_kv4_many(unsigned long long out[3]);
 #else
 #define ACES_IN(i, n) true
 #endif

@@ -88,9 +88,6 @@ struct Kv4Att {
     float scale;           // of q . k, in log2 units, times KV4_STEP
 };
 
-cudaError_t launch_kv4_attention(const Kv4Att &a, void *workspace, cudaStream_t s);
-size_t kv4_attention_ws(int B, int n, int Hq, int H, int D);
-
 struct Kv4Rows {
     uint8_t *k, *v;                        // the layer's planes
     void *xk, *xv;                         // [B, n, H, D] numbers

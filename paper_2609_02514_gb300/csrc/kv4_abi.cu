@@ -2,7 +2,7 @@
 #include <climits>
 #include <cmath>
 
-#include "kv4.cuh"
+#include "kv4_plan.cuh"
 
 using namespace aces;
 
@@ -39,6 +39,10 @@ aces_status check_rows(const void *k, const void *v, aces_dtype dt, const int32_
     if ((uintptr_t)k % es || (uintptr_t)v % es) return ACES_ERR_INVALID_ARG;
     return ACES_OK;
 }
+
+// Which kernel: bfloat16 queries of more than 16 rows a key head go to the
+// tcgen05 kernel, the others to the one that keeps its few rows in registers.
+bool many_rows(int f32, int n, int G) { return !f32 && (long long)n * G > 16; }
 
 }  // namespace
 
@@ -92,7 +96,9 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
 size_t aces_kv4_workspace_bytes(int B, int n, int Hq, int H, int D) {
     if (B < 1 || n < 1 || H < 1 || Hq < H || Hq % H != 0 || (D != 64 && D != 128)) return 0;
     if ((long long)B * n > INT_MAX / 2 || (long long)B * n * Hq > INT_MAX / 2) return 0;
-    return kv4_attention_ws(B, n, Hq, H, D);
+    const int G = Hq / H, nsm = sm_count();  // of either type
+    const size_t few = kv4_few_ws(n, G, D, nsm), many = many_rows(0, n, G) ? kv4_many_ws(n, G, D, nsm) : 0;
+    return few > many ? few : many;
 }
 
 aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_strides, const void *cache, int planes,
@@ -128,7 +134,8 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
     a.scale = (float)((double)scale * 1.4426950408889634 * (double)KV4_STEP);
-    return launch_kv4_attention(a, workspace, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
+    const auto launch = many_rows(a.f32, n, a.G) ? launch_kv4_many : launch_kv4_few;
+    return launch(a, workspace, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
 }
 
 }  // extern "C"

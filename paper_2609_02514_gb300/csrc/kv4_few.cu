@@ -66,49 +66,37 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (tid == 0) any_timeout = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
-    Kv4Start at = kv4_start<FKT, R, FW, FT>(a, RT);  // has a __syncthreads after the barriers' start
-    int e = at.e, h = at.h, x0 = at.off;
-    if (tid == 0) {
-        Kv4Info in;
-        in.valid = at.left > 0;
-        in.timeout = 0;
-        in.quantum = at.quantum;
-        in.b = in.rt = in.h = in.off = in.units = 0;
-        if (in.valid) {
-            in.b = e / RT, in.rt = e % RT, in.h = h, in.off = x0;
-            in.units = kv4_keys<FKT, R, FW>(a, in.b, in.rt).units;
-        }
-        ws.info[blockIdx.x] = in;
-    }
-    if (at.left == 0) return;
-    unsigned long long left = at.left;
-    Kv4Keys key = kv4_keys<FKT, R, FW>(a, e / RT, e % RT);
-    int x1 = (int)min((unsigned long long)key.units, x0 + left);
+    using Seg = Kv4Seg<FKT, FW>;
+    const Kv4Start at = kv4_start<FKT, FW, FT>(a, R, RT);  // has a __syncthreads after the barriers' start
+    if (tid == 0) kv4_put_info<FKT, FW>(a, ws, at, R, RT);
+    Seg cur;
+    if (!cur.start(a, R, RT, at)) return;
 
     int seq = 0;       // tiles this warp has taken, of all segments
     bool bad = false;  // a wait gave up
     // this warp's y-th tile of the segment, into the ring's next place
-    auto issue = [&](const Kv4Keys &k, int b, int hh, int tile, int place) {
+    auto issue = [&](const Seg &g, int y, int place) {
         if (lane != 0) return;
-        const int j0 = kv4_tile<FKT>(k, tile), rows = min(FKT, k.P + k.cnt - j0);
+        const int j0 = kv4_tile<FKT>(g.key, (g.x0 + y) * FW + warp), rows = min(FKT, g.key.P + g.key.cnt - j0);
         if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
         const int s = place % ST;
         const uint32_t bytes = rows * RB, dst = ring + s * C::STAGE;
-        const size_t off = ((size_t)((size_t)b * a.H + hh) * a.S + j0) * RB;
+        const size_t off = ((size_t)((size_t)(g.e / RT) * a.H + g.h) * a.S + j0) * RB;
         mbar_expect(bar0 + 8 * s, 2 * bytes);
         bulk_load(dst, a.k + off, bytes, bar0 + 8 * s);
         bulk_load(dst + FKT * RB, a.v + off, bytes, bar0 + 8 * s);
     };
-    auto my_tiles = [&](const Kv4Keys &k, int u0, int u1) {
-        const int top = min(u1 * FW, k.tiles) - u0 * FW - warp;
+    auto my_tiles = [&](const Seg &g) {
+        const int top = min(g.x1 * FW, g.key.tiles) - g.x0 * FW - warp;
         return top > 0 ? (top + FW - 1) / FW : 0;
     };
-    int mine = my_tiles(key, x0, x1);
-    for (int y = 0; y < min(ST, mine); ++y) issue(key, e / RT, h, (x0 + y) * FW + warp, seq + y);
+    int mine = my_tiles(cur);
+    for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
 
     bool first = true;
     while (true) {
-        const int b = e / RT, rt = e % RT, P = key.P, end = P + key.cnt;
+        const Kv4Keys key = cur.key;
+        const int b = cur.e / RT, rt = cur.e % RT, h = cur.h, P = key.P, end = P + key.cnt;
         // the segment's query rows
         if (tid < R) {
             const int r = rt * R + tid, i = r / a.G;
@@ -182,7 +170,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
             const int s = seq % ST;
             if (!bad && !mbar_wait(bar0 + 8 * s, (seq / ST) & 1)) bad = true;
             const uint8_t *kt = ringp + s * C::STAGE, *vt = kt + FKT * RB;
-            const int j0 = kv4_tile<FKT>(key, (x0 + y) * FW + warp);
+            const int j0 = kv4_tile<FKT>(key, (cur.x0 + y) * FW + warp);
             float S[NT][2][4];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
@@ -334,22 +322,13 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 }
             }
             __syncwarp();
-            if (y + ST < mine) issue(key, b, h, (x0 + y + ST) * FW + warp, seq + ST);
+            if (y + ST < mine) issue(cur, y + ST, seq + ST);
         }
         // the next segment, whose first tiles are on their way while this one is merged
-        const bool whole = x0 == 0 && x1 == key.units;
-        left -= x1 - x0;
-        int ne = e, nh = h + 1, nx1 = 0, nmine = 0;
-        Kv4Keys nkey = key;
-        if (left > 0) {
-            if (nh == a.H) {
-                nh = 0, ++ne;
-                nkey = kv4_keys<FKT, R, FW>(a, ne / RT, ne % RT);
-            }
-            nx1 = (int)min((unsigned long long)nkey.units, left);
-            nmine = my_tiles(nkey, 0, nx1);
-            for (int y = 0; y < min(ST, nmine); ++y) issue(nkey, ne / RT, nh, y * FW + warp, seq + y);
-        }
+        const bool whole = cur.whole();
+        const bool more = cur.next(a, R, RT);
+        mine = more ? my_tiles(cur) : 0;
+        for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
         // merge the warps
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -418,8 +397,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
             __syncthreads();  // before the next rows' sums, the next segment's row infos and its maxima
         }
         first = false;
-        if (left == 0) break;
-        e = ne, h = nh, x0 = 0, x1 = nx1, mine = nmine, key = nkey;
+        if (!more) break;
     }
     if (tid == 0 && any_timeout) ws.info[blockIdx.x].timeout = 1;
 }
@@ -429,11 +407,12 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // start inside it.  Block 0 writes the sequences' status.
 constexpr int JT_THREADS = 256;
 template <bool F32>
-__global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R) {
+__global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
     __shared__ int late;
-    const int tid = threadIdx.x, c = blockIdx.x, D = a.D;
+    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, D = a.D;
     pdl_wait();
     if (c == 0) {
+        if (y != 0) return;
         if (tid == 0) late = 0;
         __syncthreads();
         for (int x = tid; x < C; x += JT_THREADS)
@@ -451,7 +430,7 @@ __global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int
     auto piece = [&](int p) { return ws.piece + (p == 0 ? s0 : 2 * (c - 1 + p)) * stride; };
     const int D4 = D / 4;
     const Kv4Seq sq = kv4_seq(a.prefix, a.count, in.b, a.n, a.S);
-    for (int x = blockIdx.y * JT_THREADS + tid; x < R * D4; x += JT_THREADS * gridDim.y) {
+    for (int x = y * JT_THREADS + tid; x < R * D4; x += JT_THREADS * Y) {
         const int row = x / D4, d4 = x % D4;
         const long long r = (long long)in.rt * R + row;
         if (r >= (long long)a.n * a.G) break;
@@ -483,8 +462,10 @@ __global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int
 }
 
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
-    return a.f32 ? launch_after(k_kv4_join<true>, C, JT_THREADS, 1, s, a, ws, C, R)
-                 : launch_after(k_kv4_join<false>, C, JT_THREADS, 1, s, a, ws, C, R);
+    const long long rows = (long long)a.n * a.G < R ? (long long)a.n * a.G : R;
+    const int Y = (int)((rows * (a.D / 4) + JT_THREADS - 1) / JT_THREADS);  // blocks of an item: four numbers a thread
+    return a.f32 ? launch_after(k_kv4_join<true>, C * Y, JT_THREADS, 1, s, a, ws, C, R, Y)
+                 : launch_after(k_kv4_join<false>, C * Y, JT_THREADS, 1, s, a, ws, C, R, Y);
 }
 
 template <int D, bool F32, int NT>
@@ -514,13 +495,8 @@ cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
                  : (one ? run_few<128, false, 1>(a, workspace, nsm, s) : run_few<128, false, 2>(a, workspace, nsm, s));
 }
 
-size_t kv4_attention_ws(int B, int n, int Hq, int H, int D) { return kv4_few_ws(n, Hq / H, D, sm_count()); }
-cudaError_t launch_kv4_attention(const Kv4Att &a, void *workspace, cudaStream_t s) {
-    return launch_kv4_few(a, workspace, sm_count(), s);
-}
-
 #ifdef ACES_CHECKED
-cudaError_t check_take_kv4_attend(unsigned long long out[3]) { return check_take(out); }
+cudaError_t check_take_kv4_few(unsigned long long out[3]) { return check_take(out); }
 #endif
 
 }  // namespace aces

@@ -43,8 +43,8 @@ struct Kv4Keys {
     bool live;
 };
 
-template <int KT, int R, int TPU>
-__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int b, int rt) {
+template <int KT, int TPU>
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int rt) {
     Kv4Keys k;
     const Kv4Seq sq = kv4_seq(a.prefix, a.count, b, a.n, a.S);
     k.P = sq.P, k.cnt = sq.cnt;
@@ -91,19 +91,19 @@ struct Kv4Start {
     unsigned long long left;  // units to do
     int quantum, e, h, off;
 };
-template <int KT, int R, int TPU, int NTH>
-__device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int RT) {
+template <int KT, int TPU, int NTH>
+__device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     __shared__ unsigned long long red[NTH / 32];
     __shared__ int found[3];
     const int E = a.B * RT, per = (E + NTH - 1) / NTH;
     const int e0 = min(E, (int)threadIdx.x * per), e1 = min(E, e0 + per);
     unsigned long long sum = 0, total;
-    for (int e = e0; e < e1; ++e) sum += (unsigned long long)kv4_keys<KT, R, TPU>(a, e / RT, e % RT).units * a.H;
+    for (int e = e0; e < e1; ++e) sum += (unsigned long long)kv4_keys<KT, TPU>(a, R, e / RT, e % RT).units * a.H;
     unsigned long long at = block_exscan_n<NTH>(sum, red, &total);
     const unsigned long long Q = (total + gridDim.x - 1) / gridDim.x, w0 = Q * blockIdx.x;
     if (w0 >= at && w0 < at + sum) {
         for (int e = e0; e < e1; ++e) {
-            const unsigned u = (unsigned)kv4_keys<KT, R, TPU>(a, e / RT, e % RT).units;
+            const unsigned u = (unsigned)kv4_keys<KT, TPU>(a, R, e / RT, e % RT).units;
             if (w0 < at + (unsigned long long)u * a.H) {
                 const unsigned x = (unsigned)(w0 - at);
                 found[0] = e;
@@ -122,9 +122,56 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int RT) {
     return s;
 }
 
+// writes the info of the CTA's start (one thread)
+template <int KT, int TPU>
+__device__ __forceinline__ void kv4_put_info(const Kv4Att &a, const Kv4Ws &ws, const Kv4Start &at, int R, int RT) {
+    Kv4Info in;
+    in.valid = at.left > 0;
+    in.timeout = 0;
+    in.quantum = at.quantum;
+    in.b = in.rt = in.h = in.off = in.units = 0;
+    if (in.valid) {
+        in.b = at.e / RT, in.rt = at.e % RT, in.h = at.h, in.off = at.off;
+        in.units = kv4_keys<KT, TPU>(a, R, in.b, in.rt).units;
+    }
+    ws.info[blockIdx.x] = in;
+}
+
+// A CTA's segments, one after another: units [x0, x1) of an item.
+template <int KT, int TPU>
+struct Kv4Seg {
+    unsigned long long left;  // units after this segment
+    int e, h, x0, x1;
+    Kv4Keys key;
+    __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
+        e = at.e, h = at.h, x0 = at.off, left = at.left;
+        if (left == 0) return false;
+        key = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+        take();
+        return true;
+    }
+    __device__ __forceinline__ bool next(const Kv4Att &a, int R, int RT) {
+        if (left == 0) return false;
+        if (++h == a.H) {
+            h = 0, ++e;
+            key = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+        }
+        x0 = 0;
+        take();
+        return true;
+    }
+    __device__ __forceinline__ void take() {
+        x1 = (int)min((unsigned long long)key.units, x0 + left);
+        left -= x1 - x0;
+    }
+    __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == key.units; }
+};
+
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
-int kv4_few_grid(const Kv4Att &a, int nsm);
+size_t kv4_few_ws(int n, int G, int D, int nsm);
 cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
+size_t kv4_many_ws(int n, int G, int D, int nsm);
+cudaError_t launch_kv4_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
 
 // ---------------------------------------------------------------------------
 // mbarriers and bulk copies
