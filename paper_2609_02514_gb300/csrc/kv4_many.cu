@@ -9,14 +9,14 @@
 //     memory.  With more than 128 rows the groups have a half each and share
 //     the tiles; with up to 128 both have the same rows and every other tile,
 //     and are merged at the end.
-//   - eight warps turn the rows' codes into bfloat16 tiles in shared memory, in
+//   - seven warps turn the rows' codes into bfloat16 tiles in shared memory, in
 //     the 128-byte swizzle.  Keys and values lie alike ([key][64 channels] a
 //     half): the keys' product reads them along the channels, the values' along
 //     the keys (the transposed form of the second operand).
 //   - one thread issues the products: S = Q K' (both from shared memory), O += P
 //     V (P from TMEM).  While one group turns its scores into weights the
 //     other's products run.
-// P takes the place of S (D = 128): the products of both have one shape, so the
+// P takes half the place of S (D = 128): the products of both have one shape, so the
 // tensor pipe runs them in the order they were issued.  For D = 64 the shapes
 // differ and P has columns of its own.
 // Sums are rescaled only when a row's maximum grew by more than 2^8 (in the
@@ -31,15 +31,13 @@
 namespace aces {
 
 constexpr int MKT = 128;                  // keys of a tile
-constexpr int MSM = 8, MDQ = 8;           // softmax and dequantising warps
-constexpr int MT = (MSM + MDQ + 1) * 32;  // and the one that issues
+constexpr int MSM = 8, MDQ = 7;           // softmax and dequantising warps
+constexpr int MT = (MSM + MDQ + 1) * 32;  // and the one that issues: 16 warps of 128 registers
 constexpr int MDT = MDQ * 32;
 constexpr float M_LAZY = 8.0f;
-
 // -- tcgen05 ------------------------------------------------------------------
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -61,29 +59,35 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
 }
 // 32 columns of this warp's 32 rows
 __device__ __forceinline__ void tc_ld32(uint32_t addr, float (&v)[32]) {
-    uint32_t r[32];
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
         "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
         : "r"(addr));
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const float (&v)[32]) {
+// The loads before it are done.  The numbers pass through it, so nothing that
+// uses them comes before.
+__device__ __forceinline__ void tc_wait_ld(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                   "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]),
+                   "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]),
+                   "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t addr, float (&v)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"f"(v[0]),
-        "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]),
-        "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]),
-        "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]),
-        "r"(addr)
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tc_wait_ld(float (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
+                 :
+                 : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -116,6 +120,12 @@ __device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
     asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tadd.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
         : "+f"(x), "+f"(y)
         : "f"(a), "f"(b));
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // bits [lo, hi) of the word of positions [w0, w0 + 32)
@@ -151,8 +161,10 @@ struct Many {
     static constexpr int HALF = MKT * 128;                 // 128 rows of 64 channels
     static constexpr int TILE = MKT * D * 2;
     static constexpr int SMEM = 6 * TILE + 1024;           // queries of two groups, two stages of keys and values
-    static constexpr int PC = MKT * D / 32 / MDT;          // 16-byte pieces a thread dequantises of a tile
-    static constexpr int TS = 0, TO = 256, TP = D == 128 ? 0 : 384, TPX = D == 128 ? 128 : 64;  // TMEM columns
+    static constexpr int PIECES = MKT * D / 32;            // 16-byte pieces of a tile's codes
+    static constexpr int PC = (PIECES + MDT - 1) / MDT;    // that a thread dequantises (a warp's last may be none)
+    static_assert(PIECES % 32 == 0, "whole warps");
+    static constexpr int TS = 0, TO = 256, TP = D == 128 ? 64 : 384, TPX = D == 128 ? 128 : 64;  // TMEM columns
 };
 
 // Byte of 16-byte chunk c (eight channels) of a row in a swizzled tile.
@@ -164,22 +176,20 @@ struct Piece {  // 32 channels of a row and their t's
     uint32_t t[D == 128 ? 1 : 2];
 };
 
+// Without a branch and without a use, so a thread's loads are all under way at
+// once.  Rows past the sequence are its last one again: their weights are 0.
 template <int D>
 __device__ __forceinline__ void load_piece(const uint8_t *plane, size_t row0, int j0, int end, int p, Piece<D> &o) {
     constexpr int RB = Many<D>::RB, Q = D / 32;
-    const int row = p / Q, q = p % Q;
-    o.w = make_uint4(0u, 0u, 0u, 0u);
-    o.t[0] = 0u;
-    if (D == 64) o.t[D == 128 ? 0 : 1] = 0u;
-    if (j0 + row >= end) return;  // past the sequence: zeros
-    const uint8_t *r = plane + (row0 + j0 + row) * RB;
+    const int q = p % Q;
+    const uint8_t *r = plane + (row0 + min(j0 + p / Q, end - 1)) * RB;
     o.w = __ldg(reinterpret_cast<const uint4 *>(r) + q);
     if (D == 128) {
-        o.t[0] = __ldg(reinterpret_cast<const uint32_t *>(r + D / 2) + q) & KV4_T_MASK;
+        o.t[0] = __ldg(reinterpret_cast<const uint32_t *>(r + D / 2) + q);
     } else {
         const uint2 v = __ldg(reinterpret_cast<const uint2 *>(r + D / 2) + q);
-        o.t[0] = v.x & KV4_T_MASK;
-        o.t[D == 128 ? 0 : 1] = v.y & KV4_T_MASK;
+        o.t[0] = v.x;
+        o.t[D == 128 ? 0 : 1] = v.y;
     }
 }
 
@@ -188,10 +198,11 @@ __device__ __forceinline__ void store_piece(uint8_t *tile, int p, const Piece<D>
     constexpr int Q = D / 32;
     const int row = p / Q, q = p % Q;
     uint32_t w[4] = {o.w.x, o.w.y, o.w.z, o.w.w}, tt[4];
+    const uint32_t t0 = o.t[0] & KV4_T_MASK, t1 = o.t[D == 128 ? 0 : 1] & KV4_T_MASK;
     int flip = 0;
     if (D == 128) {
-        tt[0] = tt[1] = __byte_perm(o.t[0], 0, 0x1010);
-        tt[2] = tt[3] = __byte_perm(o.t[0], 0, 0x3232);
+        tt[0] = tt[1] = __byte_perm(t0, 0, 0x1010);
+        tt[2] = tt[3] = __byte_perm(t0, 0, 0x3232);
         // eight lanes have two rows; the rows' upper halves, 16 KB further, fall on
         // the same banks, so they go in another order
         flip = q & 2;
@@ -202,10 +213,10 @@ __device__ __forceinline__ void store_piece(uint8_t *tile, int p, const Piece<D>
             x = tt[0], tt[0] = tt[1] = tt[2], tt[2] = tt[3] = x;
         }
     } else {
-        tt[0] = __byte_perm(o.t[0], 0, 0x1010);
-        tt[1] = __byte_perm(o.t[0], 0, 0x3232);
-        tt[2] = __byte_perm(o.t[D == 128 ? 0 : 1], 0, 0x1010);
-        tt[3] = __byte_perm(o.t[D == 128 ? 0 : 1], 0, 0x3232);
+        tt[0] = __byte_perm(t0, 0, 0x1010);
+        tt[1] = __byte_perm(t0, 0, 0x3232);
+        tt[2] = __byte_perm(t1, 0, 0x1010);
+        tt[3] = __byte_perm(t1, 0, 0x3232);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -279,12 +290,12 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             const int b = seg.e / RT, rt = seg.e % RT, h = seg.h, P = key.P;
             const bool single = NR - (long long)rt * R <= 128;
             const int slot_row = single ? row : x * 128 + row;
-            const long long r = (long long)rt * R + slot_row;
-            const int i = (int)(r / a.G), gq = (int)(r % a.G);
-            const bool live = r < NR && key.live && i < key.cnt;
-            const int pos = live ? kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0;
-            const bool warp_live = __any_sync(0xffffffffu, live);
-            const int posmax = __reduce_max_sync(0xffffffffu, pos), imin = __reduce_min_sync(0xffffffffu, live ? i : INT_MAX);
+            const long long r0 = (long long)rt * R + slot_row;
+            const int i = (int)(r0 / a.G), gq = (int)(r0 % a.G);
+            const bool row_live = r0 < NR && key.live && i < key.cnt;
+            const int pos = row_live ? kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0;
+            const bool warp_live = __any_sync(0xffffffffu, row_live);
+            const int posmax = __reduce_max_sync(0xffffffffu, pos), imin = __reduce_min_sync(0xffffffffu, row_live ? i : INT_MAX);
             const int all_see = a.mask || !warp_live ? P : P + imin + 1;
             const int T = min(seg.x1, key.tiles) - seg.x0;  // 0 for an item without keys
             const int mine = single ? (T + 1 - x) >> 1 : T;
@@ -292,10 +303,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             {
                 const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + b * a.qb + i * a.qi + (long long)(h * a.G + gq) * a.qh;
                 const bool vec = ((uintptr_t)f & 15) == 0;
-#pragma unroll 4
+#pragma unroll 8
                 for (int c = 0; c < D / 8; ++c) {
                     uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (live) {
+                    if (row_live) {
                         if (vec) {
                             w = __ldg(reinterpret_cast<const uint4 *>(f) + c);
                         } else {
@@ -322,63 +333,76 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     uint32_t seen[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
                     if (masked) {
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) seen[w] = live ? seen_word(a, b, P, key.cnt, j0 + 32 * w, i, pos) : 0u;
+                        for (int w = 0; w < 4; ++w) seen[w] = row_live ? seen_word(a, b, P, key.cnt, j0 + 32 * w, i, pos) : 0u;
                     }
                     __syncwarp();
-                    float mx = -INFINITY;
+                    // Twice over the scores, 64 keys a round: their maximum, then the
+                    // weights.  The upper 64 keys stay in registers between; their
+                    // columns (D = 128) take the weights, so the lower ones are still
+                    // there to be read again.  One copy of each step, and not an
+                    // unrolled one: the warps of an SM run three programs, and what
+                    // does not fit the instruction cache cost half the time.
+                    float mx = -INFINITY, ref = 0.0f, v[2][32];
+#pragma unroll 1
+                    for (int round = 0; round < 4; ++round) {
+                        if (round != 2) {
+                            const int at = round == 1 ? 64 : 0;
+                            tc_ld32(tS + at, v[0]);
+                            tc_ld32(tS + at + 32, v[1]);
+                            tc_wait_ld(v[0]);
+                            tc_wait_ld(v[1]);
+                            if (masked) {
+                                const uint32_t see0 = round == 1 ? seen[2] : seen[0], see1 = round == 1 ? seen[3] : seen[1];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        float v[32];
-                        tc_ld32(tS + 32 * w, v);
-                        tc_wait_ld();
-                        if (masked) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c)
-                                if (!(seen[w] >> c & 1u)) v[c] = -INFINITY;
-                        }
-                        float m0 = v[0], m1 = v[1];
-#pragma unroll
-                        for (int c = 2; c < 32; c += 2) m0 = fmaxf(m0, v[c]), m1 = fmaxf(m1, v[c + 1]);
-                        mx = fmaxf(mx, fmaxf(m0, m1));
-                    }
-                    mx *= a.scale;
-                    const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
-                    if (__any_sync(0xffffffffu, grew)) {
-                        const float f = grew ? ex2(m - mx) : 1.0f;
-                        if (grew) m = mx;
-                        l0 *= f, l1 *= f;
-                        if (y > 0) {
-#pragma unroll
-                            for (int w = 0; w < D / 32; ++w) {
-                                float v[32];
-                                tc_ld32(tO + 32 * w, v);
-                                tc_wait_ld();
-#pragma unroll
-                                for (int c = 0; c < 32; ++c) v[c] *= f;
-                                tc_st32(tO + 32 * w, v);
+                                for (int c = 0; c < 32; ++c) {
+                                    if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
+                                    if (!(see1 >> c & 1u)) v[1][c] = -INFINITY;
+                                }
                             }
                         }
-                    }
-                    const float ref = m == -INFINITY ? 0.0f : -m;
+                        if (round < 2) {
+                            float m0 = v[0][0], m1 = v[1][0];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        float v[32];
-                        tc_ld32(tS + 32 * w, v);
-                        tc_wait_ld();
-                        if (masked) {
+                            for (int c = 1; c < 31; c += 2) m0 = max3(m0, v[0][c], v[0][c + 1]), m1 = max3(m1, v[1][c], v[1][c + 1]);
+                            mx = max3(mx, max3(m0, m1, v[0][31]), v[1][31]);
+                            if (round == 0) continue;
+                            mx *= a.scale;
+                            const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
+                            if (__any_sync(0xffffffffu, grew)) {
+                                const float f = grew ? ex2(m - mx) : 1.0f;
+                                if (grew) m = mx;
+                                l0 *= f, l1 *= f;
+                                if (y > 0) {
+#pragma unroll 1
+                                    for (int w = 0; w < D / 16; ++w) {
+                                        float o[16];
+                                        tc_ld16(tO + 16 * w, o);
+                                        tc_wait_ld(o);
+                                        uint32_t u[16];
 #pragma unroll
-                            for (int c = 0; c < 32; ++c)
-                                if (!(seen[w] >> c & 1u)) v[c] = -INFINITY;
+                                        for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(o[c] * f);
+                                        tc_st16(tO + 16 * w, u);
+                                    }
+                                }
+                            }
+                            ref = m == -INFINITY ? 0.0f : -m;
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < 2; ++w) {
+                                uint32_t pk[16];
+                                float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) {
+                                    float *e = v[w] + 2 * c;
+                                    fma2(e[0], e[1], a.scale, ref);
+                                    e[0] = ex2(e[0]), e[1] = ex2(e[1]);
+                                    add2(s0, s1, e[0], e[1]);
+                                    pk[c] = bf2_pack(e[0], e[1]);
+                                }
+                                l0 += s0, l1 += s1;
+                                tc_st16(tP + (round == 2 ? 32 : 0) + 16 * w, pk);
+                            }
                         }
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) {
-                            fma2(v[2 * c], v[2 * c + 1], a.scale, ref);
-                            v[2 * c] = ex2(v[2 * c]), v[2 * c + 1] = ex2(v[2 * c + 1]);
-                            add2(l0, l1, v[2 * c], v[2 * c + 1]);
-                            pk[c] = bf2_pack(v[2 * c], v[2 * c + 1]);
-                        }
-                        tc_st16(tP + 16 * w, pk);
                     }
                     tc_wait_st();
                 }
@@ -390,164 +414,153 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 wait(b_o + 8 * x, n_o++);
                 tc_after();
             }
-            // results
+            // results; their places are worked out here, not kept in registers
+            // through the loop (orow stands behind an asm the compiler cannot see through)
             float l = l0 + l1;
+            int srow = slot_row, se = seg.e;
+            asm volatile("" : "+r"(srow), "+r"(se));
+            const long long r = (long long)(se % RT) * R + srow;
+            const int ri = (int)(r / a.G);
+            const bool live = r < NR && seg.key.live && ri < seg.key.cnt;
             const bool whole = seg.whole();
             float *slot = ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
-            const size_t orow = ((size_t)b * a.n + i) * a.Hq + h * a.G + gq;
-            auto put = [&](int w, const float (&v)[32]) {  // channels 32 w ..
-                if (r >= NR) return;
-                if (whole) {
-                    const float k = live && l != 0.0f ? KV4_STEP / l : 0.0f;
-                    uint4 *o = reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + orow * D + 32 * w);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t u[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) u[j] = k == 0.0f ? 0u : bf2_pack(v[8 * c + 2 * j] * k, v[8 * c + 2 * j + 1] * k);
-                        o[c] = make_uint4(u[0], u[1], u[2], u[3]);
-                    }
-                } else {
-                    float4 *o = reinterpret_cast<float4 *>(slot + (size_t)slot_row * D + 32 * w);
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) o[c] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                }
-            };
-            auto put_stats = [&]() {
-                if (r >= NR) return;
-                if (whole) {
-                    if (a.lse) a.lse[orow] = live && l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-                } else {
-                    slot[(size_t)R * D + slot_row] = m;
-                    slot[(size_t)R * D + R + slot_row] = l;
-                }
-            };
-            auto sums = [&](int w, float (&v)[32]) {
+            const size_t orow = ((size_t)(se / RT) * a.n + ri) * a.Hq + seg.h * a.G + (int)(r % a.G);
+            float f = 1.0f;
+            if (single) {  // both groups have the rows
+                sm_m[x][row] = m, sm_l[x][row] = l;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const float M = fmaxf(sm_m[0][row], sm_m[1][row]), ref = M == -INFINITY ? 0.0f : M;
+                f = ex2(m - ref);
+                l = sm_l[0][row] * ex2(sm_m[0][row] - ref) + sm_l[1][row] * ex2(sm_m[1][row] - ref);
+                m = M;
+            }
+            const float k = whole ? (live && l != 0.0f ? f * KV4_STEP / l : 0.0f) : f;
+            // the second group's sums go to the first through its queries' place
+            float4 *box = reinterpret_cast<float4 *>(sq + C::TILE);  // 32 channels of 128 rows
+#pragma unroll 1
+            for (int w = 0; w < D / 32; ++w) {
+                float v[32];
                 __syncwarp();
                 if (mine > 0 && warp_live) {
                     tc_ld32(tO + 32 * w, v);
-                    tc_wait_ld();
+                    tc_wait_ld(v);
                 } else {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[c] = 0.0f;
                 }
-            };
-            if (!single) {
-#pragma unroll 1
-                for (int w = 0; w < D / 32; ++w) {
-                    float v[32];
-                    sums(w, v);
-                    put(w, v);
-                }
-                put_stats();
-            } else {
-                // the second group's sums go to the first through its queries' place
-                sm_m[x][row] = m, sm_l[x][row] = l;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                const float M = fmaxf(sm_m[0][row], sm_m[1][row]), ref2 = M == -INFINITY ? 0.0f : M, f = ex2(m - ref2);
-                l = sm_l[0][row] * ex2(sm_m[0][row] - ref2) + sm_l[1][row] * ex2(sm_m[1][row] - ref2);
-                m = M;
-                float4 *box = reinterpret_cast<float4 *>(sq + C::TILE);  // D / 2 channels of 128 rows
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    if (x == 1) {
-#pragma unroll 1
-                        for (int w = 0; w < D / 64; ++w) {
-                            float v[32];
-                            sums(half * (D / 64) + w, v);
+                if (k == 0.0f) {
 #pragma unroll
-                            for (int c = 0; c < 8; ++c)
-                                box[(w * 8 + c) * 128 + row] = make_float4(v[4 * c] * f, v[4 * c + 1] * f, v[4 * c + 2] * f, v[4 * c + 3] * f);
-                        }
+                    for (int c = 0; c < 32; ++c) v[c] = 0.0f;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[c] *= k;
+                }
+                if (single) {
+                    if (x == 1) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) box[c * 128 + row] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
                     }
                     asm volatile("bar.sync 1, 256;" ::: "memory");
                     if (x == 0) {
-#pragma unroll 1
-                        for (int w = 0; w < D / 64; ++w) {
-                            float v[32];
-                            sums(half * (D / 64) + w, v);
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) {
-                                const float4 o = box[(w * 8 + c) * 128 + row];
-                                v[4 * c] = fmaf(v[4 * c], f, o.x), v[4 * c + 1] = fmaf(v[4 * c + 1], f, o.y);
-                                v[4 * c + 2] = fmaf(v[4 * c + 2], f, o.z), v[4 * c + 3] = fmaf(v[4 * c + 3], f, o.w);
-                            }
-                            put(half * (D / 64) + w, v);
+                        for (int c = 0; c < 8; ++c) {
+                            const float4 o = box[c * 128 + row];
+                            v[4 * c] += o.x, v[4 * c + 1] += o.y, v[4 * c + 2] += o.z, v[4 * c + 3] += o.w;
                         }
                     }
                     asm volatile("bar.sync 1, 256;" ::: "memory");
+                    if (x == 1) continue;
                 }
-                if (x == 0) put_stats();
+                if (r >= NR) continue;
+                if (whole) {
+                    uint4 *o = reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + orow * D + 32 * w);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        o[c] = make_uint4(bf2_pack(v[8 * c], v[8 * c + 1]), bf2_pack(v[8 * c + 2], v[8 * c + 3]),
+                                          bf2_pack(v[8 * c + 4], v[8 * c + 5]), bf2_pack(v[8 * c + 6], v[8 * c + 7]));
+                } else {
+                    float4 *o = reinterpret_cast<float4 *>(slot + (size_t)srow * D + 32 * w);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) o[c] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                }
+            }
+            if (r < NR && !(single && x == 1)) {
+                if (!whole) {
+                    slot[(size_t)R * D + srow] = m;
+                    slot[(size_t)R * D + R + srow] = l;
+                } else if (a.lse) {
+                    a.lse[orow] = live && l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                }
             }
             first = false;
         } while (seg.next(a, R, RT));
     } else if (warp < MSM + MDQ) {
         // -- codes to bfloat16 tiles ------------------------------------------
         const int dt = tid - MSM * 32;
-        uint32_t n = 0;  // tiles done
-        Seg pre = seg;   // what is asked into the L2 ahead of the loads
-        int py = pre.x0;
-        bool pmore = dt == 0;
-        auto prefetch = [&]() {
-            while (pmore && py >= min(pre.x1, pre.key.tiles)) {
-                pmore = pre.next(a, R, RT);
-                py = pre.x0;
-            }
-            if (!pmore) return;
-            const int j0 = kv4_tile<MKT>(pre.key, py++), rows = min(MKT, pre.key.P + pre.key.cnt - j0);
-            const size_t off = ((size_t)((size_t)(pre.e / RT) * a.H + pre.h) * a.S + j0) * C::RB;
+        // Steps: a tile's keys, then its values.  The next step's rows are loaded
+        // while one is turned.
+        Piece<D> cur[C::PC], nxt[C::PC];
+        int y = seg.x0;
+        bool more = true;
+        // Rows are asked into the L2 AHEAD tiles before they are loaded: memory's
+        // latency at its full rate is about two tiles of every SM.
+        constexpr int AHEAD = 6;
+        auto prefetch = [&](int x) {
+            if (dt != 0 || x >= min(seg.x1, seg.key.tiles)) return;
+            const int j0 = kv4_tile<MKT>(seg.key, x), rows = min(MKT, seg.key.P + seg.key.cnt - j0);
+            const size_t off = ((size_t)((size_t)(seg.e / RT) * a.H + seg.h) * a.S + j0) * C::RB;
             const uint32_t bytes = rows * C::RB;
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.k + off), "r"(bytes) : "memory");
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.v + off), "r"(bytes) : "memory");
         };
-        Piece<D> pk[C::PC], pv[C::PC];
-        int y = seg.x0;
-        bool more = true;
-        auto settle = [&]() {  // y: the next tile there is
-            while (more && y >= min(seg.x1, seg.key.tiles)) {
-                more = seg.next(a, R, RT);
-                y = seg.x0;
-            }
-        };
-        auto load = [&](const uint8_t *plane, Piece<D> (&p)[C::PC]) {
+        auto load = [&](int step) {  // of tile y, which there is
             const int j0 = kv4_tile<MKT>(seg.key, y), end = seg.key.P + seg.key.cnt;
             const size_t row0 = (size_t)((size_t)(seg.e / RT) * a.H + seg.h) * a.S;
             if (!ACES_IN(j0, a.S) || !ACES_IN(end - 1, a.S)) return;
+            const uint8_t *plane = step & 1 ? a.v : a.k;
 #pragma unroll
-            for (int u = 0; u < C::PC; ++u) load_piece<D>(plane, row0, j0, end, dt + u * MDT, p[u]);
+            for (int u = 0; u < C::PC; ++u)
+                if (dt + u * MDT < C::PIECES) load_piece<D>(plane, row0, j0, end, dt + u * MDT, nxt[u]);
         };
-        for (int u = 0; u < 6; ++u) prefetch();
-        settle();
-        if (more) {
-            load(a.k, pk);
-            load(a.v, pv);
-        }
-        while (more) {
-            const uint32_t st = n & 1, ph = n >> 1;
-            prefetch();
-            wait(b_kfree + 8 * st, ph + 1);
+        bool fresh = true;
+#pragma unroll 1
+        for (uint32_t step = 0;; ++step) {  // loads step, and turns the one before
+            if ((step & 1) == 0) {
+                if (step > 0) ++y;
+                while (more && y >= min(seg.x1, seg.key.tiles)) {
+                    more = seg.next(a, R, RT);
+                    y = seg.x0;
+                    fresh = true;
+                }
+                if (more) {
+                    if (fresh)
+                        for (int u = 1; u < AHEAD; ++u) prefetch(y + u);
+                    fresh = false;
+                    prefetch(y + AHEAD);
+                }
+            }
+            if (more) load(step);
+            if (step > 0) {
+                const uint32_t t = step - 1, st = (t >> 1) & 1, v = t & 1;
+                wait((v ? b_vfree : b_kfree) + 8 * st, (t >> 2) + 1);
+                uint8_t *tile = (v ? sv : sk) + st * C::TILE;
 #pragma unroll
-            for (int u = 0; u < C::PC; ++u) store_piece<D>(sk + st * C::TILE, dt + u * MDT, pk[u]);
-            async_fence();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_kfull + 8 * st);
-            ++y;
-            settle();
-            if (more) load(a.k, pk);
-            wait(b_vfree + 8 * st, ph + 1);
+                for (int u = 0; u < C::PC; ++u)
+                    if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, cur[u]);
+                async_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+            }
+            if (!more) break;
 #pragma unroll
-            for (int u = 0; u < C::PC; ++u) store_piece<D>(sv + st * C::TILE, dt + u * MDT, pv[u]);
-            async_fence();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_vfull + 8 * st);
-            if (more) load(a.v, pv);
-            ++n;
+            for (int u = 0; u < C::PC; ++u) cur[u] = nxt[u];
         }
-    } else if (lane == 0) {
+    } else {
         // -- products ---------------------------------------------------------
+      if (warp == MSM + MDQ && lane == 0) {
         const uint32_t q0 = sm0, k0 = sm0 + 2 * C::TILE, v0 = sm0 + 4 * C::TILE;
         constexpr uint32_t ID_S = tc_idesc(MKT, false), ID_O = tc_idesc(D, true);
-        uint32_t n = 0, segs = 0, n_p[2] = {0, 0};
+        uint32_t n = 0, segs = 0, n_p0 = 0, n_p1 = 0;
         do {
             const int rt = seg.e % RT;
             const bool single = NR - (long long)rt * R <= 128;
@@ -555,42 +568,38 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             int cnt[2];
             cnt[0] = single ? (T + 1) >> 1 : T;
             cnt[1] = single ? T >> 1 : T;
-            auto scores = [&](int x, int i) {
-                const uint32_t tile = n + (single ? 2 * i + x : i), st = tile & 1;
-                wait(b_kfull + 8 * st, tile >> 1);
-                if (bad) return;
-                tc_after();
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t o = (ks >> 2) * C::HALF + (ks & 3) * 32;
-                    tc_mma_ss(tm + C::TS + x * 128, tc_desc(q0 + x * C::TILE + o, 16), tc_desc(k0 + st * C::TILE + o, 16), ID_S, ks > 0);
-                }
-                tc_commit(b_s + 8 * x);
-                if (single || x == 1) tc_commit(b_kfree + 8 * st);
-            };
-            auto values = [&](int x, int i) {
-                const uint32_t tile = n + (single ? 2 * i + x : i), st = tile & 1;
-                wait(b_vfull + 8 * st, tile >> 1);
-                wait(b_p + 8 * x, n_p[x]++);
-                if (bad) return;
-                tc_after();
-#pragma unroll
-                for (int ks = 0; ks < MKT / 16; ++ks)
-                    tc_mma_ts(tm + C::TO + x * D, tm + C::TP + x * C::TPX + 8 * ks, tc_desc(v0 + st * C::TILE + ks * 2048, C::HALF), ID_O,
-                              i > 0 || ks > 0);
-                if (single || x == 1) tc_commit(b_vfree + 8 * st);
-                if (i + 1 == cnt[x]) tc_commit(b_o + 8 * x);
-            };
             wait(b_q, segs);
-            if (cnt[0] > 0) scores(0, 0);
             wait(b_q + 8, segs);
-            if (cnt[1] > 0) scores(1, 0);
-            for (int i = 0; i < cnt[0]; ++i) {
-                values(0, i);
-                if (i + 1 < cnt[0]) scores(0, i + 1);
-                if (i < cnt[1]) {
-                    values(1, i);
-                    if (i + 1 < cnt[1]) scores(1, i + 1);
+            // each group in turn: the values of its tile i, then the scores of i + 1
+#pragma unroll 1
+            for (int u = 0; u < 2 * (cnt[0] + 1); ++u) {
+                const int x = u & 1, i = (u >> 1) - 1, mine = x ? cnt[1] : cnt[0];
+                if (i >= 0 && i < mine) {
+                    const uint32_t tile = n + (single ? 2 * i + x : i), st = tile & 1;
+                    wait(b_vfull + 8 * st, tile >> 1);
+                    wait(b_p + 8 * x, x ? n_p1++ : n_p0++);
+                    if (bad) break;
+                    tc_after();
+                    const uint64_t bd = tc_desc(v0 + st * C::TILE, C::HALF);
+#pragma unroll
+                    for (int ks = 0; ks < MKT / 16; ++ks)
+                        tc_mma_ts(tm + C::TO + x * D, tm + C::TP + x * C::TPX + 8 * ks, bd + ks * (2048 >> 4), ID_O, i > 0 || ks > 0);
+                    if (single || x == 1) tc_commit(b_vfree + 8 * st);
+                    if (i + 1 == mine) tc_commit(b_o + 8 * x);
+                }
+                if (i + 1 < mine) {
+                    const uint32_t tile = n + (single ? 2 * (i + 1) + x : i + 1), st = tile & 1;
+                    wait(b_kfull + 8 * st, tile >> 1);
+                    if (bad) break;
+                    tc_after();
+                    const uint64_t ad = tc_desc(q0 + x * C::TILE, 16), bd = tc_desc(k0 + st * C::TILE, 16);
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        const uint32_t o = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
+                        tc_mma_ss(tm + C::TS + x * 128, ad + o, bd + o, ID_S, ks > 0);
+                    }
+                    tc_commit(b_s + 8 * x);
+                    if (single || x == 1) tc_commit(b_kfree + 8 * st);
                 }
             }
             n += max(T, 0);
@@ -598,6 +607,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         } while (seg.next(a, R, RT));
         tc_commit(b_end);  // nothing runs on when the columns are given back
         if (!mbar_wait(b_end, 0)) bad = true;
+      }
     }
     if (bad) any_timeout = 1;
     __syncwarp();

@@ -48,9 +48,9 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int r
     Kv4Keys k;
     const Kv4Seq sq = kv4_seq(a.prefix, a.count, b, a.n, a.S);
     k.P = sq.P, k.cnt = sq.cnt;
-    const long long r0 = (long long)rt * R, r1 = min(r0 + R, (long long)a.n * a.G);
-    k.i0 = (int)(r0 / a.G);
-    k.i1 = min((int)((r1 - 1) / a.G), sq.cnt - 1);
+    const int r0 = rt * R, r1 = min(r0 + R, a.n * a.G);  // at most 2^30 rows
+    k.i0 = r0 / a.G;
+    k.i1 = min((r1 - 1) / a.G, sq.cnt - 1);
     k.live = sq.ok && k.i0 < sq.cnt;
     k.lo = k.hi = k.s_hi = k.st = k.mt0 = k.tiles = 0;
     if (k.live) {
