@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
         const int s = place % ST;
         const uint32_t bytes = rows * RB, dst = ring + s * C::STAGE;
-        const size_t off = ((size_t)((size_t)(g.e / RT) * a.H + g.h) * a.S + j0) * RB;
+        const size_t off = (g.row0(a) + j0) * RB;
         mbar_expect(bar0 + 8 * s, 2 * bytes);
         bulk_load(dst, a.k + off, bytes, bar0 + 8 * s);
         bulk_load(dst + FKT * RB, a.v + off, bytes, bar0 + 8 * s);
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     bool first = true;
     while (true) {
         const Kv4Keys key = cur.key;
-        const int b = cur.e / RT, rt = cur.e % RT, h = cur.h, P = key.P, end = P + key.cnt;
+        const int b = cur.b, rt = cur.rt, h = cur.h, P = key.P, end = P + key.cnt;
         // the segment's query rows
         if (tid < R) {
             const int r = rt * R + tid, i = r / a.G;

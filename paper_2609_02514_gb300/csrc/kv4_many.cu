@@ -13,12 +13,12 @@
 //     the 128-byte swizzle.  Keys and values lie alike ([key][64 channels] a
 //     half): the keys' product reads them along the channels, the values' along
 //     the keys (the transposed form of the second operand).
-//   - one thread issues the products: S = Q K' (both from shared memory), O += P
-//     V (P from TMEM).  While one group turns its scores into weights the
-//     other's products run.
-// P takes half the place of S (D = 128): the products of both have one shape, so the
-// tensor pipe runs them in the order they were issued.  For D = 64 the shapes
-// differ and P has columns of its own.
+//   - one warp issues the products, 64 keys at a time: S = Q K' (both from shared
+//     memory) into one of a group's two places, O += P V (P from TMEM, where S
+//     was).  While a group turns one S into P the next is made, so neither waits
+//     for the other's whole chain.
+// The tensor pipe runs products in the order they were issued, so an S may be
+// made in the place of a P whose product is under way.
 // Sums are rescaled only when a row's maximum grew by more than 2^8 (in the
 // weights' scale); weights stay below that and lose nothing by it.
 #define ACES_FILE 9  // site numbers of the checked build
@@ -31,6 +31,7 @@
 namespace aces {
 
 constexpr int MKT = 128;                  // keys of a tile
+constexpr int MKH = 64;                   // keys of a product
 constexpr int MSM = 8, MDQ = 7;           // softmax and dequantising warps
 constexpr int MT = (MSM + MDQ + 1) * 32;  // and the one that issues: 16 warps of 128 registers
 constexpr int MDT = MDQ * 32;
@@ -41,6 +42,11 @@ __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p;
 }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -101,8 +107,11 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&v)[16]) 
 // Shared-memory descriptor of the 128-byte swizzle: eight rows of 128 bytes are
 // 1024 bytes apart from the next eight (stride); lead: the next 64 channels of
 // an operand read along the keys.
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// (addr16: address / 16; below 2^14, as shared memory ends at 228 KB)
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr16, uint32_t lead) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(addr16 | (lead >> 4) << 16), "r"((1024u >> 4) | 1u << 14 | 2u << 29));
+    return d;
 }
 // kind::f16: float32 sums of bfloat16, M = 128, N, second operand along N
 __host__ __device__ constexpr uint32_t tc_idesc(int N, bool b_mn) {
@@ -164,7 +173,7 @@ struct Many {
     static constexpr int PIECES = MKT * D / 32;            // 16-byte pieces of a tile's codes
     static constexpr int PC = (PIECES + MDT - 1) / MDT;    // that a thread dequantises (a warp's last may be none)
     static_assert(PIECES % 32 == 0, "whole warps");
-    static constexpr int TS = 0, TO = 256, TP = D == 128 ? 64 : 384, TPX = D == 128 ? 128 : 64;  // TMEM columns
+    static constexpr int TS = 0, TP = 32, TO = 256;        // TMEM columns: S[group][2] of 64, P in the second half of S, O[group]
 };
 
 // Byte of 16-byte chunk c (eight channels) of a row in a swizzled tile.
@@ -176,13 +185,14 @@ struct Piece {  // 32 channels of a row and their t's
     uint32_t t[D == 128 ? 1 : 2];
 };
 
-// Without a branch and without a use, so a thread's loads are all under way at
-// once.  Rows past the sequence are its last one again: their weights are 0.
+// Piece p of the tile at j0 (base: the key head's first row).  Without a branch
+// and without a use, so a thread's loads are all under way at once.  Rows past
+// the sequence are its last one again: their weights are 0.
 template <int D>
-__device__ __forceinline__ void load_piece(const uint8_t *plane, size_t row0, int j0, int end, int p, Piece<D> &o) {
-    constexpr int RB = Many<D>::RB, Q = D / 32;
+__device__ __forceinline__ void load_piece(const uint8_t *base, int j0, int last, int p, Piece<D> &o) {
+    constexpr int Q = D / 32;
     const int q = p % Q;
-    const uint8_t *r = plane + (row0 + min(j0 + p / Q, end - 1)) * RB;
+    const uint8_t *r = base + (unsigned long long)(uint32_t)min(j0 + p / Q, last) * (uint32_t)Many<D>::RB;
     o.w = __ldg(reinterpret_cast<const uint4 *>(r) + q);
     if (D == 128) {
         o.t[0] = __ldg(reinterpret_cast<const uint32_t *>(r + D / 2) + q);
@@ -231,29 +241,33 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     using C = Many<D>;
     using Seg = Kv4Seg<MKT, 1>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) unsigned long long bars[17];
+    __shared__ __align__(8) unsigned long long bars[23];
     __shared__ uint32_t tmem_base;
     __shared__ float sm_m[2][128], sm_l[2][128];
     __shared__ int any_timeout;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // the same in all lanes, also for the compiler
     // tiles start on 1024 bytes
     uint8_t *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const uint32_t sm0 = smem_u32(smem);
     uint8_t *sq = smem, *sk = smem + 2 * C::TILE, *sv = smem + 4 * C::TILE;
     const uint32_t bar0 = smem_u32(bars);
-    // pairs of barriers by stage (keys, values) or by group
-    const uint32_t b_kfull = bar0, b_kfree = bar0 + 16, b_vfull = bar0 + 32, b_vfree = bar0 + 48, b_s = bar0 + 64, b_p = bar0 + 80,
-                   b_o = bar0 + 96, b_q = bar0 + 112, b_end = bar0 + 128;
+    // barriers by stage (keys, values), by group, or by group and place (2 x + place)
+    const uint32_t b_kfull = bar0, b_kfree = bar0 + 16, b_vfull = bar0 + 32, b_vfree = bar0 + 48, b_o = bar0 + 64, b_q = bar0 + 80,
+                   b_s = bar0 + 96, b_p = bar0 + 128, b_f = bar0 + 160, b_end = bar0 + 176;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(b_kfull + 8 * i, MDQ);
             mbar_init(b_vfull + 8 * i, MDQ);
             mbar_init(b_kfree + 8 * i, 1);
             mbar_init(b_vfree + 8 * i, 1);
-            mbar_init(b_s + 8 * i, 1);
             mbar_init(b_o + 8 * i, 1);
-            mbar_init(b_p + 8 * i, 4);
+            mbar_init(b_f + 8 * i, 1);
             mbar_init(b_q + 8 * i, 4);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(b_s + 8 * i, 1);
+            mbar_init(b_p + 8 * i, 4);
         }
         mbar_init(b_end, 1);
         any_timeout = 0;
@@ -270,8 +284,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     }
     __syncthreads();
     tc_after();
-    const uint32_t tm = tmem_base;
-    const long long NR = (long long)a.n * a.G;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+    const int NR = a.n * a.G;  // at most 2^30
     bool bad = false;  // a wait gave up: nothing is waited for any more
     auto wait = [&](uint32_t bar, uint32_t phase) {
         if (!bad && !mbar_wait(bar, phase & 1)) bad = true;
@@ -281,42 +295,49 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         // -- softmax: a thread a row ------------------------------------------
         const int x = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tm + lanes + C::TS + x * 128, tO = tm + lanes + C::TO + x * D, tP = tm + lanes + C::TP + x * C::TPX;
+        const uint32_t tS = tm + lanes + C::TS + x * 128, tO = tm + lanes + C::TO + x * D;
         uint8_t *myq = sq + x * C::TILE;
-        uint32_t n_s = 0, n_o = 0;  // phases passed
+        uint32_t n_s = 0, n_o = 0;  // products of scores, and segments, that were waited for
         bool first = true;
         do {
             const Kv4Keys &key = seg.key;
-            const int b = seg.e / RT, rt = seg.e % RT, h = seg.h, P = key.P;
-            const bool single = NR - (long long)rt * R <= 128;
+            const int b = seg.b, rt = seg.rt, h = seg.h, P = key.P;
+            const bool single = NR - rt * R <= 128;
             const int slot_row = single ? row : x * 128 + row;
-            const long long r0 = (long long)rt * R + slot_row;
-            const int i = (int)(r0 / a.G), gq = (int)(r0 % a.G);
+            const int r0 = rt * R + slot_row, i = r0 / a.G, gq = r0 - i * a.G;
             const bool row_live = r0 < NR && key.live && i < key.cnt;
             const int pos = row_live ? kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0;
             const bool warp_live = __any_sync(0xffffffffu, row_live);
             const int posmax = __reduce_max_sync(0xffffffffu, pos), imin = __reduce_min_sync(0xffffffffu, row_live ? i : INT_MAX);
             const int all_see = a.mask || !warp_live ? P : P + imin + 1;
             const int T = min(seg.x1, key.tiles) - seg.x0;  // 0 for an item without keys
-            const int mine = single ? (T + 1 - x) >> 1 : T;
-            // queries
+            const int mine = 2 * (single ? (T + 1 - x) >> 1 : T);  // of 64 keys
+            // queries (a row without one reads the first token's and keeps zeros)
             {
-                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + b * a.qb + i * a.qi + (long long)(h * a.G + gq) * a.qh;
-                const bool vec = ((uintptr_t)f & 15) == 0;
-#pragma unroll 8
-                for (int c = 0; c < D / 8; ++c) {
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (row_live) {
-                        if (vec) {
-                            w = __ldg(reinterpret_cast<const uint4 *>(f) + c);
-                        } else {
-                            uint32_t u[4];
-                            for (int j = 0; j < 4; ++j) u[j] = (uint32_t)__ldg(f + 8 * c + 2 * j) | (uint32_t)__ldg(f + 8 * c + 2 * j + 1) << 16;
-                            w = make_uint4(u[0], u[1], u[2], u[3]);
-                        }
-                        w.x = bf2_poison(w.x), w.y = bf2_poison(w.y), w.z = bf2_poison(w.z), w.w = bf2_poison(w.w);
+                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + b * a.qb + (row_live ? i : 0) * a.qi +
+                                          (long long)(h * a.G + (row_live ? gq : 0)) * a.qh;
+                const uint32_t keep = row_live ? 0xFFFFFFFFu : 0u;
+                if (((uintptr_t)f & 15) == 0) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D / 8; c0 += 8) {
+                        uint4 w[8];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) w[c] = __ldg(reinterpret_cast<const uint4 *>(f) + c0 + c);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            *reinterpret_cast<uint4 *>(myq + swz(row, c0 + c)) =
+                                make_uint4(bf2_poison(w[c].x) & keep, bf2_poison(w[c].y) & keep, bf2_poison(w[c].z) & keep,
+                                           bf2_poison(w[c].w) & keep);
                     }
-                    *reinterpret_cast<uint4 *>(myq + swz(row, c)) = w;
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            u[j] = bf2_poison((uint32_t)__ldg(f + 8 * c + 2 * j) | (uint32_t)__ldg(f + 8 * c + 2 * j + 1) << 16) & keep;
+                        *reinterpret_cast<uint4 *>(myq + swz(row, c)) = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
                 }
             }
             async_fence();
@@ -324,107 +345,99 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             __syncwarp();
             if (lane == 0) mbar_arrive(b_q + 8 * x);
             float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-            for (int y = 0; y < mine; ++y) {
-                wait(b_s + 8 * x, n_s++);
+#pragma unroll 1
+            for (int y = 0; y < mine; ++y, ++n_s) {
+                const uint32_t place = n_s & 1, phase = n_s >> 1, bp = 8 * (2 * x + place);
+                wait(b_s + bp, phase);
                 tc_after();
                 if (warp_live) {
-                    const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? 2 * y + x : y));
-                    const bool masked = j0 + MKT > all_see || (a.window && j0 <= posmax - a.window && j0 + MKT > a.sinks);
-                    uint32_t seen[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
+                    const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + (y & 1) * MKH;
+                    const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > a.sinks);
+                    const uint32_t at = tS + place * MKH;
+                    float v[2][32];
+                    tc_ld32(at, v[0]);
+                    tc_ld32(at + 32, v[1]);
+                    tc_wait_ld(v[0]);
+                    tc_wait_ld(v[1]);
                     if (masked) {
+                        uint32_t see0 = 0u, see1 = 0u;
+                        if (row_live) see0 = seen_word(a, b, P, key.cnt, j0, i, pos), see1 = seen_word(a, b, P, key.cnt, j0 + 32, i, pos);
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) seen[w] = row_live ? seen_word(a, b, P, key.cnt, j0 + 32 * w, i, pos) : 0u;
+                        for (int c = 0; c < 32; ++c) {
+                            if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
+                            if (!(see1 >> c & 1u)) v[1][c] = -INFINITY;
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
-                    // Twice over the scores, 64 keys a round: their maximum, then the
-                    // weights.  The upper 64 keys stay in registers between; their
-                    // columns (D = 128) take the weights, so the lower ones are still
-                    // there to be read again.  One copy of each step, and not an
-                    // unrolled one: the warps of an SM run three programs, and what
-                    // does not fit the instruction cache cost half the time.
-                    float mx = -INFINITY, ref = 0.0f, v[2][32];
-#pragma unroll 1
-                    for (int round = 0; round < 4; ++round) {
-                        if (round != 2) {
-                            const int at = round == 1 ? 64 : 0;
-                            tc_ld32(tS + at, v[0]);
-                            tc_ld32(tS + at + 32, v[1]);
-                            tc_wait_ld(v[0]);
-                            tc_wait_ld(v[1]);
-                            if (masked) {
-                                const uint32_t see0 = round == 1 ? seen[2] : seen[0], see1 = round == 1 ? seen[3] : seen[1];
+                    float m0 = v[0][0], m1 = v[0][31], m2 = v[1][0], m3 = v[1][31];
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) {
-                                    if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
-                                    if (!(see1 >> c & 1u)) v[1][c] = -INFINITY;
-                                }
+                    for (int c = 1; c < 15; c += 2) {
+                        m0 = max3(m0, v[0][c], v[0][c + 1]), m1 = max3(m1, v[0][c + 15], v[0][c + 16]);
+                        m2 = max3(m2, v[1][c], v[1][c + 1]), m3 = max3(m3, v[1][c + 15], v[1][c + 16]);
+                    }
+                    m0 = max3(m0, v[0][15], v[0][30]), m2 = max3(m2, v[1][15], v[1][30]);
+                    const float mx = fmaxf(max3(m0, m1, m2), m3) * a.scale;
+                    const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
+                    if (__any_sync(0xffffffffu, grew)) {
+                        const float f = grew ? ex2(m - mx) : 1.0f;
+                        if (grew) m = mx;
+                        l0 *= f, l1 *= f;
+                        if (y > 0) {
+                            // the last product has been added: before the next scores
+                            // were made, and for the last ones by a word of its own
+                            if (y + 1 < mine)
+                                wait(b_s + 8 * (2 * x + (place ^ 1)), (n_s + 1) >> 1);
+                            else
+                                wait(b_f + 8 * x, n_o);
+                            tc_after();
+#pragma unroll 1
+                            for (int w = 0; w < D / 16; ++w) {
+                                float o[16];
+                                tc_ld16(tO + 16 * w, o);
+                                tc_wait_ld(o);
+                                uint32_t u[16];
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(o[c] * f);
+                                tc_st16(tO + 16 * w, u);
                             }
                         }
-                        if (round < 2) {
-                            float m0 = v[0][0], m1 = v[1][0];
+                    }
+                    const float ref = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
-                            for (int c = 1; c < 31; c += 2) m0 = max3(m0, v[0][c], v[0][c + 1]), m1 = max3(m1, v[1][c], v[1][c + 1]);
-                            mx = max3(mx, max3(m0, m1, v[0][31]), v[1][31]);
-                            if (round == 0) continue;
-                            mx *= a.scale;
-                            const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
-                            if (__any_sync(0xffffffffu, grew)) {
-                                const float f = grew ? ex2(m - mx) : 1.0f;
-                                if (grew) m = mx;
-                                l0 *= f, l1 *= f;
-                                if (y > 0) {
-#pragma unroll 1
-                                    for (int w = 0; w < D / 16; ++w) {
-                                        float o[16];
-                                        tc_ld16(tO + 16 * w, o);
-                                        tc_wait_ld(o);
-                                        uint32_t u[16];
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t pk[16];
+                        float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-                                        for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(o[c] * f);
-                                        tc_st16(tO + 16 * w, u);
-                                    }
-                                }
-                            }
-                            ref = m == -INFINITY ? 0.0f : -m;
-                        } else {
-#pragma unroll
-                            for (int w = 0; w < 2; ++w) {
-                                uint32_t pk[16];
-                                float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-                                for (int c = 0; c < 16; ++c) {
-                                    float *e = v[w] + 2 * c;
-                                    fma2(e[0], e[1], a.scale, ref);
-                                    e[0] = ex2(e[0]), e[1] = ex2(e[1]);
-                                    add2(s0, s1, e[0], e[1]);
-                                    pk[c] = bf2_pack(e[0], e[1]);
-                                }
-                                l0 += s0, l1 += s1;
-                                tc_st16(tP + (round == 2 ? 32 : 0) + 16 * w, pk);
-                            }
+                        for (int c = 0; c < 16; ++c) {
+                            float *e = v[w] + 2 * c;
+                            fma2(e[0], e[1], a.scale, ref);
+                            e[0] = ex2(e[0]), e[1] = ex2(e[1]);
+                            add2(s0, s1, e[0], e[1]);
+                            pk[c] = bf2_pack(e[0], e[1]);
                         }
+                        l0 += s0, l1 += s1;
+                        tc_st16(at + C::TP + 16 * w, pk);
                     }
                     tc_wait_st();
                 }
                 tc_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(b_p + 8 * x);
+                if (lane == 0) mbar_arrive(b_p + bp);
             }
             if (mine > 0) {
                 wait(b_o + 8 * x, n_o++);
                 tc_after();
             }
             // results; their places are worked out here, not kept in registers
-            // through the loop (orow stands behind an asm the compiler cannot see through)
+            // through the loop (behind an asm the compiler cannot see through)
             float l = l0 + l1;
-            int srow = slot_row, se = seg.e;
-            asm volatile("" : "+r"(srow), "+r"(se));
-            const long long r = (long long)(se % RT) * R + srow;
-            const int ri = (int)(r / a.G);
+            int srow = slot_row, srt = seg.rt;
+            asm volatile("" : "+r"(srow), "+r"(srt));
+            const int r = srt * R + srow, ri = r / a.G;
             const bool live = r < NR && seg.key.live && ri < seg.key.cnt;
             const bool whole = seg.whole();
             float *slot = ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
-            const size_t orow = ((size_t)(se / RT) * a.n + ri) * a.Hq + seg.h * a.G + (int)(r % a.G);
+            const int orow = (seg.b * a.n + ri) * a.Hq + seg.h * a.G + (r - ri * a.G);  // at most 2^30
             float f = 1.0f;
             if (single) {  // both groups have the rows
                 sm_m[x][row] = m, sm_l[x][row] = l;
@@ -471,18 +484,40 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     asm volatile("bar.sync 1, 256;" ::: "memory");
                     if (x == 1) continue;
                 }
-                if (r >= NR) continue;
+                // The warp's rows go out in whole lines, through the place of its
+                // queries: bfloat16 rows at once, float32 pieces half a row at a time.
+                constexpr int CH = D / 8;  // 16-byte chunks of a row there
+                auto chunk = [&](int rw, int c) { return reinterpret_cast<uint4 *>(myq + rw * (D * 2) + ((c ^ (rw & 7)) << 4)); };
+                bool full;
                 if (whole) {
-                    uint4 *o = reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + orow * D + 32 * w);
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        o[c] = make_uint4(bf2_pack(v[8 * c], v[8 * c + 1]), bf2_pack(v[8 * c + 2], v[8 * c + 3]),
-                                          bf2_pack(v[8 * c + 4], v[8 * c + 5]), bf2_pack(v[8 * c + 6], v[8 * c + 7]));
+                        *chunk(row, 4 * w + c) = make_uint4(bf2_pack(v[8 * c], v[8 * c + 1]), bf2_pack(v[8 * c + 2], v[8 * c + 3]),
+                                                            bf2_pack(v[8 * c + 4], v[8 * c + 5]), bf2_pack(v[8 * c + 6], v[8 * c + 7]));
+                    full = w == D / 32 - 1;
                 } else {
-                    float4 *o = reinterpret_cast<float4 *>(slot + (size_t)srow * D + 32 * w);
+                    const int c0 = (w % (D / 64)) * 8;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) o[c] = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                    for (int c = 0; c < 8; ++c)
+                        *chunk(row, c0 + c) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
+                                                         __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+                    full = w % (D / 64) == D / 64 - 1;
                 }
+                if (!full) continue;
+                __syncwarp();
+                const int r_first = r - lane, rw0 = row - lane, sw0 = srow - lane;
+#pragma unroll 4
+                for (int z = 0; z < CH; ++z) {  // 32 / CH rows at a time
+                    const int rr = z * (32 / CH) + lane / CH, c = lane % CH;
+                    const int to = __shfl_sync(0xffffffffu, orow, rr);
+                    if (r_first + rr >= NR) continue;
+                    const uint4 o = *chunk(rw0 + rr, c);
+                    if (whole)
+                        reinterpret_cast<uint4 *>(a.out)[(size_t)to * CH + c] = o;
+                    else
+                        reinterpret_cast<uint4 *>(slot)[(size_t)(sw0 + rr) * (D / 4) + (w / (D / 64)) * CH + c] = o;
+                }
+                __syncwarp();
             }
             if (r < NR && !(single && x == 1)) {
                 if (!whole) {
@@ -497,117 +532,147 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     } else if (warp < MSM + MDQ) {
         // -- codes to bfloat16 tiles ------------------------------------------
         const int dt = tid - MSM * 32;
-        // Steps: a tile's keys, then its values.  The next step's rows are loaded
+        // Steps: the keys of two tiles, then their values (of a segment's last, odd
+        // tile its keys and values): with a group's scores two products ahead of its
+        // values, keys are wanted a tile before the other group's last values are
+        // done, so values must not come between.  The next step's rows are loaded
         // while one is turned.
         Piece<D> cur[C::PC], nxt[C::PC];
-        int y = seg.x0;
+        int y = seg.x0;     // first tile of the two
+        uint32_t n = 0;     // and its number in the rings
+        int r = 0;          // step of the two tiles
         bool more = true;
-        // Rows are asked into the L2 AHEAD tiles before they are loaded: memory's
-        // latency at its full rate is about two tiles of every SM.
-        constexpr int AHEAD = 6;
+        // Rows are asked into the L2 AHEAD tiles before they are loaded (memory's
+        // latency at its full rate is about two tiles of every SM), a line of a
+        // tile's keys or values a thread.
+        constexpr int AHEAD = 6, LINES = MKT * C::RB / 128;
+        static_assert(MKT * C::RB % 128 == 0 && 2 * LINES <= MDT, "a line a thread");
+        const uint8_t *kb = a.k, *vb = a.v;  // the key head's rows
+        int j0 = 0;
         auto prefetch = [&](int x) {
-            if (dt != 0 || x >= min(seg.x1, seg.key.tiles)) return;
-            const int j0 = kv4_tile<MKT>(seg.key, x), rows = min(MKT, seg.key.P + seg.key.cnt - j0);
-            const size_t off = ((size_t)((size_t)(seg.e / RT) * a.H + seg.h) * a.S + j0) * C::RB;
-            const uint32_t bytes = rows * C::RB;
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.k + off), "r"(bytes) : "memory");
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.v + off), "r"(bytes) : "memory");
+            if (x >= min(seg.x1, seg.key.tiles) || dt >= 2 * LINES) return;
+            const int first = kv4_tile<MKT>(seg.key, x), rows = min(MKT, seg.key.P + seg.key.cnt - first);
+            const int line = dt < LINES ? dt : dt - LINES;
+            if (line * 128 >= rows * C::RB) return;
+            const uint8_t *at = (dt < LINES ? kb : vb) + (unsigned long long)(uint32_t)first * (uint32_t)C::RB + line * 128;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
         };
-        auto load = [&](int step) {  // of tile y, which there is
-            const int j0 = kv4_tile<MKT>(seg.key, y), end = seg.key.P + seg.key.cnt;
-            const size_t row0 = (size_t)((size_t)(seg.e / RT) * a.H + seg.h) * a.S;
-            if (!ACES_IN(j0, a.S) || !ACES_IN(end - 1, a.S)) return;
-            const uint8_t *plane = step & 1 ? a.v : a.k;
+        auto load = [&](bool values) {
+            const int last = seg.key.P + seg.key.cnt - 1;
+            if (!ACES_IN(j0, a.S) || !ACES_IN(last, a.S)) return;
+            const uint8_t *base = values ? vb : kb;
 #pragma unroll
             for (int u = 0; u < C::PC; ++u)
-                if (dt + u * MDT < C::PIECES) load_piece<D>(plane, row0, j0, end, dt + u * MDT, nxt[u]);
+                if (dt + u * MDT < C::PIECES) load_piece<D>(base, j0, last, dt + u * MDT, nxt[u]);
         };
-        bool fresh = true;
+        bool fresh = true, some = false, cur_v = false;
+        uint32_t cur_n = 0;
 #pragma unroll 1
-        for (uint32_t step = 0;; ++step) {  // loads step, and turns the one before
-            if ((step & 1) == 0) {
-                if (step > 0) ++y;
-                while (more && y >= min(seg.x1, seg.key.tiles)) {
-                    more = seg.next(a, R, RT);
-                    y = seg.x0;
-                    fresh = true;
-                }
-                if (more) {
-                    if (fresh)
-                        for (int u = 1; u < AHEAD; ++u) prefetch(y + u);
-                    fresh = false;
-                    prefetch(y + AHEAD);
-                }
+        while (true) {  // loads a step, and turns the one before
+            while (more && y >= min(seg.x1, seg.key.tiles)) {
+                more = seg.next(a, R, RT);
+                y = seg.x0;
+                fresh = true;
             }
-            if (more) load(step);
-            if (step > 0) {
-                const uint32_t t = step - 1, st = (t >> 1) & 1, v = t & 1;
-                wait((v ? b_vfree : b_kfree) + 8 * st, (t >> 2) + 1);
-                uint8_t *tile = (v ? sv : sk) + st * C::TILE;
+            uint32_t nxt_n = 0;
+            bool nxt_v = false;
+            if (more) {
+                const bool two = y + 1 < min(seg.x1, seg.key.tiles);
+                const int t = two ? r & 1 : 0;
+                nxt_v = two ? r >> 1 : r;
+                nxt_n = n + t;
+                j0 = kv4_tile<MKT>(seg.key, y + t);
+                if (fresh) {
+                    fresh = false;
+                    kb = a.k + seg.row0(a) * C::RB, vb = a.v + seg.row0(a) * C::RB;
+#pragma unroll 1
+                    for (int u = 1; u < AHEAD; ++u) prefetch(y + u);
+                }
+                if (!nxt_v) prefetch(y + t + AHEAD);
+                load(nxt_v);
+                if (++r == (two ? 4 : 2)) r = 0, y += two ? 2 : 1, n += two ? 2 : 1;
+            }
+            if (some) {
+                const uint32_t st = cur_n & 1;
+                wait((cur_v ? b_vfree : b_kfree) + 8 * st, (cur_n >> 1) + 1);
+                uint8_t *tile = (cur_v ? sv : sk) + st * C::TILE;
 #pragma unroll
                 for (int u = 0; u < C::PC; ++u)
                     if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, cur[u]);
                 async_fence();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+                if (lane == 0) mbar_arrive((cur_v ? b_vfull : b_kfull) + 8 * st);
             }
             if (!more) break;
+            some = true;
+            cur_n = nxt_n, cur_v = nxt_v;
 #pragma unroll
             for (int u = 0; u < C::PC; ++u) cur[u] = nxt[u];
         }
     } else {
-        // -- products ---------------------------------------------------------
-      if (warp == MSM + MDQ && lane == 0) {
+        // -- products: the whole warp goes along, so that addresses stay in uniform
+        // registers, and one lane issues -------------------------------------
         const uint32_t q0 = sm0, k0 = sm0 + 2 * C::TILE, v0 = sm0 + 4 * C::TILE;
-        constexpr uint32_t ID_S = tc_idesc(MKT, false), ID_O = tc_idesc(D, true);
-        uint32_t n = 0, segs = 0, n_p0 = 0, n_p1 = 0;
+        constexpr uint32_t ID_S = tc_idesc(MKH, false), ID_O = tc_idesc(D, true);
+        const bool leader = elect_one();
+        auto go = [&](uint32_t bar, uint32_t phase) {  // wait(), with one answer for the warp
+            if (bad) return;
+            for (int t = 0; t < 16; ++t)
+                if (mbar_try(bar, phase & 1)) return;
+            bad = !__all_sync(0xffffffffu, mbar_wait_slow(bar, phase & 1));
+        };
+        uint32_t n = 0, segs = 0, np0 = 0, np1 = 0;  // tiles, segments and each group's products of scores so far
         do {
-            const int rt = seg.e % RT;
-            const bool single = NR - (long long)rt * R <= 128;
-            const int T = min(seg.x1, seg.key.tiles) - seg.x0;
-            int cnt[2];
-            cnt[0] = single ? (T + 1) >> 1 : T;
-            cnt[1] = single ? T >> 1 : T;
-            wait(b_q, segs);
-            wait(b_q + 8, segs);
-            // each group in turn: the values of its tile i, then the scores of i + 1
+            const bool single = NR - seg.rt * R <= 128;
+            const int T = __shfl_sync(0xffffffffu, min(seg.x1, seg.key.tiles) - seg.x0, 0);
+            const int cnt0 = 2 * (single ? (T + 1) >> 1 : T), cnt1 = 2 * (single ? T >> 1 : T);
+            go(b_q, segs);
+            go(b_q + 8, segs);
+            // each group in turn: the values of its 64 keys i, then the scores of i + 2
 #pragma unroll 1
-            for (int u = 0; u < 2 * (cnt[0] + 1); ++u) {
-                const int x = u & 1, i = (u >> 1) - 1, mine = x ? cnt[1] : cnt[0];
+            for (int u = -4; u < 2 * cnt0 && !bad; ++u) {
+                const int x = u & 1, i = u >> 1, mine = x ? cnt1 : cnt0;  // i from -2
+                const uint32_t np = (x ? np1 : np0) + i;                   // the product's number
+                const uint32_t place = 2 * x + (np & 1), ts = tm + C::TS + place * MKH;
+                const bool both = single || x == 1, odd = i & 1;           // a tile's first use, its last
                 if (i >= 0 && i < mine) {
-                    const uint32_t tile = n + (single ? 2 * i + x : i), st = tile & 1;
-                    wait(b_vfull + 8 * st, tile >> 1);
-                    wait(b_p + 8 * x, x ? n_p1++ : n_p0++);
-                    if (bad) break;
+                    const uint32_t tile = n + (single ? (i & ~1) + x : i >> 1), st = tile & 1;
+                    if (!odd && (single || x == 0)) go(b_vfull + 8 * st, tile >> 1);
+                    go(b_p + 8 * place, np >> 1);
                     tc_after();
-                    const uint64_t bd = tc_desc(v0 + st * C::TILE, C::HALF);
+                    const uint32_t bd = (v0 + st * C::TILE + (i & 1) * (MKH * 128)) >> 4, to = tm + C::TO + x * D;
+                    if (leader && !bad) {
 #pragma unroll
-                    for (int ks = 0; ks < MKT / 16; ++ks)
-                        tc_mma_ts(tm + C::TO + x * D, tm + C::TP + x * C::TPX + 8 * ks, bd + ks * (2048 >> 4), ID_O, i > 0 || ks > 0);
-                    if (single || x == 1) tc_commit(b_vfree + 8 * st);
-                    if (i + 1 == mine) tc_commit(b_o + 8 * x);
-                }
-                if (i + 1 < mine) {
-                    const uint32_t tile = n + (single ? 2 * (i + 1) + x : i + 1), st = tile & 1;
-                    wait(b_kfull + 8 * st, tile >> 1);
-                    if (bad) break;
-                    tc_after();
-                    const uint64_t ad = tc_desc(q0 + x * C::TILE, 16), bd = tc_desc(k0 + st * C::TILE, 16);
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const uint32_t o = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
-                        tc_mma_ss(tm + C::TS + x * 128, ad + o, bd + o, ID_S, ks > 0);
+                        for (int ks = 0; ks < MKH / 16; ++ks)
+                            tc_mma_ts(to, ts + C::TP + 8 * ks, tc_desc(bd + ks * (2048 >> 4), C::HALF), ID_O, i > 0 || ks > 0);
+                        if (odd && both) tc_commit(b_vfree + 8 * st);
+                        if (i + 2 == mine) tc_commit(b_f + 8 * x);
+                        if (i + 1 == mine) tc_commit(b_o + 8 * x);
                     }
-                    tc_commit(b_s + 8 * x);
-                    if (single || x == 1) tc_commit(b_kfree + 8 * st);
                 }
+                if (i + 2 < mine) {
+                    const int k = i + 2;
+                    const uint32_t tile = n + (single ? (k & ~1) + x : k >> 1), st = tile & 1;
+                    if (!odd && (single || x == 0)) go(b_kfull + 8 * st, tile >> 1);
+                    const uint32_t ad = (q0 + x * C::TILE) >> 4, bd = (k0 + st * C::TILE + (k & 1) * (MKH * 128)) >> 4;
+                    if (leader && !bad) {
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            const uint32_t o = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
+                            tc_mma_ss(ts, tc_desc(ad + o, 16), tc_desc(bd + o, 16), ID_S, ks > 0);
+                        }
+                        tc_commit(b_s + 8 * place);
+                        if (odd && both) tc_commit(b_kfree + 8 * st);
+                    }
+                }
+                __syncwarp();
             }
             n += max(T, 0);
+            np0 += max(cnt0, 0), np1 += max(cnt1, 0);
             ++segs;
         } while (seg.next(a, R, RT));
-        tc_commit(b_end);  // nothing runs on when the columns are given back
+        if (leader) tc_commit(b_end);  // nothing runs on when the columns are given back
         if (!mbar_wait(b_end, 0)) bad = true;
-      }
     }
     if (bad) any_timeout = 1;
     __syncwarp();

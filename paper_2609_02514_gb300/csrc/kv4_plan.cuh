@@ -141,20 +141,21 @@ __device__ __forceinline__ void kv4_put_info(const Kv4Att &a, const Kv4Ws &ws, c
 template <int KT, int TPU>
 struct Kv4Seg {
     unsigned long long left;  // units after this segment
-    int e, h, x0, x1;
+    int b, rt, h, x0, x1;
     Kv4Keys key;
     __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
-        e = at.e, h = at.h, x0 = at.off, left = at.left;
+        b = at.e / RT, rt = at.e - b * RT, h = at.h, x0 = at.off, left = at.left;
         if (left == 0) return false;
-        key = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+        key = kv4_keys<KT, TPU>(a, R, b, rt);
         take();
         return true;
     }
     __device__ __forceinline__ bool next(const Kv4Att &a, int R, int RT) {
         if (left == 0) return false;
         if (++h == a.H) {
-            h = 0, ++e;
-            key = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+            h = 0;
+            if (++rt == RT) rt = 0, ++b;
+            key = kv4_keys<KT, TPU>(a, R, b, rt);
         }
         x0 = 0;
         take();
@@ -164,6 +165,8 @@ struct Kv4Seg {
         x1 = (int)min((unsigned long long)key.units, x0 + left);
         left -= x1 - x0;
     }
+    // first row of the item's key head in a plane
+    __device__ __forceinline__ size_t row0(const Kv4Att &a) const { return (size_t)((size_t)b * a.H + h) * a.S; }
     __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == key.units; }
 };
 
