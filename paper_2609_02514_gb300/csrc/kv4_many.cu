@@ -13,10 +13,9 @@
 //     the 128-byte swizzle.  Keys and values lie alike ([key][64 channels] a
 //     half): the keys' product reads them along the channels, the values' along
 //     the keys (the transposed form of the second operand).
-//   - one warp issues the products, 64 keys at a time: S = Q K' (both from shared
-//     memory) into one of a group's two places, O += P V (P from TMEM, where S
-//     was).  While a group turns one S into P the next is made, so neither waits
-//     for the other's whole chain.
+//   - one warp issues the products: S = Q K' of a tile (both from shared memory),
+//     O += P V of half a tile at a time (P from TMEM, in the place of its half of
+//     S).  While one group turns its scores into weights the other's products run.
 // The tensor pipe runs products in the order they were issued, so an S may be
 // made in the place of a P whose product is under way.
 // Sums are rescaled only when a row's maximum grew by more than 2^8 (in the
@@ -31,7 +30,7 @@
 namespace aces {
 
 constexpr int MKT = 128;                  // keys of a tile
-constexpr int MKH = 64;                   // keys of a product
+constexpr int MKH = 64;                   // keys of a step of weights
 constexpr int MSM = 8, MDQ = 7;           // softmax and dequantising warps
 constexpr int MT = (MSM + MDQ + 1) * 32;  // and the one that issues: 16 warps of 128 registers
 constexpr int MDT = MDQ * 32;
@@ -173,7 +172,7 @@ struct Many {
     static constexpr int PIECES = MKT * D / 32;            // 16-byte pieces of a tile's codes
     static constexpr int PC = (PIECES + MDT - 1) / MDT;    // that a thread dequantises (a warp's last may be none)
     static_assert(PIECES % 32 == 0, "whole warps");
-    static constexpr int TS = 0, TP = 32, TO = 256;        // TMEM columns: S[group][2] of 64, P in the second half of S, O[group]
+    static constexpr int TS = 0, TP = 32, TO = 256;        // TMEM columns: S[group], a half's P in the second half of that half, O[group]
 };
 
 // Byte of 16-byte chunk c (eight channels) of a row in a swizzled tile.
@@ -241,7 +240,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     using C = Many<D>;
     using Seg = Kv4Seg<MKT, 1>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) unsigned long long bars[23];
+    __shared__ __align__(8) unsigned long long bars[21];
     __shared__ uint32_t tmem_base;
     __shared__ float sm_m[2][128], sm_l[2][128];
     __shared__ int any_timeout;
@@ -252,9 +251,9 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     const uint32_t sm0 = smem_u32(smem);
     uint8_t *sq = smem, *sk = smem + 2 * C::TILE, *sv = smem + 4 * C::TILE;
     const uint32_t bar0 = smem_u32(bars);
-    // barriers by stage (keys, values), by group, or by group and place (2 x + place)
+    // barriers by stage (keys, values), by group, or by group and half (2 x + half)
     const uint32_t b_kfull = bar0, b_kfree = bar0 + 16, b_vfull = bar0 + 32, b_vfree = bar0 + 48, b_o = bar0 + 64, b_q = bar0 + 80,
-                   b_s = bar0 + 96, b_p = bar0 + 128, b_f = bar0 + 160, b_end = bar0 + 176;
+                   b_s = bar0 + 96, b_f = bar0 + 112, b_p = bar0 + 128, b_end = bar0 + 160;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(b_kfull + 8 * i, MDQ);
@@ -262,13 +261,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             mbar_init(b_kfree + 8 * i, 1);
             mbar_init(b_vfree + 8 * i, 1);
             mbar_init(b_o + 8 * i, 1);
-            mbar_init(b_f + 8 * i, 1);
             mbar_init(b_q + 8 * i, 4);
-        }
-        for (int i = 0; i < 4; ++i) {
             mbar_init(b_s + 8 * i, 1);
-            mbar_init(b_p + 8 * i, 4);
+            mbar_init(b_f + 8 * i, 1);
         }
+        for (int i = 0; i < 4; ++i) mbar_init(b_p + 8 * i, 4);
         mbar_init(b_end, 1);
         any_timeout = 0;
     }
@@ -297,7 +294,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tm + lanes + C::TS + x * 128, tO = tm + lanes + C::TO + x * D;
         uint8_t *myq = sq + x * C::TILE;
-        uint32_t n_s = 0, n_o = 0;  // products of scores, and segments, that were waited for
+        uint32_t n_s = 0, n_o = 0;  // tiles and segments before this one
         bool first = true;
         do {
             const Kv4Keys &key = seg.key;
@@ -346,14 +343,16 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             if (lane == 0) mbar_arrive(b_q + 8 * x);
             float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
 #pragma unroll 1
-            for (int y = 0; y < mine; ++y, ++n_s) {
-                const uint32_t place = n_s & 1, phase = n_s >> 1, bp = 8 * (2 * x + place);
-                wait(b_s + bp, phase);
-                tc_after();
+            for (int y = 0; y < mine; ++y) {
+                const int half = y & 1;
+                if (half == 0) {
+                    wait(b_s + 8 * x, n_s);
+                    tc_after();
+                }
                 if (warp_live) {
-                    const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + (y & 1) * MKH;
+                    const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + half * MKH;
                     const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > a.sinks);
-                    const uint32_t at = tS + place * MKH;
+                    const uint32_t at = tS + half * MKH;
                     float v[2][32];
                     tc_ld32(at, v[0]);
                     tc_ld32(at + 32, v[1]);
@@ -383,12 +382,9 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                         if (grew) m = mx;
                         l0 *= f, l1 *= f;
                         if (y > 0) {
-                            // the last product has been added: before the next scores
-                            // were made, and for the last ones by a word of its own
-                            if (y + 1 < mine)
-                                wait(b_s + 8 * (2 * x + (place ^ 1)), (n_s + 1) >> 1);
-                            else
-                                wait(b_f + 8 * x, n_o);
+                            // what was added last is there: before these scores were
+                            // made, or (the first half's) by a word of its own
+                            if (half == 1) wait(b_f + 8 * x, n_s);
                             tc_after();
 #pragma unroll 1
                             for (int w = 0; w < D / 16; ++w) {
@@ -422,7 +418,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 }
                 tc_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(b_p + bp);
+                if (lane == 0) mbar_arrive(b_p + 8 * (2 * x + half));
+                n_s += half;
             }
             if (mine > 0) {
                 wait(b_o + 8 * x, n_o++);
@@ -532,15 +529,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     } else if (warp < MSM + MDQ) {
         // -- codes to bfloat16 tiles ------------------------------------------
         const int dt = tid - MSM * 32;
-        // Steps: the keys of two tiles, then their values (of a segment's last, odd
-        // tile its keys and values): with a group's scores two products ahead of its
-        // values, keys are wanted a tile before the other group's last values are
-        // done, so values must not come between.  The next step's rows are loaded
+        // Steps: a tile's keys, then its values.  The next step's rows are loaded
         // while one is turned.
         Piece<D> cur[C::PC], nxt[C::PC];
-        int y = seg.x0;     // first tile of the two
-        uint32_t n = 0;     // and its number in the rings
-        int r = 0;          // step of the two tiles
+        int y = seg.x0;
+        uint32_t step = 0;  // the one to load: 2 x the tile's number in the rings (+ 1: values)
         bool more = true;
         // Rows are asked into the L2 AHEAD tiles before they are loaded (memory's
         // latency at its full rate is about two tiles of every SM), a line of a
@@ -565,8 +558,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             for (int u = 0; u < C::PC; ++u)
                 if (dt + u * MDT < C::PIECES) load_piece<D>(base, j0, last, dt + u * MDT, nxt[u]);
         };
-        bool fresh = true, some = false, cur_v = false;
-        uint32_t cur_n = 0;
+        bool fresh = true;
 #pragma unroll 1
         while (true) {  // loads a step, and turns the one before
             while (more && y >= min(seg.x1, seg.key.tiles)) {
@@ -574,38 +566,33 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 y = seg.x0;
                 fresh = true;
             }
-            uint32_t nxt_n = 0;
-            bool nxt_v = false;
             if (more) {
-                const bool two = y + 1 < min(seg.x1, seg.key.tiles);
-                const int t = two ? r & 1 : 0;
-                nxt_v = two ? r >> 1 : r;
-                nxt_n = n + t;
-                j0 = kv4_tile<MKT>(seg.key, y + t);
                 if (fresh) {
                     fresh = false;
                     kb = a.k + seg.row0(a) * C::RB, vb = a.v + seg.row0(a) * C::RB;
 #pragma unroll 1
                     for (int u = 1; u < AHEAD; ++u) prefetch(y + u);
                 }
-                if (!nxt_v) prefetch(y + t + AHEAD);
-                load(nxt_v);
-                if (++r == (two ? 4 : 2)) r = 0, y += two ? 2 : 1, n += two ? 2 : 1;
+                if ((step & 1) == 0) {
+                    j0 = kv4_tile<MKT>(seg.key, y);
+                    prefetch(y + AHEAD);
+                }
+                load(step & 1);
+                y += step & 1;
             }
-            if (some) {
-                const uint32_t st = cur_n & 1;
-                wait((cur_v ? b_vfree : b_kfree) + 8 * st, (cur_n >> 1) + 1);
-                uint8_t *tile = (cur_v ? sv : sk) + st * C::TILE;
+            if (step > 0) {
+                const uint32_t st = (step - 1) >> 1 & 1, v = (step - 1) & 1;
+                wait((v ? b_vfree : b_kfree) + 8 * st, ((step - 1) >> 2) + 1);
+                uint8_t *tile = (v ? sv : sk) + st * C::TILE;
 #pragma unroll
                 for (int u = 0; u < C::PC; ++u)
                     if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, cur[u]);
                 async_fence();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((cur_v ? b_vfull : b_kfull) + 8 * st);
+                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
             }
             if (!more) break;
-            some = true;
-            cur_n = nxt_n, cur_v = nxt_v;
+            ++step;
 #pragma unroll
             for (int u = 0; u < C::PC; ++u) cur[u] = nxt[u];
         }
@@ -613,7 +600,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         // -- products: the whole warp goes along, so that addresses stay in uniform
         // registers, and one lane issues -------------------------------------
         const uint32_t q0 = sm0, k0 = sm0 + 2 * C::TILE, v0 = sm0 + 4 * C::TILE;
-        constexpr uint32_t ID_S = tc_idesc(MKH, false), ID_O = tc_idesc(D, true);
+        constexpr uint32_t ID_S = tc_idesc(MKT, false), ID_O = tc_idesc(D, true);
         const bool leader = elect_one();
         auto go = [&](uint32_t bar, uint32_t phase) {  // wait(), with one answer for the warp
             if (bad) return;
@@ -621,54 +608,58 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 if (mbar_try(bar, phase & 1)) return;
             bad = !__all_sync(0xffffffffu, mbar_wait_slow(bar, phase & 1));
         };
-        uint32_t n = 0, segs = 0, np0 = 0, np1 = 0;  // tiles, segments and each group's products of scores so far
+        uint32_t n = 0, segs = 0, n0 = 0, n1 = 0;  // tiles, segments and each group's tiles so far
         do {
             const bool single = NR - seg.rt * R <= 128;
             const int T = __shfl_sync(0xffffffffu, min(seg.x1, seg.key.tiles) - seg.x0, 0);
-            const int cnt0 = 2 * (single ? (T + 1) >> 1 : T), cnt1 = 2 * (single ? T >> 1 : T);
+            const int cnt0 = single ? (T + 1) >> 1 : T, cnt1 = single ? T >> 1 : T;
             go(b_q, segs);
             go(b_q + 8, segs);
-            // each group in turn: the values of its 64 keys i, then the scores of i + 2
+            // each group in turn: the values of its tile i, then the scores of i + 1
 #pragma unroll 1
-            for (int u = -4; u < 2 * cnt0 && !bad; ++u) {
-                const int x = u & 1, i = u >> 1, mine = x ? cnt1 : cnt0;  // i from -2
-                const uint32_t np = (x ? np1 : np0) + i;                   // the product's number
-                const uint32_t place = 2 * x + (np & 1), ts = tm + C::TS + place * MKH;
-                const bool both = single || x == 1, odd = i & 1;           // a tile's first use, its last
+            for (int u = -2; u < 2 * cnt0 && !bad; ++u) {
+                const int x = u & 1, i = u >> 1, mine = x ? cnt1 : cnt0;  // i from -1
+                const uint32_t ts = tm + C::TS + x * MKT;
+                const bool first = single || x == 0, last = single || x == 1;  // of a tile's users
                 if (i >= 0 && i < mine) {
-                    const uint32_t tile = n + (single ? (i & ~1) + x : i >> 1), st = tile & 1;
-                    if (!odd && (single || x == 0)) go(b_vfull + 8 * st, tile >> 1);
-                    go(b_p + 8 * place, np >> 1);
-                    tc_after();
-                    const uint32_t bd = (v0 + st * C::TILE + (i & 1) * (MKH * 128)) >> 4, to = tm + C::TO + x * D;
-                    if (leader && !bad) {
+                    const uint32_t tile = n + (single ? 2 * i + x : i), st = tile & 1, ph = (x ? n1 : n0) + i;
+                    const uint32_t bd = (v0 + st * C::TILE) >> 4, to = tm + C::TO + x * D;
+                    if (first) go(b_vfull + 8 * st, tile >> 1);
 #pragma unroll
-                        for (int ks = 0; ks < MKH / 16; ++ks)
-                            tc_mma_ts(to, ts + C::TP + 8 * ks, tc_desc(bd + ks * (2048 >> 4), C::HALF), ID_O, i > 0 || ks > 0);
-                        if (odd && both) tc_commit(b_vfree + 8 * st);
-                        if (i + 2 == mine) tc_commit(b_f + 8 * x);
+                    for (int half = 0; half < 2; ++half) {
+                        go(b_p + 8 * (2 * x + half), ph);
+                        tc_after();
+                        if (leader && !bad) {
+#pragma unroll
+                            for (int ks = 0; ks < MKH / 16; ++ks)
+                                tc_mma_ts(to, ts + half * MKH + C::TP + 8 * ks, tc_desc(bd + (half * (MKH / 16) + ks) * (2048 >> 4), C::HALF),
+                                          ID_O, i > 0 || half > 0 || ks > 0);
+                            if (half == 0) tc_commit(b_f + 8 * x);
+                        }
+                    }
+                    if (leader && !bad) {
+                        if (last) tc_commit(b_vfree + 8 * st);
                         if (i + 1 == mine) tc_commit(b_o + 8 * x);
                     }
                 }
-                if (i + 2 < mine) {
-                    const int k = i + 2;
-                    const uint32_t tile = n + (single ? (k & ~1) + x : k >> 1), st = tile & 1;
-                    if (!odd && (single || x == 0)) go(b_kfull + 8 * st, tile >> 1);
-                    const uint32_t ad = (q0 + x * C::TILE) >> 4, bd = (k0 + st * C::TILE + (k & 1) * (MKH * 128)) >> 4;
+                if (i + 1 < mine) {
+                    const uint32_t tile = n + (single ? 2 * (i + 1) + x : i + 1), st = tile & 1;
+                    if (first) go(b_kfull + 8 * st, tile >> 1);
+                    const uint32_t ad = (q0 + x * C::TILE) >> 4, bd = (k0 + st * C::TILE) >> 4;
                     if (leader && !bad) {
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks) {
                             const uint32_t o = ((ks >> 2) * C::HALF + (ks & 3) * 32) >> 4;
                             tc_mma_ss(ts, tc_desc(ad + o, 16), tc_desc(bd + o, 16), ID_S, ks > 0);
                         }
-                        tc_commit(b_s + 8 * place);
-                        if (odd && both) tc_commit(b_kfree + 8 * st);
+                        tc_commit(b_s + 8 * x);
+                        if (last) tc_commit(b_kfree + 8 * st);
                     }
                 }
                 __syncwarp();
             }
             n += max(T, 0);
-            np0 += max(cnt0, 0), np1 += max(cnt1, 0);
+            n0 += max(cnt0, 0), n1 += max(cnt1, 0);
             ++segs;
         } while (seg.next(a, R, RT));
         if (leader) tc_commit(b_end);  // nothing runs on when the columns are given back
