@@ -3,13 +3,15 @@
 // tensor cores.
 //
 // A persistent CTA an SM works on items of up to 256 query rows, 128 keys a
-// tile, with its warps in four parts:
+// tile, with its warps in five parts:
 //   - two softmax groups of four warps, a thread a row: each has 128 rows of
 //     scores S, of weights P and of sums O in TMEM and its queries in shared
 //     memory.  With more than 128 rows the groups have a half each and share
 //     the tiles; with up to 128 both have the same rows and every other tile,
 //     and are merged at the end.
-//   - seven warps turn the rows' codes into bfloat16 tiles in shared memory, in
+//   - one warp brings tiles of rows into a ring in shared memory (bulk copies, as a
+//     tile's rows lie in one piece);
+//   - six warps turn their codes into bfloat16 tiles in shared memory, in
 //     the 128-byte swizzle.  Keys and values lie alike ([key][64 channels] a
 //     half): the keys' product reads them along the channels, the values' along
 //     the keys (the transposed form of the second operand).
@@ -31,8 +33,9 @@ namespace aces {
 
 constexpr int MKT = 128;                  // keys of a tile
 constexpr int MKH = 64;                   // keys of a step of weights
-constexpr int MSM = 8, MDQ = 7;           // softmax and dequantising warps
-constexpr int MT = (MSM + MDQ + 1) * 32;  // and the one that issues: 16 warps of 128 registers
+constexpr int MSM = 8, MDQ = 6;           // softmax and dequantising warps
+constexpr int MLD = MSM + MDQ, MMM = MLD + 1;  // the warp that loads, the one that issues
+constexpr int MT = (MMM + 1) * 32;        // 16 warps of 128 registers
 constexpr int MDT = MDQ * 32;
 constexpr float M_LAZY = 8.0f;
 // -- tcgen05 ------------------------------------------------------------------
@@ -168,7 +171,8 @@ struct Many {
     static constexpr int RB = kv4_row_bytes(D);
     static constexpr int HALF = MKT * 128;                 // 128 rows of 64 channels
     static constexpr int TILE = MKT * D * 2;
-    static constexpr int SMEM = 6 * TILE + 1024;           // queries of two groups, two stages of keys and values
+    static constexpr int RAW = MKT * RB, NR = D == 128 ? 3 : 6;  // a tile's keys or values as they are, and how many
+    static constexpr int SMEM = 6 * TILE + NR * RAW + 1024;  // queries of two groups, two stages of keys and values
     static constexpr int PIECES = MKT * D / 32;            // 16-byte pieces of a tile's codes
     static constexpr int PC = (PIECES + MDT - 1) / MDT;    // that a thread dequantises (a warp's last may be none)
     static_assert(PIECES % 32 == 0, "whole warps");
@@ -184,19 +188,16 @@ struct Piece {  // 32 channels of a row and their t's
     uint32_t t[D == 128 ? 1 : 2];
 };
 
-// Piece p of the tile at j0 (base: the key head's first row).  Without a branch
-// and without a use, so a thread's loads are all under way at once.  Rows past
-// the sequence are its last one again: their weights are 0.
 template <int D>
-__device__ __forceinline__ void load_piece(const uint8_t *base, int j0, int last, int p, Piece<D> &o) {
+__device__ __forceinline__ void load_piece(const uint8_t *raw, int p, Piece<D> &o) {
     constexpr int Q = D / 32;
     const int q = p % Q;
-    const uint8_t *r = base + (unsigned long long)(uint32_t)min(j0 + p / Q, last) * (uint32_t)Many<D>::RB;
-    o.w = __ldg(reinterpret_cast<const uint4 *>(r) + q);
+    const uint8_t *r = raw + p / Q * Many<D>::RB;
+    o.w = reinterpret_cast<const uint4 *>(r)[q];
     if (D == 128) {
-        o.t[0] = __ldg(reinterpret_cast<const uint32_t *>(r + D / 2) + q);
+        o.t[0] = reinterpret_cast<const uint32_t *>(r + D / 2)[q];
     } else {
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(r + D / 2) + q);
+        const uint2 v = reinterpret_cast<const uint2 *>(r + D / 2)[q];
         o.t[0] = v.x;
         o.t[D == 128 ? 0 : 1] = v.y;
     }
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     using C = Many<D>;
     using Seg = Kv4Seg<MKT, 1>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) unsigned long long bars[21];
+    __shared__ __align__(8) unsigned long long bars[33];
     __shared__ uint32_t tmem_base;
     __shared__ float sm_m[2][128], sm_l[2][128];
     __shared__ int any_timeout;
@@ -249,11 +250,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     // tiles start on 1024 bytes
     uint8_t *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const uint32_t sm0 = smem_u32(smem);
-    uint8_t *sq = smem, *sk = smem + 2 * C::TILE, *sv = smem + 4 * C::TILE;
+    uint8_t *sq = smem, *sk = smem + 2 * C::TILE, *sv = smem + 4 * C::TILE, *raw = smem + 6 * C::TILE;
     const uint32_t bar0 = smem_u32(bars);
     // barriers by stage (keys, values), by group, or by group and half (2 x + half)
     const uint32_t b_kfull = bar0, b_kfree = bar0 + 16, b_vfull = bar0 + 32, b_vfree = bar0 + 48, b_o = bar0 + 64, b_q = bar0 + 80,
-                   b_s = bar0 + 96, b_f = bar0 + 112, b_p = bar0 + 128, b_end = bar0 + 160;
+                   b_s = bar0 + 96, b_f = bar0 + 112, b_p = bar0 + 128, b_end = bar0 + 160, b_rfull = bar0 + 168, b_rfree = bar0 + 216;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(b_kfull + 8 * i, MDQ);
@@ -266,6 +267,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             mbar_init(b_f + 8 * i, 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(b_p + 8 * i, 4);
+        for (int i = 0; i < C::NR; ++i) {
+            mbar_init(b_rfull + 8 * i, 1);
+            mbar_init(b_rfree + 8 * i, MDQ);
+        }
         mbar_init(b_end, 1);
         any_timeout = 0;
     }
@@ -274,7 +279,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     if (tid == 0) kv4_put_info<MKT, 1>(a, ws, at, R, RT);
     Seg seg;
     if (!seg.start(a, R, RT, at)) return;
-    if (warp == MSM + MDQ) {
+    if (warp == MMM) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         tc_before();
@@ -529,72 +534,66 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     } else if (warp < MSM + MDQ) {
         // -- codes to bfloat16 tiles ------------------------------------------
         const int dt = tid - MSM * 32;
-        // Steps: a tile's keys, then its values.  The next step's rows are loaded
-        // while one is turned.
-        Piece<D> cur[C::PC], nxt[C::PC];
-        int y = seg.x0;
-        uint32_t step = 0;  // the one to load: 2 x the tile's number in the rings (+ 1: values)
-        bool more = true;
-        // Rows are asked into the L2 AHEAD tiles before they are loaded (memory's
-        // latency at its full rate is about two tiles of every SM), a line of a
-        // tile's keys or values a thread.
-        constexpr int AHEAD = 6, LINES = MKT * C::RB / 128;
-        static_assert(MKT * C::RB % 128 == 0 && 2 * LINES <= MDT, "a line a thread");
-        const uint8_t *kb = a.k, *vb = a.v;  // the key head's rows
-        int j0 = 0;
-        auto prefetch = [&](int x) {
-            if (x >= min(seg.x1, seg.key.tiles) || dt >= 2 * LINES) return;
-            const int first = kv4_tile<MKT>(seg.key, x), rows = min(MKT, seg.key.P + seg.key.cnt - first);
-            const int line = dt < LINES ? dt : dt - LINES;
-            if (line * 128 >= rows * C::RB) return;
-            const uint8_t *at = (dt < LINES ? kb : vb) + (unsigned long long)(uint32_t)first * (uint32_t)C::RB + line * 128;
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
-        };
-        auto load = [&](bool values) {
-            const int last = seg.key.P + seg.key.cnt - 1;
-            if (!ACES_IN(j0, a.S) || !ACES_IN(last, a.S)) return;
-            const uint8_t *base = values ? vb : kb;
+        uint32_t step = 0;  // 2 x the tile's number (+ 1: its values)
+        do {
+            const int T = min(seg.x1, seg.key.tiles) - seg.x0;
+#pragma unroll 1
+            for (int y = 0; y < 2 * T; ++y, ++step) {
+                const uint32_t st = (step >> 1) & 1, v = step & 1, rs = step % C::NR;
+                Piece<D> p[C::PC];
+                wait(b_rfull + 8 * rs, step / C::NR);
 #pragma unroll
-            for (int u = 0; u < C::PC; ++u)
-                if (dt + u * MDT < C::PIECES) load_piece<D>(base, j0, last, dt + u * MDT, nxt[u]);
-        };
-        bool fresh = true;
-#pragma unroll 1
-        while (true) {  // loads a step, and turns the one before
-            while (more && y >= min(seg.x1, seg.key.tiles)) {
-                more = seg.next(a, R, RT);
-                y = seg.x0;
-                fresh = true;
-            }
-            if (more) {
-                if (fresh) {
-                    fresh = false;
-                    kb = a.k + seg.row0(a) * C::RB, vb = a.v + seg.row0(a) * C::RB;
-#pragma unroll 1
-                    for (int u = 1; u < AHEAD; ++u) prefetch(y + u);
-                }
-                if ((step & 1) == 0) {
-                    j0 = kv4_tile<MKT>(seg.key, y);
-                    prefetch(y + AHEAD);
-                }
-                load(step & 1);
-                y += step & 1;
-            }
-            if (step > 0) {
-                const uint32_t st = (step - 1) >> 1 & 1, v = (step - 1) & 1;
-                wait((v ? b_vfree : b_kfree) + 8 * st, ((step - 1) >> 2) + 1);
+                for (int u = 0; u < C::PC; ++u)
+                    if (dt + u * MDT < C::PIECES) load_piece<D>(raw + rs * C::RAW, dt + u * MDT, p[u]);
+                wait((v ? b_vfree : b_kfree) + 8 * st, (step >> 2) + 1);
                 uint8_t *tile = (v ? sv : sk) + st * C::TILE;
 #pragma unroll
                 for (int u = 0; u < C::PC; ++u)
-                    if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, cur[u]);
+                    if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, p[u]);
                 async_fence();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+                if (lane == 0) {
+                    mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+                    mbar_arrive(b_rfree + 8 * rs);
+                }
             }
-            if (!more) break;
-            ++step;
-#pragma unroll
-            for (int u = 0; u < C::PC; ++u) cur[u] = nxt[u];
+        } while (seg.next(a, R, RT));
+    } else if (warp == MLD) {
+        // -- rows into the ring: keys, values, keys ... -----------------------
+        if (lane == 0) {
+            // Rows are asked into the L2 AHEAD tiles before they are loaded: memory's
+            // latency at its full rate is more than the ring holds.
+            constexpr int AHEAD = 6;
+            const uint32_t raw0 = smem_u32(raw);
+            uint32_t step = 0;
+            do {
+                const uint8_t *kb = a.k + seg.row0(a) * C::RB, *vb = a.v + seg.row0(a) * C::RB;  // the key head's rows
+                const int top = min(seg.x1, seg.key.tiles), end = seg.key.P + seg.key.cnt;
+                int ahead = seg.x0 + 1;
+#pragma unroll 1
+                for (int y = seg.x0; y < top; ++y) {
+                    for (; ahead < min(top, y + AHEAD); ++ahead) {
+                        const int j0 = kv4_tile<MKT>(seg.key, ahead);
+                        const uint32_t bytes = min(MKT, end - j0) * C::RB;
+                        const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)C::RB;
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(kb + off), "r"(bytes) : "memory");
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(vb + off), "r"(bytes) : "memory");
+                    }
+                    const int j0 = kv4_tile<MKT>(seg.key, y);
+                    // past the sequence's end the ring keeps what it has: any bytes are
+                    // numbers, and their weights are 0
+                    const uint32_t bytes = min(MKT, end - j0) * C::RB;
+                    const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)C::RB;
+                    const bool in = ACES_IN(j0, a.S) && ACES_IN(end - 1, a.S);
+#pragma unroll 1
+                    for (int v = 0; v < 2; ++v, ++step) {
+                        const uint32_t rs = step % C::NR;
+                        wait(b_rfree + 8 * rs, step / C::NR + 1);
+                        mbar_expect(b_rfull + 8 * rs, in ? bytes : 0);
+                        if (in) bulk_load(raw0 + rs * C::RAW, (v ? vb : kb) + off, bytes, b_rfull + 8 * rs);
+                    }
+                }
+            } while (seg.next(a, R, RT));
         }
     } else {
         // -- products: the whole warp goes along, so that addresses stay in uniform
@@ -670,7 +669,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     tc_before();
     __syncthreads();
     if (tid == 0 && any_timeout) ws.info[blockIdx.x].timeout = 1;
-    if (warp == MSM + MDQ) {
+    if (warp == MMM) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
     }
