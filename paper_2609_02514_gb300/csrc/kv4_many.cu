@@ -545,6 +545,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
 #pragma unroll
                 for (int u = 0; u < C::PC; ++u)
                     if (dt + u * MDT < C::PIECES) load_piece<D>(raw + rs * C::RAW, dt + u * MDT, p[u]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_rfree + 8 * rs);
                 wait((v ? b_vfree : b_kfree) + 8 * st, (step >> 2) + 1);
                 uint8_t *tile = (v ? sv : sk) + st * C::TILE;
 #pragma unroll
@@ -552,10 +554,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, p[u]);
                 async_fence();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
-                    mbar_arrive(b_rfree + 8 * rs);
-                }
+                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
             }
         } while (seg.next(a, R, RT));
     } else if (warp == MLD) {
