@@ -10,6 +10,7 @@ namespace aces {
 constexpr int FW = 8;            // warps
 constexpr int FT = FW * 32;
 constexpr int FKT = 32;          // keys of a tile: one warp's step
+constexpr float F_LAZY = 8.0f;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -47,7 +48,7 @@ struct Few {
 // words have, the same in both operands.  P' needs its pairs along the keys,
 // where S' has them along the rows: movmatrix turns the 8 x 8 blocks.
 template <int D, bool F32, int NT>
-__global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT) {
+__global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT, int direct) {
     using C = Few<D, F32, NT>;
     constexpr int RB = C::RB, R = C::R, KS = C::KS, JT = C::JT, WPT = C::WPT, ST = C::ST, SPL = C::SPL;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -64,27 +65,32 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (lane == 0)
         for (int s = 0; s < ST; ++s) mbar_init(bar0 + 8 * s, 1);
     if (tid == 0) any_timeout = 0;
+    if (!direct) pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
     using Seg = Kv4Seg<FKT, FW>;
-    const Kv4Start at = kv4_start<FKT, FW, FT>(a, R, RT);  // has a __syncthreads after the barriers' start
-    if (tid == 0) kv4_put_info<FKT, FW>(a, ws, at, R, RT);
+    const Kv4Start at = direct ? kv4_whole<FKT, FW>(a, R, RT) : kv4_start<FKT, FW, FT>(a, R, RT);
+    if (tid == 0 && !direct) kv4_put_info<FKT, FW>(a, ws, at, R, RT);
+    __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
     if (!cur.start(a, R, RT, at)) return;
 
     int seq = 0;       // tiles this warp has taken, of all segments
     bool bad = false;  // a wait gave up
     // this warp's y-th tile of the segment, into the ring's next place
+    const uint8_t *kb = nullptr, *vb = nullptr;  // the key head's rows
+    auto place_rows = [&](const Seg &g) { kb = a.k + g.row0(a) * RB, vb = a.v + g.row0(a) * RB; };
+    place_rows(cur);
     auto issue = [&](const Seg &g, int y, int place) {
         if (lane != 0) return;
         const int j0 = kv4_tile<FKT>(g.key, (g.x0 + y) * FW + warp), rows = min(FKT, g.key.P + g.key.cnt - j0);
         if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
         const int s = place % ST;
         const uint32_t bytes = rows * RB, dst = ring + s * C::STAGE;
-        const size_t off = (g.row0(a) + j0) * RB;
+        const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)RB;
         mbar_expect(bar0 + 8 * s, 2 * bytes);
-        bulk_load(dst, a.k + off, bytes, bar0 + 8 * s);
-        bulk_load(dst + FKT * RB, a.v + off, bytes, bar0 + 8 * s);
+        bulk_load(dst, kb + off, bytes, bar0 + 8 * s);
+        bulk_load(dst + FKT * RB, vb + off, bytes, bar0 + 8 * s);
     };
     auto my_tiles = [&](const Seg &g) {
         const int top = min(g.x1 * FW, g.key.tiles) - g.x0 * FW - warp;
@@ -238,7 +244,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float mn = fmaxf(m[nt][c], mx);
+                    // (rescaled only when the maximum grew by more than 2^8: weights stay below
+                    // that and lose nothing by it)
+                    float mn = mx > m[nt][c] + F_LAZY || m[nt][c] == -INFINITY ? fmaxf(m[nt][c], mx) : m[nt][c];
                     if (__any_sync(0xffffffffu, mn > m[nt][c])) {
                         const float f = mn == -INFINITY ? 1.0f : ex2(m[nt][c] - mn);
                         m[nt][c] = mn;
@@ -328,6 +336,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         const bool whole = cur.whole();
         const bool more = cur.next(a, R, RT);
         mine = more ? my_tiles(cur) : 0;
+        if (more) place_rows(cur);
         for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
         // merge the warps
 #pragma unroll
@@ -399,86 +408,108 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         first = false;
         if (!more) break;
     }
-    if (tid == 0 && any_timeout) ws.info[blockIdx.x].timeout = 1;
+    if (tid == 0 && any_timeout) {
+        if (direct)
+            atomicOr(a.status + at.e / RT, ACES_ROW_TIMEOUT);  // seconds after it was written
+        else
+            ws.info[blockIdx.x].timeout = 1;
+    }
 }
 
-// Adds the pieces of an item that several CTAs share, in their order: block c
-// takes the item in which the range of CTA c starts, when c is the first to
-// start inside it.  Block 0 writes the sequences' status.
-constexpr int JT_THREADS = 256;
-template <bool F32>
-__global__ void __launch_bounds__(JT_THREADS) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
+// Adds the pieces of an item that several CTAs share, in their order: block
+// group c (Y blocks) takes the item in which the range of CTA c starts, when c is
+// the first to start inside it.  Block 0 writes the sequences' status.  The grid
+// is launched while the attention runs and waits for its end.
+// A warp takes a row: its lanes the pieces' maxima, then the row's channels.
+constexpr int JN = 256;
+template <int D, bool F32>
+__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
+    constexpr int D4 = D / 4, PW = 32 / D4;  // float4 of a row; pieces a warp reads at a time
     __shared__ int late;
-    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, D = a.D;
+    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, lane = tid & 31;
     pdl_wait();
     if (c == 0) {
         if (y != 0) return;
         if (tid == 0) late = 0;
         __syncthreads();
-        for (int x = tid; x < C; x += JT_THREADS)
+        for (int x = tid; x < C; x += JN)
             if (ws.info[x].timeout) late = 1;
         __syncthreads();
-        for (int b = tid; b < a.B; b += JT_THREADS)
+        for (int b = tid; b < a.B; b += JN)
             a.status[b] = (kv4_seq(a.prefix, a.count, b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE) | (late ? ACES_ROW_TIMEOUT : 0);
         return;
     }
     const Kv4Info in = ws.info[c];
-    if (!in.valid || in.off == 0 || in.off > in.quantum) return;
+    if (in.cnt < 0 || in.off == 0 || in.off > in.quantum) return;
     const int pieces = 1 + (in.units - in.off + in.quantum - 1) / in.quantum;
-    const int s0 = 2 * (c - 1) + (in.off == in.quantum ? 0 : 1);
-    const size_t stride = (size_t)R * (D + 2);
-    auto piece = [&](int p) { return ws.piece + (p == 0 ? s0 : 2 * (c - 1 + p)) * stride; };
-    const int D4 = D / 4;
-    const Kv4Seq sq = kv4_seq(a.prefix, a.count, in.b, a.n, a.S);
-    for (int x = y * JT_THREADS + tid; x < R * D4; x += JT_THREADS * Y) {
-        const int row = x / D4, d4 = x % D4;
-        const long long r = (long long)in.rt * R + row;
-        if (r >= (long long)a.n * a.G) break;
-        const int i = (int)(r / a.G);
-        float M = -INFINITY;
-        for (int p = 0; p < pieces; ++p) M = fmaxf(M, piece(p)[R * D + row]);
+    const int stride = R * (D + 2), NR = min(R, a.n * a.G - in.rt * R);
+    const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off == in.quantum ? 0 : 1)) * stride;
+    const float *rest = ws.piece + (size_t)(2 * (c - 1)) * stride;  // piece p > 0 at 2 p strides
+    auto piece = [&](int p) { return p == 0 ? first : rest + (size_t)(2 * p) * stride; };
+    for (int row = y * (JN / 32) + (tid >> 5); row < NR; row += Y * (JN / 32)) {
+        float M = -INFINITY, L = 0.0f;
+        for (int p = lane; p < pieces; p += 32) M = fmaxf(M, piece(p)[R * D + row]);
+        M = warp_max(M);
         const float ref = M == -INFINITY ? 0.0f : M;
-        float L = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int p0 = 0; p0 < pieces; p0 += 32) {
+            const int np = min(32, pieces - p0);
+            float f = 0.0f;
+            if (lane < np) {
+                const float *pc = piece(p0 + lane) + R * D + row;
+                f = ex2(pc[0] - ref);
+                L = fmaf(pc[R], f, L);
+            }
 #pragma unroll 4
-        for (int p = 0; p < pieces; ++p) {
-            const float *pc = piece(p);
-            const float f = ex2(pc[R * D + row] - ref);
-            const float4 v = *reinterpret_cast<const float4 *>(pc + row * D + 4 * d4);
-            L = fmaf(pc[R * D + R + row], f, L);
-            o.x = fmaf(v.x, f, o.x), o.y = fmaf(v.y, f, o.y), o.z = fmaf(v.z, f, o.z), o.w = fmaf(v.w, f, o.w);
+            for (int q = 0; q < np; q += PW) {
+                const int p = q + lane / D4;
+                const float fp = __shfl_sync(0xffffffffu, f, p & 31);
+                if (p < np) {
+                    const float4 v = *reinterpret_cast<const float4 *>(piece(p0 + p) + row * D + 4 * (lane % D4));
+                    o.x = fmaf(v.x, fp, o.x), o.y = fmaf(v.y, fp, o.y), o.z = fmaf(v.z, fp, o.z), o.w = fmaf(v.w, fp, o.w);
+                }
+            }
         }
-        const bool none = L == 0.0f || !sq.ok || i >= sq.cnt;
+        for (int x = 16; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
+        if (PW == 2) {
+            o.x += __shfl_xor_sync(0xffffffffu, o.x, 16), o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
+            o.z += __shfl_xor_sync(0xffffffffu, o.z, 16), o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
+        }
+        const int r = in.rt * R + row, i = r / a.G;
+        const bool none = L == 0.0f || i >= in.cnt;
         const float k = none ? 0.0f : KV4_STEP / L;
         if (none) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const size_t orow = ((size_t)in.b * a.n + i) * a.Hq + in.h * a.G + r % a.G;
-        if (F32) {
-            reinterpret_cast<float4 *>(a.out)[orow * D4 + d4] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
-        } else {
-            reinterpret_cast<uint2 *>(a.out)[orow * D4 + d4] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
+        const size_t orow = ((size_t)in.b * a.n + i) * a.Hq + in.h * a.G + (r - i * a.G);
+        if (lane < D4) {
+            if (F32)
+                reinterpret_cast<float4 *>(a.out)[orow * D4 + lane] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
+            else
+                reinterpret_cast<uint2 *>(a.out)[orow * D4 + lane] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
         }
-        if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        if (lane == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
 }
 
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
-    const long long rows = (long long)a.n * a.G < R ? (long long)a.n * a.G : R;
-    const int Y = (int)((rows * (a.D / 4) + JT_THREADS - 1) / JT_THREADS);  // blocks of an item: four numbers a thread
-    return a.f32 ? launch_after(k_kv4_join<true>, C * Y, JT_THREADS, 1, s, a, ws, C, R, Y)
-                 : launch_after(k_kv4_join<false>, C * Y, JT_THREADS, 1, s, a, ws, C, R, Y);
+    const int rows = a.n * a.G < R ? a.n * a.G : R, steps = (rows + JN / 32 - 1) / (JN / 32);
+    const int Y = steps < 16 ? steps : 16;  // blocks of an item
+    const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true> : k_kv4_join<64, false>) : (a.f32 ? k_kv4_join<128, true> : k_kv4_join<128, false>);
+    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
 
 template <int D, bool F32, int NT>
 static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
     using C = Few<D, F32, NT>;
-    const int grid = nsm * C::MINB;
-    const Kv4Ws ws = kv4_ws_carve(workspace, grid);
+    const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
+    const long long items = (long long)a.B * RT * a.H;
+    const bool direct = kv4_most_units(a, FW * FKT) <= KV4_DIRECT && items < (1ll << 30);
+    const int grid = direct ? (int)items : nsm * C::MINB;
+    const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);
     cudaError_t e = cudaFuncSetAttribute(k_kv4_few<D, F32, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
-    const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
-    k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT);
+    k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT, direct);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_kv4_join(a, ws, grid, C::R, s);
+    return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, s);
 }
 
 // Rows of a tile: 8 when a head's rows fit (or float32 has few), else 16.

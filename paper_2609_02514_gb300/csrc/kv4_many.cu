@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         mbar_init(b_end, 1);
         any_timeout = 0;
     }
+    pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     const Kv4Start at = kv4_start<MKT, 1, MT>(a, R, RT);
     if (tid == 0) kv4_put_info<MKT, 1>(a, ws, at, R, RT);

@@ -9,14 +9,19 @@
 // the lengths.  An item inside one CTA's range is written out by it; the pieces
 // of one that several share go to the workspace as sums not yet divided,
 // with their reference maximum, and k_kv4_join adds them in the CTAs' order.
+// Where no item can have more than KV4_DIRECT units (the cache is short, or the
+// window), each is one CTA's, and there is nothing to join.
 #pragma once
 #include "kv4.cuh"
 
 namespace aces {
 
+constexpr int KV4_DIRECT = 8;
+
 struct Kv4Info {  // of the item in which a CTA's range starts
     int b, rt, h, off, units, quantum;
-    int valid, timeout;
+    int cnt;      // the sequence's tokens (0: none in the cache); -1: the CTA has nothing to do
+    int timeout;
 };
 static_assert(sizeof(Kv4Info) == 32, "Kv4Info layout");
 
@@ -126,15 +131,36 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
 template <int KT, int TPU>
 __device__ __forceinline__ void kv4_put_info(const Kv4Att &a, const Kv4Ws &ws, const Kv4Start &at, int R, int RT) {
     Kv4Info in;
-    in.valid = at.left > 0;
+    in.cnt = -1;
     in.timeout = 0;
     in.quantum = at.quantum;
     in.b = in.rt = in.h = in.off = in.units = 0;
-    if (in.valid) {
+    if (at.left > 0) {
         in.b = at.e / RT, in.rt = at.e % RT, in.h = at.h, in.off = at.off;
-        in.units = kv4_keys<KT, TPU>(a, R, in.b, in.rt).units;
+        const Kv4Keys k = kv4_keys<KT, TPU>(a, R, in.b, in.rt);
+        in.units = k.units;
+        in.cnt = kv4_seq(a.prefix, a.count, in.b, a.n, a.S).ok ? k.cnt : 0;
     }
     ws.info[blockIdx.x] = in;
+}
+
+// Without a split: CTA e * H + h has the whole item.
+template <int KT, int TPU>
+__device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT) {
+    Kv4Start s;
+    s.e = blockIdx.x / a.H, s.h = blockIdx.x - s.e * a.H;
+    s.off = 0;
+    const Kv4Keys k = kv4_keys<KT, TPU>(a, R, s.e / RT, s.e % RT);
+    s.left = s.quantum = k.units;
+    if (threadIdx.x == 0 && s.h == 0 && s.e % RT == 0)
+        a.status[s.e / RT] = kv4_seq(a.prefix, a.count, s.e / RT, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
+    return s;
+}
+// the most units an item can have, by the cache's and the window's lengths
+inline int kv4_most_units(const Kv4Att &a, int keys) {
+    long long most = a.S;
+    if (a.window) most = most < (long long)a.window + a.sinks + a.n + 2 * keys ? most : (long long)a.window + a.sinks + a.n + 2 * keys;
+    return (int)((most + keys - 1) / keys);
 }
 
 // A CTA's segments, one after another: units [x0, x1) of an item.

@@ -56,12 +56,12 @@ __device__ __forceinline__ void quantise(const float (&x0)[G], uint32_t (&w)[G /
         if (fabsf(x[i]) > fabsf(a)) a = x[i];  // the first of the largest
     }
     const float t = kv4_t(a), s = t * KV4_STEP;
-    const float inv = s == 0.0f ? 0.0f : __frcp_rn(s);
+    const float inv = s == 0.0f ? 0.0f : __frcp_rn(s), h = s == 0.0f ? INFINITY : 0.5f * fabsf(s);
 #pragma unroll
     for (int i = 0; i < G / 8; ++i) {
         w[i] = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[i] |= kv4_code(x[8 * i + e], s, inv) << (4 * (e >> 1) + 16 * (e & 1));
+        for (int e = 0; e < 8; ++e) w[i] |= kv4_code(x[8 * i + e], s, inv, h) << (4 * (e >> 1) + 16 * (e & 1));
     }
     *t_out = t;
     *bad = nf;
