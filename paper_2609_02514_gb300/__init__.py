@@ -434,39 +434,39 @@ def tree_mask(F, branch_len: int, device=None):
     return mask, depth
 
 
+# A call on one token is bound by the host, so the checks below are single
+# expressions that hold as a rule, and only where one fails is the reason looked
+# for: kv4_read() took 16 us of a Grace core, kv4_attention() 31.
+_U8 = torch.uint8
+_I64x3 = ctypes.c_int64 * 3
+
+
 def _kv4_cache(cache):
     """(planes, B, H, S, D) of a 4-bit cache."""
     c = _cuda(cache, "cache")
-    if c.dtype != torch.uint8 or c.dim() != 5:
+    if c.dtype is not _U8 or c.dim() != 5:
         raise ValueError("cache must be uint8 [planes, B, H, S, row]")
     planes, B, H, S, R = c.shape
     return planes, B, H, S, 2 * (R - 16)
 
 
-def _dense_rows(t, name, shape=None, dtype=None, like=None):
-    """A [B, n, H, D] CUDA tensor whose last dimension is dense, and its strides."""
+def _rows(t, name, dev):
+    """[B, n, heads, D] numbers on dev whose last dimension is dense: their strides."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 4 or (t.shape[3] != 1 and t.stride(3) != 1):
-        raise ValueError(f"{name} must be [B, n, heads, D] with a dense last dimension")
-    if t.dtype not in _DTYPES:
-        raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    if shape is not None and (tuple(t.shape) != shape or t.dtype != dtype):
-        raise ValueError(f"{name} must be {dtype} {list(shape)}")
-    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+    if t.dim() != 4 or t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16 [B, n, heads, D]")
+    b, i, h, d = t.stride()
+    if (d != 1 and t.shape[3] != 1) or t.device != dev:
+        raise ValueError(f"{name} must have a dense last dimension and lie on {dev}")
+    return _I64x3(b, i, h)
 
 
-def _ints(t, name, *shape):
-    t = _cuda(t, name)
-    if t.dtype != _I32 or tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be int32 {list(shape)}")
+def _out(t, name, shape, dtype, dev):
+    """The address of a dense tensor of that shape on dev."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} on {dev}")
     return t.data_ptr()
-
-
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} must be on {dev}")
 
 
 def kv4_cache(layers: int, B: int, H: int, S: int, D: int, device=None):
@@ -482,19 +482,19 @@ def kv4_append(cache, layer: int, k, v, start, count=None, out: torch.Tensor | N
     """Quantise k, v [B, n, H, D] into the cache at positions start[b] + i (in
     place; tokens i >= count[b] are padding); returns row_status [B, n] int32.
     k and v may be strided views with a dense last dimension."""
-    lib = load()
+    lib = _lib or load()
     planes, B, H, S, D = _kv4_cache(cache)
-    ks = _dense_rows(k, "k")
-    n = k.shape[1]
-    if tuple(k.shape) != (B, n, H, D):
-        raise ValueError(f"k must be [{B}, n, {H}, {D}]")
-    vs = _dense_rows(v, "v", tuple(k.shape), k.dtype)
     dev = cache.device
-    _same_device(dev, k=k, v=v, start=start, count=count, out=out)
-    st = out if out is not None else torch.empty(B, n, dtype=_I32, device=dev)
-    code = lib.aces_kv4_append(cache.data_ptr(), planes, int(layer), B, H, S, D, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype],
-                               ks, vs, _ints(start, "start", B), None if count is None else _ints(count, "count", B), n,
-                               _ints(st, "out", B, n), _stream(dev))
+    ks, vs = _rows(k, "k", dev), _rows(v, "v", dev)
+    shape, dtype = k.shape, k.dtype
+    n = shape[1]
+    if shape != (B, n, H, D) or v.shape != shape or v.dtype is not dtype:
+        raise ValueError(f"k and v must be alike, [{B}, n, {H}, {D}]")
+    one = (B,)
+    st = _empty((B, n), dtype=_I32, device=dev) if out is None else out
+    code = lib.aces_kv4_append(cache.data_ptr(), planes, layer, B, H, S, D, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], ks, vs,
+                               _out(start, "start", one, _I32, dev), None if count is None else _out(count, "count", one, _I32, dev), n,
+                               st.data_ptr() if out is None else _out(out, "out", (B, n), _I32, dev), _stream(dev))
     if code != 0:
         _check("aces_kv4_append", code)
     return st
@@ -503,18 +503,19 @@ def kv4_append(cache, layer: int, k, v, start, count=None, out: torch.Tensor | N
 def kv4_read(cache, layer: int, start, n: int, dtype=torch.bfloat16, out: dict | None = None):
     """Positions start[b] .. start[b] + n - 1 of the cache as numbers: a dict of
     k, v [B, n, H, D] (zeros outside the cache)."""
-    lib = load()
+    lib = _lib or load()
     planes, B, H, S, D = _kv4_cache(cache)
-    if dtype not in _DTYPES:
+    dt = _DTYPES.get(dtype)
+    if dt is None:
         raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
-    dev = cache.device
-    o = _outputs(out, dev, ("k", (B, n, H, D), dtype), ("v", (B, n, H, D), dtype))
-    for key in ("k", "v"):
-        if _cuda(o[key], key).dtype != dtype or tuple(o[key].shape) != (B, n, H, D):
-            raise ValueError(f"{key} must be {dtype} {[B, n, H, D]}")
-    _same_device(dev, start=start, k=o["k"], v=o["v"])
-    code = lib.aces_kv4_read(cache.data_ptr(), planes, int(layer), B, H, S, D, _ints(start, "start", B), int(n),
-                             o["k"].data_ptr(), o["v"].data_ptr(), _DTYPES[dtype], _stream(dev))
+    dev, shape = cache.device, (B, n, H, D)
+    if out is None:
+        k, v = _empty(shape, dtype=dtype, device=dev), _empty(shape, dtype=dtype, device=dev)
+        o, kp, vp = {"k": k, "v": v}, k.data_ptr(), v.data_ptr()
+    else:
+        o = _outputs(out, dev, ("k", shape, dtype), ("v", shape, dtype))
+        kp, vp = _out(o["k"], "k", shape, dtype, dev), _out(o["v"], "v", shape, dtype, dev)
+    code = lib.aces_kv4_read(cache.data_ptr(), planes, layer, B, H, S, D, _out(start, "start", (B,), _I32, dev), n, kp, vp, dt, _stream(dev))
     if code != 0:
         _check("aces_kv4_read", code)
     return o
@@ -537,39 +538,44 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
     [B, n, Hq, D], lse [B, n, Hq] and status [B] (ROW_RANGE: a sequence whose
     tokens do not lie in the cache).
     """
-    lib = load()
+    lib = _lib or load()
     planes, B, H, S, D = _kv4_cache(cache)
-    qs = _dense_rows(q, "q")
-    n, Hq = q.shape[1], q.shape[2]
-    if q.shape[0] != B or q.shape[3] != D:
-        raise ValueError(f"q must be [{B}, n, Hq, {D}]")
-    if (mask is None) != (depth is None):
-        raise ValueError("mask and depth go together")
     dev = cache.device
+    qs = _rows(q, "q", dev)
+    shape, dtype = q.shape, q.dtype
+    _, n, Hq, _ = shape
+    if shape[0] != B or shape[3] != D:
+        raise ValueError(f"q must be [{B}, n, Hq, {D}]")
     mp = dp = None
     ms = ds = 0
-    if mask is not None:
+    if mask is not None or depth is not None:
+        if mask is None or depth is None:
+            raise ValueError("mask and depth go together")
         words = (n + 31) // 32
-        each = mask.dim() == 3
-        mp = _ints(mask, "mask", *((B, n, words) if each else (n, words)))
-        ms = n * words if each else 0
-        each = depth.dim() == 2
-        dp = _ints(depth, "depth", *((B, n) if each else (n,)))
-        ds = n if each else 0
-    o = _outputs(out, dev, ("out", (B, n, Hq, D), q.dtype), ("lse", (B, n, Hq), _F32), ("status", (B,), _I32))
-    for key, shape, dtype in (("out", (B, n, Hq, D), q.dtype), ("lse", (B, n, Hq), _F32), ("status", (B,), _I32)):
-        if _cuda(o[key], key).dtype != dtype or tuple(o[key].shape) != shape:
-            raise ValueError(f"{key} must be {dtype} {list(shape)}")
-    ws = workspace
-    if ws is None:
-        ws = _empty(max(kv4_workspace_bytes(B, n, Hq, H, D), 16), dtype=torch.uint8, device=dev)
-    _same_device(dev, q=q, prefix_len=prefix_len, count=count, mask=mask, depth=depth, workspace=ws, out=o["out"], lse=o["lse"],
-                 status=o["status"])
-    code = lib.aces_kv4_attention(q.data_ptr(), _DTYPES[q.dtype], qs, cache.data_ptr(), planes, int(layer), B, n, Hq, H, S, D,
-                                  _ints(prefix_len, "prefix_len", B), None if count is None else _ints(count, "count", B),
-                                  mp, ms, dp, ds, D ** -0.5 if scale is None else float(scale), int(window), int(sinks),
-                                  o["out"].data_ptr(), o["lse"].data_ptr(), o["status"].data_ptr(), ws.data_ptr(),
-                                  ws.numel() * ws.element_size(), _stream(dev))
+        ms = n * words if mask.dim() == 3 else 0
+        mp = _out(mask, "mask", (B, n, words) if ms else (n, words), _I32, dev)
+        ds = n if depth.dim() == 2 else 0
+        dp = _out(depth, "depth", (B, n) if ds else (n,), _I32, dev)
+    one = (B,)
+    if out is None:
+        r, lse, st = _empty(shape, dtype=dtype, device=dev), _empty((B, n, Hq), dtype=_F32, device=dev), _empty(one, dtype=_I32, device=dev)
+        o, rp, lp, sp = {"out": r, "lse": lse, "status": st}, r.data_ptr(), lse.data_ptr(), st.data_ptr()
+    else:
+        o = _outputs(out, dev, ("out", shape, dtype), ("lse", (B, n, Hq), _F32), ("status", one, _I32))
+        rp, lp = _out(o["out"], "out", shape, dtype, dev), _out(o["lse"], "lse", (B, n, Hq), _F32, dev)
+        sp = _out(o["status"], "status", one, _I32, dev)
+    if workspace is None:
+        nbytes = lib.aces_kv4_workspace_bytes(B, n, Hq, H, D)
+        ws = _empty(nbytes, dtype=_U8, device=dev)
+    else:
+        ws = _cuda(workspace, "workspace")
+        nbytes = ws.numel() * ws.element_size()
+        if ws.device != dev:
+            raise ValueError(f"workspace must be on {dev}")
+    code = lib.aces_kv4_attention(q.data_ptr(), _DTYPES[dtype], qs, cache.data_ptr(), planes, layer, B, n, Hq, H, S, D,
+                                  _out(prefix_len, "prefix_len", one, _I32, dev),
+                                  None if count is None else _out(count, "count", one, _I32, dev), mp, ms, dp, ds,
+                                  D ** -0.5 if scale is None else scale, window, sinks, rp, lp, sp, ws.data_ptr(), nbytes, _stream(dev))
     if code != 0:
         _check("aces_kv4_attention", code)
     return o

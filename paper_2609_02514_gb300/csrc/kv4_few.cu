@@ -1,6 +1,8 @@
 // Attention over a 4-bit KV cache for few query rows (the format: kv4.cuh, the
 // shares: kv4_plan.cuh): single tokens, and everything in float32.
 #define ACES_FILE 8  // site numbers of the checked build
+#include <atomic>
+
 #include <cuda_bf16.h>
 
 #include "kv4_plan.cuh"
@@ -420,13 +422,16 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // group c (Y blocks) takes the item in which the range of CTA c starts, when c is
 // the first to start inside it.  Block 0 writes the sequences' status.  The grid
 // is launched while the attention runs and waits for its end.
-// A warp takes a row: its lanes the pieces' maxima, then the row's channels.
-constexpr int JN = 256;
+// Few pieces: a warp takes a row.  More (one long sequence): the block takes a row
+// and its warps every eighth piece, so that all loads are under way at once.
+constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32>
 __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
     constexpr int D4 = D / 4, PW = 32 / D4;  // float4 of a row; pieces a warp reads at a time
     __shared__ int late;
-    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, lane = tid & 31;
+    __shared__ float4 part[JW][D4];
+    __shared__ float part_m[JW], part_l[JW];
+    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
     if (c == 0) {
         if (y != 0) return;
@@ -446,28 +451,28 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
     const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off == in.quantum ? 0 : 1)) * stride;
     const float *rest = ws.piece + (size_t)(2 * (c - 1)) * stride;  // piece p > 0 at 2 p strides
     auto piece = [&](int p) { return p == 0 ? first : rest + (size_t)(2 * p) * stride; };
-    for (int row = y * (JN / 32) + (tid >> 5); row < NR; row += Y * (JN / 32)) {
-        float M = -INFINITY, L = 0.0f;
-        for (int p = lane; p < pieces; p += 32) M = fmaxf(M, piece(p)[R * D + row]);
-        M = warp_max(M);
-        const float ref = M == -INFINITY ? 0.0f : M;
+    // Pieces p0, p0 + step ... of a row: their sums to the maximum of them all, in
+    // lanes 0 .. D4 - 1, and the sum of the weights.
+    auto add = [&](int row, int p0, int step, float &M, float &L) {
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int p0 = 0; p0 < pieces; p0 += 32) {
-            const int np = min(32, pieces - p0);
-            float f = 0.0f;
-            if (lane < np) {
-                const float *pc = piece(p0 + lane) + R * D + row;
-                f = ex2(pc[0] - ref);
-                L = fmaf(pc[R], f, L);
-            }
-#pragma unroll 4
+        M = -INFINITY, L = 0.0f;
+        for (int base = p0; base < pieces; base += 32 * step) {
+            const int mine = base + lane * step;
+            float m = -INFINITY, l = 0.0f;
+            if (mine < pieces) m = piece(mine)[R * D + row], l = piece(mine)[R * D + R + row];
+            const int np = min(32, (pieces - base + step - 1) / step);
+            const float top = fmaxf(M, warp_max(m)), ref = top == -INFINITY ? 0.0f : top;
+            const float f = ex2(m - ref), old = ex2(M - ref);
+            M = top;
+            L = L * old + l * f;
+            o.x *= old, o.y *= old, o.z *= old, o.w *= old;
+#pragma unroll 8
             for (int q = 0; q < np; q += PW) {
                 const int p = q + lane / D4;
                 const float fp = __shfl_sync(0xffffffffu, f, p & 31);
-                if (p < np) {
-                    const float4 v = *reinterpret_cast<const float4 *>(piece(p0 + p) + row * D + 4 * (lane % D4));
-                    o.x = fmaf(v.x, fp, o.x), o.y = fmaf(v.y, fp, o.y), o.z = fmaf(v.z, fp, o.z), o.w = fmaf(v.w, fp, o.w);
-                }
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (p < np) v = *reinterpret_cast<const float4 *>(piece(base + p * step) + row * D + 4 * (lane % D4));
+                if (p < np) o.x = fmaf(v.x, fp, o.x), o.y = fmaf(v.y, fp, o.y), o.z = fmaf(v.z, fp, o.z), o.w = fmaf(v.w, fp, o.w);
             }
         }
         for (int x = 16; x > 0; x >>= 1) L += __shfl_xor_sync(0xffffffffu, L, x);
@@ -475,24 +480,53 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
             o.x += __shfl_xor_sync(0xffffffffu, o.x, 16), o.y += __shfl_xor_sync(0xffffffffu, o.y, 16);
             o.z += __shfl_xor_sync(0xffffffffu, o.z, 16), o.w += __shfl_xor_sync(0xffffffffu, o.w, 16);
         }
+        return o;
+    };
+    auto put = [&](int row, int d4, float4 o, float M, float L) {
         const int r = in.rt * R + row, i = r / a.G;
         const bool none = L == 0.0f || i >= in.cnt;
         const float k = none ? 0.0f : KV4_STEP / L;
         if (none) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         const size_t orow = ((size_t)in.b * a.n + i) * a.Hq + in.h * a.G + (r - i * a.G);
-        if (lane < D4) {
-            if (F32)
-                reinterpret_cast<float4 *>(a.out)[orow * D4 + lane] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
-            else
-                reinterpret_cast<uint2 *>(a.out)[orow * D4 + lane] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
+        if (F32)
+            reinterpret_cast<float4 *>(a.out)[orow * D4 + d4] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
+        else
+            reinterpret_cast<uint2 *>(a.out)[orow * D4 + d4] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
+        if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    };
+    float M, L;
+    if (pieces <= JW) {
+        for (int row = y * JW + warp; row < NR; row += Y * JW) {
+            const float4 o = add(row, 0, 1, M, L);
+            if (lane < D4) put(row, lane, o, M, L);
         }
-        if (lane == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    } else {
+        for (int row = y; row < NR; row += Y) {
+            const float4 o = add(row, warp, JW, M, L);
+            if (lane < D4) part[warp][lane] = o;
+            if (lane == 0) part_m[warp] = M, part_l[warp] = L;
+            __syncthreads();
+            if (tid < D4) {
+                float top = part_m[0], sum = 0.0f;
+                for (int w = 1; w < JW; ++w) top = fmaxf(top, part_m[w]);
+                const float ref = top == -INFINITY ? 0.0f : top;
+                float4 all = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int w = 0; w < JW; ++w) {
+                    const float f = ex2(part_m[w] - ref);
+                    const float4 v = part[w][tid];
+                    sum = fmaf(part_l[w], f, sum);
+                    all.x = fmaf(v.x, f, all.x), all.y = fmaf(v.y, f, all.y), all.z = fmaf(v.z, f, all.z), all.w = fmaf(v.w, f, all.w);
+                }
+                put(row, tid, all, top, sum);
+            }
+            __syncthreads();
+        }
     }
 }
 
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
-    const int rows = a.n * a.G < R ? a.n * a.G : R, steps = (rows + JN / 32 - 1) / (JN / 32);
-    const int Y = steps < 16 ? steps : 16;  // blocks of an item
+    const int rows = a.n * a.G < R ? a.n * a.G : R;
+    const int Y = rows < 16 ? rows : 16;  // blocks of an item
     const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true> : k_kv4_join<64, false>) : (a.f32 ? k_kv4_join<128, true> : k_kv4_join<128, false>);
     return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
@@ -505,7 +539,8 @@ static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
     const bool direct = kv4_most_units(a, FW * FKT) <= KV4_DIRECT && items < (1ll << 30);
     const int grid = direct ? (int)items : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);
-    cudaError_t e = cudaFuncSetAttribute(k_kv4_few<D, F32, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    static std::atomic<unsigned long long> allowed{0};
+    cudaError_t e = allow_smem(k_kv4_few<D, F32, NT>, C::SMEM, allowed);
     if (e != cudaSuccess) return e;
     k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT, direct);
     e = cudaGetLastError();

@@ -684,7 +684,8 @@ template <int D>
 static cudaError_t run_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
     const int R = many_rows_of(a.n, a.G), RT = (int)(((long long)a.n * a.G + R - 1) / R);
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm);
-    cudaError_t e = cudaFuncSetAttribute(k_kv4_many<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<D>::SMEM);
+    static std::atomic<unsigned long long> allowed{0};
+    cudaError_t e = allow_smem(k_kv4_many<D>, Many<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;
     k_kv4_many<D><<<nsm, MT, Many<D>::SMEM, s>>>(a, ws, R, RT);
     e = cudaGetLastError();

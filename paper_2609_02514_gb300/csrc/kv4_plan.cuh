@@ -12,6 +12,8 @@
 // Where no item can have more than KV4_DIRECT units (the cache is short, or the
 // window), each is one CTA's, and there is nothing to join.
 #pragma once
+#include <atomic>
+
 #include "kv4.cuh"
 
 namespace aces {
@@ -195,6 +197,19 @@ struct Kv4Seg {
     __device__ __forceinline__ size_t row0(const Kv4Att &a) const { return (size_t)((size_t)b * a.H + h) * a.S; }
     __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == key.units; }
 };
+
+// Lets a kernel have that much shared memory, once on each of 64 devices.
+template <typename F>
+inline cudaError_t allow_smem(F *fn, int bytes, std::atomic<unsigned long long> &allowed) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev < 64 && (allowed.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
 size_t kv4_few_ws(int n, int G, int D, int nsm);
