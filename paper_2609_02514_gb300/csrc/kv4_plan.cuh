@@ -270,14 +270,21 @@ __device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) 
 }
 // -24 t of two t's (exact: two and five significant bits)
 __device__ __forceinline__ uint32_t kv4_offset(uint32_t t2) { return bf2_fma(t2, 0xC1C0C1C0u, 0x80008000u); }
+// a & 0x00780078 | 0x41804180 as one instruction (written in C it becomes two: an
+// instruction has room for one of the constants)
+__device__ __forceinline__ uint32_t kv4_sixteen(uint32_t a) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(0x00780078u), "r"(0x41804180u));
+    return d;
+}
 // Four pairs of values from a word whose halves hold four codes each, pair j
 // the codes at bits 4 j: a code at bits 3..6 of 16.0 makes 16 + c, and (16 + c)
 // t - 24 t = (c - 8) t is exact.
 __device__ __forceinline__ void kv4_pairs(uint32_t w, uint32_t t2, uint32_t off, uint32_t (&p)[4]) {
-    p[0] = bf2_fma(((w << 3) & 0x00780078u) | 0x41804180u, t2, off);
-    p[1] = bf2_fma(((w >> 1) & 0x00780078u) | 0x41804180u, t2, off);
-    p[2] = bf2_fma(((w >> 5) & 0x00780078u) | 0x41804180u, t2, off);
-    p[3] = bf2_fma(((w >> 9) & 0x00780078u) | 0x41804180u, t2, off);
+    p[0] = bf2_fma(kv4_sixteen(w << 3), t2, off);
+    p[1] = bf2_fma(kv4_sixteen(w >> 1), t2, off);
+    p[2] = bf2_fma(kv4_sixteen(w >> 5), t2, off);
+    p[3] = bf2_fma(kv4_sixteen(w >> 9), t2, off);
 }
 // bfloat16 pair with infinities made NaN, so a query that is not finite spoils
 // its row whatever the keys' signs
