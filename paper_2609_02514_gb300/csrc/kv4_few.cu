@@ -12,6 +12,7 @@ namespace aces {
 constexpr int FW = 8;            // warps
 constexpr int FT = FW * 32;
 constexpr int FKT = 32;          // keys of a tile: one warp's step
+constexpr int FFIX = 1;          // units an item costs beside its keys
 constexpr float F_LAZY = 8.0f;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -56,7 +57,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) unsigned long long bars[FW * ST];
     __shared__ float sm_m[FW][R], sm_l[FW][R];
-    __shared__ int2 rowinfo[R];                 // token and position of a row
+    __shared__ int2 rowinfo[2][R];              // token and position of a row, of this segment and the next
     __shared__ int any_timeout;
     float *merge = reinterpret_cast<float *>(smem + C::RING);
     uint2 *qs = reinterpret_cast<uint2 *>(smem + C::RING + C::MERGE);
@@ -70,9 +71,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (!direct) pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
-    using Seg = Kv4Seg<FKT, FW>;
-    const Kv4Start at = direct ? kv4_whole<FKT, FW>(a, R, RT) : kv4_start<FKT, FW, FT>(a, R, RT);
-    if (tid == 0 && !direct) kv4_put_info<FKT, FW>(a, ws, at, R, RT);
+    using Seg = Kv4Seg<FKT, FW, FFIX>;
+    const Kv4Start at = direct ? kv4_whole<FKT, FW, FFIX>(a, R, RT) : kv4_start<FKT, FW, FFIX, FT>(a, R, RT);
+    if (tid == 0 && !direct) kv4_put_info<FFIX>(ws, at);
     __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
     if (!cur.start(a, R, RT, at)) return;
@@ -101,69 +102,80 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     int mine = my_tiles(cur);
     for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
 
+    // Eight channels of a query row, part sp of three (float32: 24 bits in parts of
+    // eight).  A row that is none reads the first one's and becomes zeros, so the
+    // loads need no branch and are all under way at once.
+    const bool q_vec = !F32 && (((uintptr_t)a.q | (uintptr_t)(2 * a.qb) | (uintptr_t)(2 * a.qi) | (uintptr_t)(2 * a.qh)) & 15) == 0;
+    auto q_words = [&](const Seg &sg, int row, int word, int sp, uint32_t (&o)[4]) {
+        const int r = sg.rt * R + row, ri = r / a.G;
+        const bool ok = r < a.n * a.G && sg.key.live && ri < sg.key.cnt;
+        const int i = ok ? ri : 0, gq = ok ? r - ri * a.G : 0;
+        const long long p = sg.b * a.qb + i * a.qi + (long long)(sg.h * a.G + gq) * a.qh + 8 * word;
+        if (F32) {
+            const float *f = reinterpret_cast<const float *>(a.q) + p;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __ldg(f + j);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v0 = v[2 * j], v1 = v[2 * j + 1];
+                uint32_t w = bf2_pack(v0, v1);
+                for (int x = 0; x < sp; ++x) {
+                    v0 -= bf_lo(w), v1 -= bf_hi(w);
+                    w = bf2_pack(v0, v1);
+                }
+                o[j] = w;
+            }
+        } else {
+            const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + p;
+            if (q_vec) {
+                const uint4 w = ldg16(f);
+                o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = (uint32_t)__ldg(f + 2 * j) | (uint32_t)__ldg(f + 2 * j + 1) << 16;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = ok ? bf2_poison(o[j]) : 0u;
+    };
+    uint32_t q[C::QREG ? 2 * KS : 1];
+    auto q_regs = [&](const Seg &sg) {
+        if (!C::QREG) return;
+        uint32_t o[WPT][4];
+#pragma unroll
+        for (int w = 0; w < WPT; ++w) q_words(sg, g, WPT * t + w, 0, o[w]);
+#pragma unroll
+        for (int x = 0; x < 4 * WPT; ++x) q[C::QREG ? x : 0] = o[x >> 2][x & 3];
+    };
+    auto q_info = [&](const Seg &sg, int to) {  // token and position of the rows
+        if (tid >= R) return;
+        const int r = sg.rt * R + tid, i = r / a.G;
+        const bool ok = r < a.n * a.G && sg.key.live && i < sg.key.cnt;
+        rowinfo[to][tid] = ok ? make_int2(i, kv4_pos(sg.key.P, a.mask ? a.depth + sg.b * a.depth_b : nullptr, i)) : make_int2(-1, 0);
+    };
+    q_regs(cur);
+    q_info(cur, 0);
+    __syncthreads();
+    int info = 0;  // which of the two is this segment's
     bool first = true;
     while (true) {
         const Kv4Keys key = cur.key;
         const int b = cur.b, rt = cur.rt, h = cur.h, P = key.P, end = P + key.cnt;
-        // the segment's query rows
-        if (tid < R) {
-            const int r = rt * R + tid, i = r / a.G;
-            const bool ok = r < a.n * a.G && key.live && i < key.cnt;
-            rowinfo[tid] = ok ? make_int2(i, kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i)) : make_int2(-1, 0);
-        }
-        uint32_t q[C::QREG ? 2 * KS : 1];
-        auto q_words = [&](int row, int word, int sp, uint32_t (&o)[4]) {  // eight channels of a query row
-            const int r = rt * R + row;
-            o[0] = o[1] = o[2] = o[3] = 0u;
-            const int i = r / a.G;
-            if (!(r < a.n * a.G && key.live && i < key.cnt)) return;
-            const long long p = b * a.qb + i * a.qi + (long long)(h * a.G + r % a.G) * a.qh + 8 * word;
-            if (F32) {
-                const float *f = reinterpret_cast<const float *>(a.q) + p;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float v0 = __ldg(f + 2 * j), v1 = __ldg(f + 2 * j + 1);
-                    uint32_t w = bf2_pack(v0, v1);
-                    for (int s = 0; s < sp; ++s) {
-                        v0 -= bf_lo(w), v1 -= bf_hi(w);
-                        w = bf2_pack(v0, v1);
-                    }
-                    o[j] = bf2_poison(w);
-                }
-            } else {
-                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + p;
-                if (((uintptr_t)f & 15) == 0) {
-                    const uint4 w = ldg16(f);
-                    o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = (uint32_t)__ldg(f + 2 * j) | (uint32_t)__ldg(f + 2 * j + 1) << 16;
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = bf2_poison(o[j]);
-            }
-        };
-        if (C::QREG) {
-#pragma unroll
-            for (int w = 0; w < WPT; ++w) {
-                uint32_t o[4];
-                q_words(g, WPT * t + w, 0, o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) q[C::QREG ? 4 * w + j : 0] = o[j];
-            }
-        } else {
+        const int2 *rows = rowinfo[info];
+        if (!C::QREG) {
             for (int x = tid; x < NT * SPL * (KS / 2) * 32; x += FT) {  // one word: two steps of a lane
                 const int l = x & 31, w = (x >> 5) % WPT, sp = (x >> 5) / WPT % SPL, nt = (x >> 5) / WPT / SPL;
                 uint32_t o[4];
-                q_words(nt * 8 + (l >> 2), WPT * (l & 3) + w, sp, o);
+                q_words(cur, nt * 8 + (l >> 2), WPT * (l & 3) + w, sp, o);
                 qs[((nt * SPL + sp) * KS + 2 * w) * 32 + l] = make_uint2(o[0], o[1]);
                 qs[((nt * SPL + sp) * KS + 2 * w + 1) * 32 + l] = make_uint2(o[2], o[3]);
             }
         }
-        __syncthreads();
+        if (!C::QREG) __syncthreads();
         int posmax = 0;
         if (a.window)
-            for (int r = 0; r < R; ++r) posmax = max(posmax, rowinfo[r].y);
+            for (int r = 0; r < R; ++r) posmax = max(posmax, rows[r].y);
         const int all_see = P + (a.mask ? 0 : key.i0 + 1);  // positions below it are new to no row
 
         float O[NT][JT][4], m[NT][2], l[NT][2];
@@ -231,7 +243,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int2 ri = rowinfo[nt * 8 + 2 * t + c];
+                        const int2 ri = rows[nt * 8 + 2 * t + c];
 #pragma unroll
                         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -340,6 +352,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         mine = more ? my_tiles(cur) : 0;
         if (more) place_rows(cur);
         for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
+        if (more) {
+            q_regs(cur);
+            q_info(cur, info ^ 1);
+        }
         // merge the warps
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -383,7 +399,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                     if (!whole) {
                         slot[row * D + d] = o;
                     } else if (r < a.n * a.G) {
-                        const float v = L[c] == 0.0f || rowinfo[row].x < 0 ? 0.0f : o * KV4_STEP / L[c];
+                        const float v = L[c] == 0.0f || rows[row].x < 0 ? 0.0f : o * KV4_STEP / L[c];
                         const size_t at_o = (((size_t)b * a.n + i) * a.Hq + h * a.G + r % a.G) * D + d;
                         if (F32)
                             reinterpret_cast<float *>(a.out)[at_o] = v;
@@ -401,18 +417,19 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                         slot[R * D + R + row] = L[c];
                     } else if (a.lse && r < a.n * a.G) {
                         a.lse[((size_t)b * a.n + i) * a.Hq + h * a.G + r % a.G] =
-                            L[c] == 0.0f || rowinfo[row].x < 0 ? -INFINITY : (M[c] + log2f(L[c])) * 0.6931471805599453f;
+                            L[c] == 0.0f || rows[row].x < 0 ? -INFINITY : (M[c] + log2f(L[c])) * 0.6931471805599453f;
                     }
                 }
             }
             __syncthreads();  // before the next rows' sums, the next segment's row infos and its maxima
         }
         first = false;
+        info ^= 1;
         if (!more) break;
     }
     if (tid == 0 && any_timeout) {
         if (direct)
-            atomicOr(a.status + at.e / RT, ACES_ROW_TIMEOUT);  // seconds after it was written
+            atomicOr(a.status + at.b, ACES_ROW_TIMEOUT);  // seconds after it was written
         else
             ws.info[blockIdx.x].timeout = 1;
     }
@@ -426,7 +443,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // and its warps every eighth piece, so that all loads are under way at once.
 constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32>
-__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
+__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y, int fix) {
     constexpr int D4 = D / 4, PW = 32 / D4;  // float4 of a row; pieces a warp reads at a time
     __shared__ int late;
     __shared__ float4 part[JW][D4];
@@ -445,10 +462,11 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
         return;
     }
     const Kv4Info in = ws.info[c];
-    if (in.cnt < 0 || in.off == 0 || in.off > in.quantum) return;
+    // inside the item, beyond its FIX units, and the first to start there
+    if (in.cnt < 0 || in.off <= fix || in.off - in.quantum > fix) return;
     const int pieces = 1 + (in.units - in.off + in.quantum - 1) / in.quantum;
     const int stride = R * (D + 2), NR = min(R, a.n * a.G - in.rt * R);
-    const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off == in.quantum ? 0 : 1)) * stride;
+    const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off >= in.quantum ? 0 : 1)) * stride;
     const float *rest = ws.piece + (size_t)(2 * (c - 1)) * stride;  // piece p > 0 at 2 p strides
     auto piece = [&](int p) { return p == 0 ? first : rest + (size_t)(2 * p) * stride; };
     // Pieces p0, p0 + step ... of a row: their sums to the maximum of them all, in
@@ -524,11 +542,11 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
     }
 }
 
-cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, int fix, cudaStream_t s) {
     const int rows = a.n * a.G < R ? a.n * a.G : R;
     const int Y = rows < 16 ? rows : 16;  // blocks of an item
     const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true> : k_kv4_join<64, false>) : (a.f32 ? k_kv4_join<128, true> : k_kv4_join<128, false>);
-    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
+    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y, fix);
 }
 
 template <int D, bool F32, int NT>
@@ -544,7 +562,7 @@ static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
     if (e != cudaSuccess) return e;
     k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT, direct);
     e = cudaGetLastError();
-    return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, s);
+    return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, FFIX, s);
 }
 
 // Rows of a tile: 8 when a head's rows fit (or float32 has few), else 16.

@@ -6,9 +6,12 @@
 // counts the units of all items itself (one thread an entry (b, row tile), all
 // of whose heads have the same) and takes the units [c Q, (c + 1) Q), Q the
 // whole number that spreads them over the grid: CTAs are equally long whatever
-// the lengths.  An item inside one CTA's range is written out by it; the pieces
-// of one that several share go to the workspace as sums not yet divided,
-// with their reference maximum, and k_kv4_join adds them in the CTAs' order.
+// the lengths.  What an item costs beside its keys (its queries, its merge, its
+// way out) counts as FIX units before its first: without, a CTA that got the
+// short sequences of a ragged batch took twice the others' time.  An item inside
+// one CTA's range is written out by it; the pieces of one that several share go
+// to the workspace as sums not yet divided, with their reference maximum, and
+// k_kv4_join adds them in the CTAs' order.
 // Where no item can have more than KV4_DIRECT units (the cache is short, or the
 // window), each is one CTA's, and there is nothing to join.
 #pragma once
@@ -20,7 +23,7 @@ namespace aces {
 
 constexpr int KV4_DIRECT = 8;
 
-struct Kv4Info {  // of the item in which a CTA's range starts
+struct Kv4Info {  // of the item in which a CTA's range starts (off and units with the FIX)
     int b, rt, h, off, units, quantum;
     int cnt;      // the sequence's tokens (0: none in the cache); -1: the CTA has nothing to do
     int timeout;
@@ -93,69 +96,60 @@ __device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end,
     return !a.window || kp > pos - a.window || kp < a.sinks;
 }
 
-// A CTA's range and the item it starts in, by all NTH threads.
+// A CTA's range and the item it starts in, by all NTH threads.  off and left
+// count the FIX units.
 struct Kv4Start {
-    unsigned long long left;  // units to do
-    int quantum, e, h, off;
+    unsigned long long left;
+    int quantum, b, rt, h, off, cnt;
+    Kv4Keys key;
 };
-template <int KT, int TPU, int NTH>
+template <int KT, int TPU, int FIX, int NTH>
 __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     __shared__ unsigned long long red[NTH / 32];
-    __shared__ int found[3];
+    __shared__ Kv4Start found;
     const int E = a.B * RT, per = (E + NTH - 1) / NTH;
     const int e0 = min(E, (int)threadIdx.x * per), e1 = min(E, e0 + per);
     unsigned long long sum = 0, total;
-    for (int e = e0; e < e1; ++e) sum += (unsigned long long)kv4_keys<KT, TPU>(a, R, e / RT, e % RT).units * a.H;
+    Kv4Keys k;
+    for (int e = e0; e < e1; ++e) {
+        k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+        sum += (unsigned long long)(k.units + FIX) * a.H;
+    }
     unsigned long long at = block_exscan_n<NTH>(sum, red, &total);
     const unsigned long long Q = (total + gridDim.x - 1) / gridDim.x, w0 = Q * blockIdx.x;
     if (w0 >= at && w0 < at + sum) {
         for (int e = e0; e < e1; ++e) {
-            const unsigned u = (unsigned)kv4_keys<KT, TPU>(a, R, e / RT, e % RT).units;
+            if (per > 1) k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+            const unsigned u = k.units + FIX;
             if (w0 < at + (unsigned long long)u * a.H) {
                 const unsigned x = (unsigned)(w0 - at);
-                found[0] = e;
-                found[1] = (int)(x / u);
-                found[2] = (int)(x % u);
+                found.b = e / RT, found.rt = e % RT, found.h = (int)(x / u), found.off = (int)(x % u);
+                found.cnt = kv4_seq(a.prefix, a.count, found.b, a.n, a.S).ok ? k.cnt : 0;
+                found.key = k;
                 break;
             }
             at += (unsigned long long)u * a.H;
         }
     }
     __syncthreads();
-    Kv4Start s;
+    Kv4Start s = found;
     s.left = w0 < total ? min(Q, total - w0) : 0;
     s.quantum = (int)Q;
-    s.e = found[0], s.h = found[1], s.off = found[2];
     return s;
 }
 
-// writes the info of the CTA's start (one thread)
-template <int KT, int TPU>
-__device__ __forceinline__ void kv4_put_info(const Kv4Att &a, const Kv4Ws &ws, const Kv4Start &at, int R, int RT) {
-    Kv4Info in;
-    in.cnt = -1;
-    in.timeout = 0;
-    in.quantum = at.quantum;
-    in.b = in.rt = in.h = in.off = in.units = 0;
-    if (at.left > 0) {
-        in.b = at.e / RT, in.rt = at.e % RT, in.h = at.h, in.off = at.off;
-        const Kv4Keys k = kv4_keys<KT, TPU>(a, R, in.b, in.rt);
-        in.units = k.units;
-        in.cnt = kv4_seq(a.prefix, a.count, in.b, a.n, a.S).ok ? k.cnt : 0;
-    }
-    ws.info[blockIdx.x] = in;
-}
-
-// Without a split: CTA e * H + h has the whole item.
-template <int KT, int TPU>
+// Without a split: a CTA has the whole item.
+template <int KT, int TPU, int FIX>
 __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT) {
     Kv4Start s;
-    s.e = blockIdx.x / a.H, s.h = blockIdx.x - s.e * a.H;
+    const int e = blockIdx.x / a.H;
+    s.h = blockIdx.x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
     s.off = 0;
-    const Kv4Keys k = kv4_keys<KT, TPU>(a, R, s.e / RT, s.e % RT);
-    s.left = s.quantum = k.units;
-    if (threadIdx.x == 0 && s.h == 0 && s.e % RT == 0)
-        a.status[s.e / RT] = kv4_seq(a.prefix, a.count, s.e / RT, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
+    s.key = kv4_keys<KT, TPU>(a, R, s.b, s.rt);
+    s.left = s.quantum = s.key.units + FIX;
+    s.cnt = s.key.cnt;
+    if (threadIdx.x == 0 && s.h == 0 && s.rt == 0)
+        a.status[s.b] = kv4_seq(a.prefix, a.count, s.b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
     return s;
 }
 // the most units an item can have, by the cache's and the window's lengths
@@ -165,18 +159,27 @@ inline int kv4_most_units(const Kv4Att &a, int keys) {
     return (int)((most + keys - 1) / keys);
 }
 
+// writes the info of the CTA's start (one thread)
+template <int FIX>
+__device__ __forceinline__ void kv4_put_info(const Kv4Ws &ws, const Kv4Start &at) {
+    Kv4Info in;
+    const bool some = at.left > 0;
+    in.b = at.b, in.rt = at.rt, in.h = at.h, in.off = at.off, in.units = at.key.units + FIX, in.quantum = at.quantum;
+    in.cnt = some ? at.cnt : -1;
+    in.timeout = 0;
+    ws.info[blockIdx.x] = in;
+}
+
 // A CTA's segments, one after another: units [x0, x1) of an item.
-template <int KT, int TPU>
+template <int KT, int TPU, int FIX>
 struct Kv4Seg {
     unsigned long long left;  // units after this segment
     int b, rt, h, x0, x1;
     Kv4Keys key;
     __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
-        b = at.e / RT, rt = at.e - b * RT, h = at.h, x0 = at.off, left = at.left;
-        if (left == 0) return false;
-        key = kv4_keys<KT, TPU>(a, R, b, rt);
-        take();
-        return true;
+        if (at.left == 0) return false;
+        b = at.b, rt = at.rt, h = at.h, left = at.left, key = at.key;
+        return take(at.off);
     }
     __device__ __forceinline__ bool next(const Kv4Att &a, int R, int RT) {
         if (left == 0) return false;
@@ -185,13 +188,15 @@ struct Kv4Seg {
             if (++rt == RT) rt = 0, ++b;
             key = kv4_keys<KT, TPU>(a, R, b, rt);
         }
-        x0 = 0;
-        take();
-        return true;
+        return take(0);
     }
-    __device__ __forceinline__ void take() {
-        x1 = (int)min((unsigned long long)key.units, x0 + left);
-        left -= x1 - x0;
+    // from unit `off` of the item on; false when the range ends among its FIX units
+    // (one that starts among them has the item's first unit, or ends there too)
+    __device__ __forceinline__ bool take(int off) {
+        const int to = (int)min((unsigned long long)(key.units + FIX), off + left);
+        left -= to - off;
+        x0 = max(off - FIX, 0), x1 = max(to - FIX, 0);
+        return x1 > x0;
     }
     // first row of the item's key head in a plane
     __device__ __forceinline__ size_t row0(const Kv4Att &a) const { return (size_t)((size_t)b * a.H + h) * a.S; }
@@ -211,7 +216,7 @@ inline cudaError_t allow_smem(F *fn, int bytes, std::atomic<unsigned long long> 
     return e;
 }
 
-cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, int fix, cudaStream_t s);
 size_t kv4_few_ws(int n, int G, int D, int nsm);
 cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
 size_t kv4_many_ws(int n, int G, int D, int nsm);
