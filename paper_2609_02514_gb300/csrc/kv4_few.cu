@@ -12,7 +12,7 @@ namespace aces {
 constexpr int FW = 8;            // warps
 constexpr int FT = FW * 32;
 constexpr int FKT = 32;          // keys of a tile: one warp's step
-constexpr int FFIX = 1;          // units an item costs beside its keys
+constexpr int FFIX = 3;          // units an item costs beside its keys
 constexpr float F_LAZY = 8.0f;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -99,18 +99,30 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         const int top = min(g.x1 * FW, g.key.tiles) - g.x0 * FW - warp;
         return top > 0 ? (top + FW - 1) / FW : 0;
     };
-    int mine = my_tiles(cur);
-    for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
-
     // Eight channels of a query row, part sp of three (float32: 24 bits in parts of
     // eight).  A row that is none reads the first one's and becomes zeros, so the
     // loads need no branch and are all under way at once.
     const bool q_vec = !F32 && (((uintptr_t)a.q | (uintptr_t)(2 * a.qb) | (uintptr_t)(2 * a.qi) | (uintptr_t)(2 * a.qh)) & 15) == 0;
-    auto q_words = [&](const Seg &sg, int row, int word, int sp, uint32_t (&o)[4]) {
+    auto q_at = [&](const Seg &sg, int row, int word, bool &ok) {
         const int r = sg.rt * R + row, ri = r / a.G;
-        const bool ok = r < a.n * a.G && sg.key.live && ri < sg.key.cnt;
+        ok = r < a.n * a.G && sg.key.live && ri < sg.key.cnt;
         const int i = ok ? ri : 0, gq = ok ? r - ri * a.G : 0;
-        const long long p = sg.b * a.qb + i * a.qi + (long long)(sg.h * a.G + gq) * a.qh + 8 * word;
+        return sg.b * a.qb + i * a.qi + (long long)(sg.h * a.G + gq) * a.qh + 8 * word;
+    };
+    auto q_load = [&](const Seg &sg, int row, int word, uint32_t (&o)[4]) {  // bfloat16, as they are
+        bool ok;
+        const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + q_at(sg, row, word, ok);
+        if (q_vec) {
+            const uint4 w = ldg16(f);
+            o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = (uint32_t)__ldg(f + 2 * j) | (uint32_t)__ldg(f + 2 * j + 1) << 16;
+        }
+    };
+    auto q_words = [&](const Seg &sg, int row, int word, int sp, uint32_t (&o)[4]) {
+        bool ok;
+        const long long p = q_at(sg, row, word, ok);
         if (F32) {
             const float *f = reinterpret_cast<const float *>(a.q) + p;
             float v[8];
@@ -127,26 +139,25 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 o[j] = w;
             }
         } else {
-            const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + p;
-            if (q_vec) {
-                const uint4 w = ldg16(f);
-                o[0] = w.x, o[1] = w.y, o[2] = w.z, o[3] = w.w;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = (uint32_t)__ldg(f + 2 * j) | (uint32_t)__ldg(f + 2 * j + 1) << 16;
-            }
+            q_load(sg, row, word, o);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = ok ? bf2_poison(o[j]) : 0u;
     };
     uint32_t q[C::QREG ? 2 * KS : 1];
-    auto q_regs = [&](const Seg &sg) {
+    // The queries in registers: asked for before the rows, behind which they would
+    // come, and used when the rows are there.
+    auto q_ask = [&](const Seg &sg) {
         if (!C::QREG) return;
         uint32_t o[WPT][4];
 #pragma unroll
-        for (int w = 0; w < WPT; ++w) q_words(sg, g, WPT * t + w, 0, o[w]);
+        for (int w = 0; w < WPT; ++w) q_load(sg, g, WPT * t + w, o[w]);
 #pragma unroll
         for (int x = 0; x < 4 * WPT; ++x) q[C::QREG ? x : 0] = o[x >> 2][x & 3];
+    };
+    auto q_use = [&](bool ok) {
+#pragma unroll
+        for (int x = 0; x < (C::QREG ? 2 * KS : 0); ++x) q[C::QREG ? x : 0] = ok ? bf2_poison(q[C::QREG ? x : 0]) : 0u;
     };
     auto q_info = [&](const Seg &sg, int to) {  // token and position of the rows
         if (tid >= R) return;
@@ -154,7 +165,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         const bool ok = r < a.n * a.G && sg.key.live && i < sg.key.cnt;
         rowinfo[to][tid] = ok ? make_int2(i, kv4_pos(sg.key.P, a.mask ? a.depth + sg.b * a.depth_b : nullptr, i)) : make_int2(-1, 0);
     };
-    q_regs(cur);
+    q_ask(cur);
+    int mine = my_tiles(cur);
+    for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
+
     q_info(cur, 0);
     __syncthreads();
     int info = 0;  // which of the two is this segment's
@@ -163,6 +177,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         const Kv4Keys key = cur.key;
         const int b = cur.b, rt = cur.rt, h = cur.h, P = key.P, end = P + key.cnt;
         const int2 *rows = rowinfo[info];
+        q_use(rows[g].x >= 0);
         if (!C::QREG) {
             for (int x = tid; x < NT * SPL * (KS / 2) * 32; x += FT) {  // one word: two steps of a lane
                 const int l = x & 31, w = (x >> 5) % WPT, sp = (x >> 5) / WPT % SPL, nt = (x >> 5) / WPT / SPL;
@@ -350,12 +365,12 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         const bool whole = cur.whole();
         const bool more = cur.next(a, R, RT);
         mine = more ? my_tiles(cur) : 0;
-        if (more) place_rows(cur);
-        for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
         if (more) {
-            q_regs(cur);
-            q_info(cur, info ^ 1);
+            place_rows(cur);
+            q_ask(cur);
         }
+        for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
+        if (more) q_info(cur, info ^ 1);
         // merge the warps
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)

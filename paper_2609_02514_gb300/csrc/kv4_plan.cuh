@@ -54,9 +54,8 @@ struct Kv4Keys {
 };
 
 template <int KT, int TPU>
-__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int rt) {
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq &sq, int rt) {
     Kv4Keys k;
-    const Kv4Seq sq = kv4_seq(a.prefix, a.count, b, a.n, a.S);
     k.P = sq.P, k.cnt = sq.cnt;
     const int r0 = rt * R, r1 = min(r0 + R, a.n * a.G);  // at most 2^30 rows
     k.i0 = r0 / a.G;
@@ -73,6 +72,10 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int r
     }
     k.units = max(1, (k.tiles + TPU - 1) / TPU);
     return k;
+}
+template <int KT, int TPU>
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int rt) {
+    return kv4_keys<KT, TPU>(a, R, kv4_seq(a.prefix, a.count, b, a.n, a.S), rt);
 }
 // first key of the x-th tile
 template <int KT>
@@ -175,18 +178,31 @@ template <int KT, int TPU, int FIX>
 struct Kv4Seg {
     unsigned long long left;  // units after this segment
     int b, rt, h, x0, x1;
+    int next_P, next_cnt;     // of the next sequence, loaded long before they are wanted
     Kv4Keys key;
+    __device__ __forceinline__ void ask(const Kv4Att &a) {
+        const int nb = min(b + 1, a.B - 1);
+        next_P = a.prefix[nb];
+        next_cnt = a.count ? a.count[nb] : a.n;
+    }
     __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
         if (at.left == 0) return false;
         b = at.b, rt = at.rt, h = at.h, left = at.left, key = at.key;
+        ask(a);
         return take(at.off);
     }
     __device__ __forceinline__ bool next(const Kv4Att &a, int R, int RT) {
         if (left == 0) return false;
         if (++h == a.H) {
             h = 0;
-            if (++rt == RT) rt = 0, ++b;
-            key = kv4_keys<KT, TPU>(a, R, b, rt);
+            Kv4Seq sq{key.P, key.cnt, true};
+            if (++rt == RT) {
+                rt = 0, ++b;
+                sq.P = next_P, sq.cnt = next_cnt;
+                ask(a);
+            }
+            sq.ok = sq.P >= 0 && sq.cnt >= 0 && sq.cnt <= a.n && (long long)sq.P + sq.cnt <= a.S;
+            key = kv4_keys<KT, TPU>(a, R, sq, rt);
         }
         return take(0);
     }
