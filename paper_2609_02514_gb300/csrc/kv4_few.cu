@@ -12,7 +12,13 @@ namespace aces {
 constexpr int FW = 8;            // warps
 constexpr int FT = FW * 32;
 constexpr int FKT = 32;          // keys of a tile: one warp's step
-constexpr int FFIX = 3;          // units an item costs beside its keys
+// Measured on 304 CTAs of ragged single tokens: 3.4 thousand cycles a unit (eight
+// tiles), 9.5 thousand an item.
+struct FewCost {
+    static constexpr int FIX = 3, MOST = 1;
+    static __device__ __forceinline__ int weight(const Kv4Keys &) { return 1; }
+    static __device__ __forceinline__ int all(const Kv4Keys &k) { return FIX + k.units; }
+};
 constexpr float F_LAZY = 8.0f;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -71,9 +77,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (!direct) pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
-    using Seg = Kv4Seg<FKT, FW, FFIX>;
-    const Kv4Start at = direct ? kv4_whole<FKT, FW, FFIX>(a, R, RT) : kv4_start<FKT, FW, FFIX, FT>(a, R, RT);
-    if (tid == 0 && !direct) kv4_put_info<FFIX>(ws, at);
+    using Seg = Kv4Seg<FKT, FW, FewCost>;
+    const Kv4Start at = direct ? kv4_whole<FKT, FW, FewCost>(a, R, RT) : kv4_start<FKT, FW, FewCost, FT>(a, R, RT);
+    if (tid == 0 && !direct) kv4_put_info<FewCost>(ws, at);
     __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
     if (!cur.start(a, R, RT, at)) return;
@@ -458,7 +464,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // and its warps every eighth piece, so that all loads are under way at once.
 constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32>
-__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y, int fix) {
+__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
     constexpr int D4 = D / 4, PW = 32 / D4;  // float4 of a row; pieces a warp reads at a time
     __shared__ int late;
     __shared__ float4 part[JW][D4];
@@ -477,9 +483,9 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
         return;
     }
     const Kv4Info in = ws.info[c];
-    // inside the item, beyond its FIX units, and the first to start there
-    if (in.cnt < 0 || in.off <= fix || in.off - in.quantum > fix) return;
-    const int pieces = 1 + (in.units - in.off + in.quantum - 1) / in.quantum;
+    // inside the item, and the first to start there
+    if (in.cnt < 0 || in.off < in.inside || in.off - in.quantum >= in.inside) return;
+    const int pieces = 1 + (in.all - in.off + in.quantum - 1) / in.quantum;
     const int stride = R * (D + 2), NR = min(R, a.n * a.G - in.rt * R);
     const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off >= in.quantum ? 0 : 1)) * stride;
     const float *rest = ws.piece + (size_t)(2 * (c - 1)) * stride;  // piece p > 0 at 2 p strides
@@ -557,11 +563,11 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
     }
 }
 
-cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, int fix, cudaStream_t s) {
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
     const int rows = a.n * a.G < R ? a.n * a.G : R;
     const int Y = rows < 16 ? rows : 16;  // blocks of an item
     const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true> : k_kv4_join<64, false>) : (a.f32 ? k_kv4_join<128, true> : k_kv4_join<128, false>);
-    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y, fix);
+    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
 
 template <int D, bool F32, int NT>
@@ -577,7 +583,7 @@ static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
     if (e != cudaSuccess) return e;
     k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT, direct);
     e = cudaGetLastError();
-    return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, FFIX, s);
+    return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, s);
 }
 
 // Rows of a tile: 8 when a head's rows fit (or float32 has few), else 16.

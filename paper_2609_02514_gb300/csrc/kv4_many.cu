@@ -37,7 +37,14 @@ constexpr int MSM = 8, MDQ = 6;           // softmax and dequantising warps
 constexpr int MLD = MSM + MDQ, MMM = MLD + 1;  // the warp that loads, the one that issues
 constexpr int MT = (MMM + 1) * 32;        // 16 warps of 128 registers
 constexpr int MDT = MDQ * 32;
-constexpr int MFIX = 4;                   // tiles' time that an item costs beside its keys
+// Measured on 152 CTAs, in thousands of cycles: a tile of two groups' rows 4.1 (D =
+// 64: 4.4), of one's 2.7; an item 15.5 (D = 64: 10.2).
+template <int D>
+struct ManyCost {
+    static constexpr int FIX = D == 128 ? 23 : 14, MOST = 6;
+    static __device__ __forceinline__ int weight(const Kv4Keys &k) { return k.rows <= 128 ? 4 : 6; }
+    static __device__ __forceinline__ int all(const Kv4Keys &k) { return FIX + k.units * weight(k); }
+};
 constexpr float M_LAZY = 8.0f;
 // -- tcgen05 ------------------------------------------------------------------
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -240,7 +247,8 @@ __device__ __forceinline__ void store_piece(uint8_t *tile, int p, const Piece<D>
 template <int D>
 __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, int RT) {
     using C = Many<D>;
-    using Seg = Kv4Seg<MKT, 1, MFIX>;
+    using Cost = ManyCost<D>;
+    using Seg = Kv4Seg<MKT, 1, Cost>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) unsigned long long bars[33];
     __shared__ uint32_t tmem_base;
@@ -277,8 +285,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     }
     pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    const Kv4Start at = kv4_start<MKT, 1, MFIX, MT>(a, R, RT);
-    if (tid == 0) kv4_put_info<MFIX>(ws, at);
+    const Kv4Start at = kv4_start<MKT, 1, Cost, MT>(a, R, RT);
+    if (tid == 0) kv4_put_info<Cost>(ws, at);
     Seg seg;
     if (!seg.start(a, R, RT, at)) return;
     if (warp == MMM) {
@@ -690,7 +698,7 @@ static cudaError_t run_many(const Kv4Att &a, void *workspace, int nsm, cudaStrea
     if (e != cudaSuccess) return e;
     k_kv4_many<D><<<nsm, MT, Many<D>::SMEM, s>>>(a, ws, R, RT);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_kv4_join(a, ws, nsm, R, MFIX, s);
+    return e != cudaSuccess ? e : launch_kv4_join(a, ws, nsm, R, s);
 }
 
 cudaError_t launch_kv4_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {

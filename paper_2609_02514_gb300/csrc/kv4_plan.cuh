@@ -6,9 +6,10 @@
 // counts the units of all items itself (one thread an entry (b, row tile), all
 // of whose heads have the same) and takes the units [c Q, (c + 1) Q), Q the
 // whole number that spreads them over the grid: CTAs are equally long whatever
-// the lengths.  What an item costs beside its keys (its queries, its merge, its
-// way out) counts as FIX units before its first: without, a CTA that got the
-// short sequences of a ragged batch took twice the others' time.  An item inside
+// the lengths.  Units are counted by their time (Cost::weight), and what an item
+// costs beside its keys (its queries, its merge, its way out) counts as Cost::FIX
+// before its first: without, a CTA that got the short sequences of a ragged
+// batch took twice the others' time.  An item inside
 // one CTA's range is written out by it; the pieces of one that several share go
 // to the workspace as sums not yet divided, with their reference maximum, and
 // k_kv4_join adds them in the CTAs' order.
@@ -23,12 +24,16 @@ namespace aces {
 
 constexpr int KV4_DIRECT = 8;
 
-struct Kv4Info {  // of the item in which a CTA's range starts (off and units with the FIX)
-    int b, rt, h, off, units, quantum;
+struct Kv4Info {  // of the item in which a CTA's range starts
+    int b, rt, h;
+    int off, all;  // where in the item, of what in all, in the measure of Cost
+    int inside;    // the least `off` that lies beyond its first unit
+    int quantum;
     int cnt;      // the sequence's tokens (0: none in the cache); -1: the CTA has nothing to do
     int timeout;
+    int pad[3];
 };
-static_assert(sizeof(Kv4Info) == 32, "Kv4Info layout");
+static_assert(sizeof(Kv4Info) == 48, "Kv4Info layout");
 
 // Workspace: Kv4Info[C], then 2 C pieces of R * (D + 2) floats (a CTA's first
 // piece and its last).
@@ -50,6 +55,7 @@ struct Kv4Keys {
     int P, cnt, i0, i1;    // tokens [i0, i1]
     int lo, hi, s_hi;
     int st, mt0, tiles, units;
+    int rows;              // of the tile
     bool live;
 };
 
@@ -58,6 +64,7 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq
     Kv4Keys k;
     k.P = sq.P, k.cnt = sq.cnt;
     const int r0 = rt * R, r1 = min(r0 + R, a.n * a.G);  // at most 2^30 rows
+    k.rows = r1 - r0;
     k.i0 = r0 / a.G;
     k.i1 = min((r1 - 1) / a.G, sq.cnt - 1);
     k.live = sq.ok && k.i0 < sq.cnt;
@@ -99,14 +106,14 @@ __device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end,
     return !a.window || kp > pos - a.window || kp < a.sinks;
 }
 
-// A CTA's range and the item it starts in, by all NTH threads.  off and left
-// count the FIX units.
+// A CTA's range and the item it starts in, by all NTH threads.  off and left are
+// in the measure of Cost.
 struct Kv4Start {
     unsigned long long left;
     int quantum, b, rt, h, off, cnt;
     Kv4Keys key;
 };
-template <int KT, int TPU, int FIX, int NTH>
+template <int KT, int TPU, class Cost, int NTH>
 __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     __shared__ unsigned long long red[NTH / 32];
     __shared__ Kv4Start found;
@@ -116,14 +123,15 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     Kv4Keys k;
     for (int e = e0; e < e1; ++e) {
         k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
-        sum += (unsigned long long)(k.units + FIX) * a.H;
+        sum += (unsigned long long)Cost::all(k) * a.H;
     }
     unsigned long long at = block_exscan_n<NTH>(sum, red, &total);
-    const unsigned long long Q = (total + gridDim.x - 1) / gridDim.x, w0 = Q * blockIdx.x;
+    // (at least a unit's weight: no CTA between two others is left without one)
+    const unsigned long long Q = max((total + gridDim.x - 1) / gridDim.x, (unsigned long long)Cost::MOST), w0 = Q * blockIdx.x;
     if (w0 >= at && w0 < at + sum) {
         for (int e = e0; e < e1; ++e) {
             if (per > 1) k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
-            const unsigned u = k.units + FIX;
+            const unsigned u = Cost::all(k);
             if (w0 < at + (unsigned long long)u * a.H) {
                 const unsigned x = (unsigned)(w0 - at);
                 found.b = e / RT, found.rt = e % RT, found.h = (int)(x / u), found.off = (int)(x % u);
@@ -142,14 +150,14 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
 }
 
 // Without a split: a CTA has the whole item.
-template <int KT, int TPU, int FIX>
+template <int KT, int TPU, class Cost>
 __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT) {
     Kv4Start s;
     const int e = blockIdx.x / a.H;
     s.h = blockIdx.x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
     s.off = 0;
     s.key = kv4_keys<KT, TPU>(a, R, s.b, s.rt);
-    s.left = s.quantum = s.key.units + FIX;
+    s.left = s.quantum = Cost::all(s.key);
     s.cnt = s.key.cnt;
     if (threadIdx.x == 0 && s.h == 0 && s.rt == 0)
         a.status[s.b] = kv4_seq(a.prefix, a.count, s.b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
@@ -163,20 +171,20 @@ inline int kv4_most_units(const Kv4Att &a, int keys) {
 }
 
 // writes the info of the CTA's start (one thread)
-template <int FIX>
+template <class Cost>
 __device__ __forceinline__ void kv4_put_info(const Kv4Ws &ws, const Kv4Start &at) {
     Kv4Info in;
-    const bool some = at.left > 0;
-    in.b = at.b, in.rt = at.rt, in.h = at.h, in.off = at.off, in.units = at.key.units + FIX, in.quantum = at.quantum;
-    in.cnt = some ? at.cnt : -1;
+    in.b = at.b, in.rt = at.rt, in.h = at.h, in.off = at.off, in.all = Cost::all(at.key), in.quantum = at.quantum;
+    in.inside = Cost::FIX + Cost::weight(at.key);
+    in.cnt = at.left > 0 ? at.cnt : -1;
     in.timeout = 0;
     ws.info[blockIdx.x] = in;
 }
 
 // A CTA's segments, one after another: units [x0, x1) of an item.
-template <int KT, int TPU, int FIX>
+template <int KT, int TPU, class Cost>
 struct Kv4Seg {
-    unsigned long long left;  // units after this segment
+    unsigned long long left;  // after this segment, in the measure of Cost
     int b, rt, h, x0, x1;
     int next_P, next_cnt;     // of the next sequence, loaded long before they are wanted
     Kv4Keys key;
@@ -206,12 +214,13 @@ struct Kv4Seg {
         }
         return take(0);
     }
-    // from unit `off` of the item on; false when the range ends among its FIX units
-    // (one that starts among them has the item's first unit, or ends there too)
+    // From `off` of the item on, or as far as the range goes: a unit is the CTA's in
+    // whose range the end of its weight lies.  False when the range ends before the
+    // item's first unit does.
     __device__ __forceinline__ bool take(int off) {
-        const int to = (int)min((unsigned long long)(key.units + FIX), off + left);
+        const int to = (int)min((unsigned long long)Cost::all(key), off + left), wt = Cost::weight(key);
         left -= to - off;
-        x0 = max(off - FIX, 0), x1 = max(to - FIX, 0);
+        x0 = max(off - Cost::FIX, 0) / wt, x1 = max(to - Cost::FIX, 0) / wt;
         return x1 > x0;
     }
     // first row of the item's key head in a plane
@@ -232,7 +241,7 @@ inline cudaError_t allow_smem(F *fn, int bytes, std::atomic<unsigned long long> 
     return e;
 }
 
-cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, int fix, cudaStream_t s);
+cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
 size_t kv4_few_ws(int n, int G, int D, int nsm);
 cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
 size_t kv4_many_ws(int n, int G, int D, int nsm);
