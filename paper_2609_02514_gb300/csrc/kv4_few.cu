@@ -460,8 +460,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // group c (Y blocks) takes the item in which the range of CTA c starts, when c is
 // the first to start inside it.  Block 0 writes the sequences' status.  The grid
 // is launched while the attention runs and waits for its end.
-// Few pieces: a warp takes a row.  More (one long sequence): the block takes a row
-// and its warps every eighth piece, so that all loads are under way at once.
+// Two or three pieces (the rule): a warp takes two rows, all their loads under way
+// at once.  More (one long sequence): the block takes a row and its warps every
+// eighth piece.
 constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32>
 __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
@@ -534,10 +535,38 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
         if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     };
     float M, L;
-    if (pieces <= JW) {
-        for (int row = y * JW + warp; row < NR; row += Y * JW) {
-            const float4 o = add(row, 0, 1, M, L);
-            if (lane < D4) put(row, lane, o, M, L);
+    if (pieces <= 3) {
+        constexpr int RW = 2 * PW;  // rows of a warp at a time (D = 64: a half warp a row)
+        for (int row0 = (y * JW + warp) * RW; row0 < NR; row0 += Y * JW * RW) {
+            float4 v[2][3];
+            float m[2][3], l[2][3];
+            const int d4 = lane % D4;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = min(row0 + x * PW + lane / D4, NR - 1);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    const float *pc = piece(min(p, pieces - 1));
+                    v[x][p] = *reinterpret_cast<const float4 *>(pc + row * D + 4 * d4);
+                    m[x][p] = pc[R * D + row], l[x][p] = pc[R * D + R + row];
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = row0 + x * PW + lane / D4;
+                if (pieces < 3) m[x][2] = -INFINITY;
+                const float top = fmaxf(fmaxf(m[x][0], m[x][1]), m[x][2]), ref = top == -INFINITY ? 0.0f : top;
+                float sum = 0.0f;
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    if (p >= pieces) break;
+                    const float f = ex2(m[x][p] - ref);
+                    sum = fmaf(l[x][p], f, sum);
+                    o.x = fmaf(v[x][p].x, f, o.x), o.y = fmaf(v[x][p].y, f, o.y), o.z = fmaf(v[x][p].z, f, o.z), o.w = fmaf(v[x][p].w, f, o.w);
+                }
+                if (row < NR) put(row, d4, o, top, sum);
+            }
         }
     } else {
         for (int row = y; row < NR; row += Y) {
