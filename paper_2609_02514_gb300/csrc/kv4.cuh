@@ -39,18 +39,29 @@ __device__ __forceinline__ float kv4_t(float a) {
     return __uint_as_float((u & 0x80000000u) | m);
 }
 
-// code of x for the step s (inv: about 1 / s; h: |s| / 2; a step of 0: 0 and infinity).  The estimate of
-// x / s may be a little off; the rest d = x - r s is exact (r s has at most nine
-// bits, and d lies on x's grid below |x| or is x), so it decides, on a half to
-// even.  Whole numbers live in the low bits of 1.5 * 2^23 + r: no conversions,
-// which run at a quarter of the rate.
+// Code of x for the step s (inv: 1 / s; h: |s| / 2; a step of 0: 0 and infinity).
+// Whole numbers live in the low bits of 1.5 * 2^23 + r: no conversions, which run
+// at a quarter of the rate.  |x| is at most 8.25 |s|, and above 8 |s| only on the
+// side of -8, so only the other end is cut.
+//   bfloat16 x: the quotient after one Newton step is exact where it can be held,
+//   and a half can; any other is further from a half than that step's error.
+//   float32 x: the estimate may be a little off; the rest d = x - r s is exact (r s
+//   has at most nine bits, and d lies on x's grid below |x| or is x), so it
+//   decides, on a half to even.
+template <bool F32>
 __device__ __forceinline__ uint32_t kv4_code(float x, float s, float inv, float h) {
     constexpr float BIG = 12582912.0f;
-    const float e = fmaf(x, inv, BIG), r = e - BIG, d = fmaf(-r, s, x);
-    const bool odd = __float_as_uint(e) & 1u;
-    const float one = __uint_as_float(0x3F800000u | ((__float_as_uint(d) ^ __float_as_uint(s)) & 0x80000000u));
-    const float off = fabsf(d) > h || (odd && fabsf(d) == h) ? one : 0.0f;
-    return __float_as_uint(fminf(fmaxf(r + off, -8.0f), 7.0f) + (BIG + 8.0f)) & 15u;
+    float e;
+    if (F32) {
+        e = fmaf(x, inv, BIG);
+        const float d = fmaf(BIG - e, s, x);
+        const float one = __uint_as_float(0x3F800000u | ((__float_as_uint(d) ^ __float_as_uint(s)) & 0x80000000u));
+        if (fabsf(d) > h || (fabsf(d) == h && (__float_as_uint(e) & 1u))) e += one;
+    } else {
+        const float q = x * inv;
+        e = fmaf(fmaf(-q, s, x), inv, q) + BIG;
+    }
+    return (__float_as_uint(fminf(e, BIG + 7.0f)) ^ 8u) & 15u;
 }
 
 // The number of a sequence's cached positions and of its new ones.

@@ -45,33 +45,40 @@ __device__ __forceinline__ void load_group(const void *base, long long at, bool 
 }
 
 // D / 8 numbers -> D / 64 words of codes and the group's t
-template <int G>
-__device__ __forceinline__ void quantise(const float (&x0)[G], uint32_t (&w)[G / 8], float *t_out, bool *bad) {
-    float x[G], a = 0.0f;
-    bool nf = false;
+template <int G, bool F32>
+__device__ __forceinline__ void quantise(float (&x)[G], uint32_t (&w)[G / 8], float *t_out, bool *bad) {
+    float m = 0.0f, z = 0.0f;
 #pragma unroll
-    for (int i = 0; i < G; ++i) {
-        nf |= !(fabsf(x0[i]) <= FLT_MAX);
-        x[i] = x0[i] == x0[i] ? fminf(fmaxf(x0[i], -KV4_CAP), KV4_CAP) : 0.0f;
-        if (fabsf(x[i]) > fabsf(a)) a = x[i];  // the first of the largest
+    for (int i = 0; i < G; ++i) m = fmaxf(m, fabsf(x[i])), z = fmaf(x[i], 0.0f, z);  // z is NaN when any is not finite
+    *bad = z != z;
+    if (*bad || m > KV4_CAP) {
+        m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -KV4_CAP), KV4_CAP) : 0.0f;
+            m = fmaxf(m, fabsf(x[i]));
+        }
     }
+    float a = 0.0f;
+#pragma unroll
+    for (int i = G - 1; i >= 0; --i)
+        if (fabsf(x[i]) == m) a = x[i];  // the first of the largest
     const float t = kv4_t(a), s = t * KV4_STEP;
     const float inv = s == 0.0f ? 0.0f : __frcp_rn(s), h = s == 0.0f ? INFINITY : 0.5f * fabsf(s);
 #pragma unroll
     for (int i = 0; i < G / 8; ++i) {
         w[i] = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[i] |= kv4_code(x[8 * i + e], s, inv, h) << (4 * (e >> 1) + 16 * (e & 1));
+        for (int e = 0; e < 8; ++e) w[i] |= kv4_code<F32>(x[8 * i + e], s, inv, h) << (4 * (e >> 1) + 16 * (e & 1));
     }
     *t_out = t;
-    *bad = nf;
 }
 
 template <int D, bool F32>
-__global__ void __launch_bounds__(NT4) k_kv4_append(Kv4Rows a, int T) {
+__global__ void __launch_bounds__(NT4) k_kv4_append(Kv4Rows a, int lt) {
     constexpr int G = D / KV4_GROUPS, RB = kv4_row_bytes(D);
     __shared__ int st[8];
-    const int per = (a.n + T - 1) / T;  // CTAs of a sequence
+    const int T = 1 << lt, per = (a.n + T - 1) >> lt;  // CTAs of a sequence
     const int b = blockIdx.x / per, i0 = (blockIdx.x - b * per) * T;
     const int start = a.start[b], cnt = a.count ? a.count[b] : a.n;
     if (threadIdx.x < T) st[threadIdx.x] = 0;
@@ -79,7 +86,7 @@ __global__ void __launch_bounds__(NT4) k_kv4_append(Kv4Rows a, int T) {
     const int total = 2 * a.H * T * KV4_GROUPS;
     for (int x = threadIdx.x; x < total; x += NT4) {
         const int g = x % KV4_GROUPS, r = x / KV4_GROUPS;
-        const int tok = r % T, ph = r / T, plane = ph >= a.H, h = ph - plane * a.H;
+        const int tok = r & (T - 1), ph = r >> lt, plane = ph >= a.H, h = ph - plane * a.H;
         const int i = i0 + tok;
         if (i >= a.n || i >= cnt) continue;
         const long long pos = (long long)start + i;
@@ -92,7 +99,7 @@ __global__ void __launch_bounds__(NT4) k_kv4_append(Kv4Rows a, int T) {
         bool bad;
         const long long at = plane ? b * a.vb + i * a.vi + h * a.vh : b * a.kb + i * a.ki + h * a.kh;
         load_group<G, F32>(plane ? a.xv : a.xk, at + g * G, a.vec, v);
-        quantise<G>(v, w, &t, &bad);
+        quantise<G, F32>(v, w, &t, &bad);
         if (bad) atomicOr(&st[tok], ACES_ROW_NONFINITE);
         if (!ACES_IN(pos, a.S)) continue;
         uint8_t *row = (plane ? a.v : a.k) + ((size_t)((size_t)b * a.H + h) * a.S + (size_t)pos) * RB;
@@ -108,15 +115,15 @@ __global__ void __launch_bounds__(NT4) k_kv4_append(Kv4Rows a, int T) {
 }
 
 template <int D, bool F32>
-__global__ void __launch_bounds__(NT4) k_kv4_read(Kv4Rows a, int T) {
+__global__ void __launch_bounds__(NT4) k_kv4_read(Kv4Rows a, int lt) {
     constexpr int G = D / KV4_GROUPS, RB = kv4_row_bytes(D);
-    const int per = (a.n + T - 1) / T;
+    const int T = 1 << lt, per = (a.n + T - 1) >> lt;
     const int b = blockIdx.x / per, i0 = (blockIdx.x - b * per) * T;
     const int start = a.start[b];
     const int total = 2 * a.H * T * KV4_GROUPS;
     for (int x = threadIdx.x; x < total; x += NT4) {
         const int g = x % KV4_GROUPS, r = x / KV4_GROUPS;
-        const int tok = r % T, ph = r / T, plane = ph >= a.H, h = ph - plane * a.H;
+        const int tok = r & (T - 1), ph = r >> lt, plane = ph >= a.H, h = ph - plane * a.H;
         const int i = i0 + tok;
         if (i >= a.n) continue;
         const long long pos = (long long)start + i;
@@ -156,14 +163,14 @@ __global__ void __launch_bounds__(NT4) k_kv4_read(Kv4Rows a, int T) {
     }
 }
 
-// Tokens of a CTA: eight neighbours (rows of 640 or 384 bytes in a piece)
-// once that still gives every SM four CTAs, else one.
-static int tokens_per_cta(const Kv4Rows &a, int nsm) { return (long long)a.B * a.n >= 8ll * 4 * nsm ? 8 : 1; }
+// Tokens of a CTA (their logarithm): eight neighbours (rows of 640 or 384 bytes in a
+// piece) once that still gives every SM four CTAs, else one.
+static int tokens_per_cta(const Kv4Rows &a, int nsm) { return (long long)a.B * a.n >= 8ll * 4 * nsm ? 3 : 0; }
 
 template <bool APPEND>
 static cudaError_t launch_rows(const Kv4Rows &a, int nsm, cudaStream_t s) {
-    const int T = tokens_per_cta(a, nsm);
-    const long long grid = (long long)a.B * ((a.n + T - 1) / T);
+    const int lt = tokens_per_cta(a, nsm);
+    const long long grid = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
     void (*fn)(Kv4Rows, int) = nullptr;
     if (APPEND)
         fn = a.D == 64 ? (a.f32 ? k_kv4_append<64, true> : k_kv4_append<64, false>)
@@ -171,7 +178,7 @@ static cudaError_t launch_rows(const Kv4Rows &a, int nsm, cudaStream_t s) {
     else
         fn = a.D == 64 ? (a.f32 ? k_kv4_read<64, true> : k_kv4_read<64, false>)
                        : (a.f32 ? k_kv4_read<128, true> : k_kv4_read<128, false>);
-    fn<<<(unsigned)grid, NT4, 0, s>>>(a, T);
+    fn<<<(unsigned)grid, NT4, 0, s>>>(a, lt);
     return cudaGetLastError();
 }
 
