@@ -525,6 +525,32 @@ def kv4_workspace_bytes(B: int, n: int, Hq: int, H: int, D: int) -> int:
     return int(load().aces_kv4_workspace_bytes(int(B), int(n), int(Hq), int(H), int(D)))
 
 
+_kv4_sizes = {}                # workspace bytes by shape
+_kv4_kept = threading.local()  # .ws: (address, bytes, tensor) by device and stream
+
+
+def _kv4_scratch(B, n, Hq, H, D, dev, stream):
+    """Address and bytes of the workspace that this thread keeps for a stream: its
+    calls there come one after another.  (An allocation and its release take 3 us
+    of the host.)  A call that is being captured gets one of its own."""
+    key = (B, n, Hq, H, D, dev)
+    need = _kv4_sizes.get(key)
+    if need is None:
+        need = _kv4_sizes[key] = max(kv4_workspace_bytes(B, n, Hq, H, D), 16)
+    if torch.cuda.is_current_stream_capturing():
+        ws = _empty(need, dtype=_U8, device=dev)
+        return ws.data_ptr(), need, ws
+    try:
+        kept = _kv4_kept.ws
+    except AttributeError:
+        kept = _kv4_kept.ws = {}
+    ws = kept.get((dev, stream))
+    if ws is None or ws[1] < need:
+        t = _empty(need, dtype=_U8, device=dev)
+        ws = kept[(dev, stream)] = (t.data_ptr(), need, t)
+    return ws
+
+
 def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count=None, scale: float | None = None,
                   window: int = 0, sinks: int = 0, out: dict | None = None, workspace: torch.Tensor | None = None):
     """Attention of q [B, n, Hq, D] over the layer's cache, whose positions
@@ -564,18 +590,18 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
         o = _outputs(out, dev, ("out", shape, dtype), ("lse", (B, n, Hq), _F32), ("status", one, _I32))
         rp, lp = _out(o["out"], "out", shape, dtype, dev), _out(o["lse"], "lse", (B, n, Hq), _F32, dev)
         sp = _out(o["status"], "status", one, _I32, dev)
+    stream = _stream(dev)
     if workspace is None:
-        nbytes = lib.aces_kv4_workspace_bytes(B, n, Hq, H, D)
-        ws = _empty(nbytes, dtype=_U8, device=dev)
+        wp, nbytes, _ = _kv4_scratch(B, n, Hq, H, D, dev, stream)
     else:
         ws = _cuda(workspace, "workspace")
-        nbytes = ws.numel() * ws.element_size()
+        wp, nbytes = ws.data_ptr(), ws.numel() * ws.element_size()
         if ws.device != dev:
             raise ValueError(f"workspace must be on {dev}")
     code = lib.aces_kv4_attention(q.data_ptr(), _DTYPES[dtype], qs, cache.data_ptr(), planes, layer, B, n, Hq, H, S, D,
                                   _out(prefix_len, "prefix_len", one, _I32, dev),
                                   None if count is None else _out(count, "count", one, _I32, dev), mp, ms, dp, ds,
-                                  D ** -0.5 if scale is None else scale, window, sinks, rp, lp, sp, ws.data_ptr(), nbytes, _stream(dev))
+                                  D ** -0.5 if scale is None else scale, window, sinks, rp, lp, sp, wp, nbytes, stream)
     if code != 0:
         _check("aces_kv4_attention", code)
     return o
