@@ -41,8 +41,15 @@ aces_status check_rows(const void *k, const void *v, aces_dtype dt, const int32_
 }
 
 // Which kernel: bfloat16 queries of more than 16 rows a key head go to the
-// tcgen05 kernel, the others to the one that keeps its few rows in registers.
-bool many_rows(int f32, int n, int G) { return !f32 && (long long)n * G > 16; }
+// tcgen05 kernel, the others (and up to 32 rows of a few key heads, where latency
+// counts) to the one that keeps its few rows in registers.  Measured (us, D = 128,
+// eight key heads, few rows / tcgen05): 16 rows, 16 sequences of 16000 117 / 174,
+// 64 of 4000 133 / 193; 32 rows, the same 211 / 177 and 244 / 197, and one
+// sequence of 16000 33 / 37; 20 rows, one of 4000 20 / 27.
+bool many_rows(int f32, int B, int H, int n, int G) {
+    const long long rows = (long long)n * G;
+    return !f32 && rows > ((long long)B * H <= 32 ? 32 : 16);
+}
 
 }  // namespace
 
@@ -97,7 +104,7 @@ size_t aces_kv4_workspace_bytes(int B, int n, int Hq, int H, int D) {
     if (B < 1 || n < 1 || H < 1 || Hq < H || Hq % H != 0 || (D != 64 && D != 128)) return 0;
     if ((long long)B * n > INT_MAX / 2 || (long long)B * n * Hq > INT_MAX / 2) return 0;
     const int G = Hq / H, nsm = sm_count();  // of either type
-    const size_t few = kv4_few_ws(n, G, D, nsm), many = many_rows(0, n, G) ? kv4_many_ws(n, G, D, nsm) : 0;
+    const size_t few = kv4_few_ws(n, G, D, nsm), many = many_rows(0, B, H, n, G) ? kv4_many_ws(n, G, D, nsm) : 0;
     return few > many ? few : many;
 }
 
@@ -134,7 +141,7 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
     a.window = window;
     a.sinks = window > 0 ? sinks : 0;
     a.scale = (float)((double)scale * 1.4426950408889634 * (double)KV4_STEP);
-    const auto launch = many_rows(a.f32, n, a.G) ? launch_kv4_many : launch_kv4_few;
+    const auto launch = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many : launch_kv4_few;
     return launch(a, workspace, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
 }
 

@@ -14,7 +14,9 @@
 // to the workspace as sums not yet divided, with their reference maximum, and
 // k_kv4_join adds them in the CTAs' order.
 // Where no item can have more than KV4_DIRECT units (the cache is short, or the
-// window), each is one CTA's, and there is nothing to join.
+// window), each is one CTA's, and there is nothing to join (the few-row kernel;
+// measured at 1000 keys, with / without a split: 16 sequences of eight key heads
+// 25 / 17 us, 64 41 / 39; at 4000 keys one sequence 16 / 31).
 #pragma once
 #include <atomic>
 
