@@ -364,6 +364,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                     }
                 }
             }
+            // The next copy into this place comes after these loads only if they are over:
+            // a fence between the two kinds of access.
+            async_fence();
             __syncwarp();
             if (y + ST < mine) issue(cur, y + ST, seq + ST);
         }

@@ -58,7 +58,6 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p;
 }
-__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -499,7 +498,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 // The warp's rows go out in whole lines, through the place of its
                 // queries: bfloat16 rows at once, float32 pieces half a row at a time.
                 constexpr int CH = D / 8;  // 16-byte chunks of a row there
-                auto chunk = [&](int rw, int c) { return reinterpret_cast<uint4 *>(myq + rw * (D * 2) + ((c ^ (rw & 7)) << 4)); };
+                // (each warp in its own rows' place: another may be at the next segment's queries)
+                auto chunk = [&](int rw, int c) { return reinterpret_cast<uint4 *>(myq + swz(rw, c)); };
                 bool full;
                 if (whole) {
 #pragma unroll
@@ -555,8 +555,6 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
 #pragma unroll
                 for (int u = 0; u < C::PC; ++u)
                     if (dt + u * MDT < C::PIECES) load_piece<D>(raw + rs * C::RAW, dt + u * MDT, p[u]);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_rfree + 8 * rs);
                 wait((v ? b_vfree : b_kfree) + 8 * st, (step >> 2) + 1);
                 uint8_t *tile = (v ? sv : sk) + st * C::TILE;
 #pragma unroll
@@ -564,7 +562,12 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     if (dt + u * MDT < C::PIECES) store_piece<D>(tile, dt + u * MDT, p[u]);
                 async_fence();
                 __syncwarp();
-                if (lane == 0) mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+                // The rows' place is given back only here: the next copy into it is not
+                // ordered after loads that are still under way.
+                if (lane == 0) {
+                    mbar_arrive((v ? b_vfull : b_kfull) + 8 * st);
+                    mbar_arrive(b_rfree + 8 * rs);
+                }
             }
         } while (seg.next(a, R, RT));
     } else if (warp == MLD) {
