@@ -136,6 +136,8 @@ def _open(path):
               lib.aces_cache_lookup, lib.aces_resample_sparse, lib.aces_tree_budget, lib.aces_branch_alloc,
               lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention):
         f.restype = I
+    # what the native half of the binding calls
+    lib.kv4_entries = tuple(ctypes.cast(f, P).value for f in (lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention))
     if hasattr(lib, "aces_checked_violation"):
         lib.aces_checked_violation.argtypes = [P]
         lib.aces_checked_violation.restype = I
@@ -434,39 +436,27 @@ def tree_mask(F, branch_len: int, device=None):
     return mask, depth
 
 
-# A call on one token is bound by the host, so the checks below are single
-# expressions that hold as a rule, and only where one fails is the reason looked
-# for: kv4_read() took 16 us of a Grace core, kv4_attention() 31.
+# The 4-bit cache's calls check their arguments, allocate and launch in the native
+# half of the binding (csrc/binding.cpp).
 _U8 = torch.uint8
-_I64x3 = ctypes.c_int64 * 3
+_native_module = None
 
 
-def _kv4_cache(cache):
-    """(planes, B, H, S, D) of a 4-bit cache."""
-    c = _cuda(cache, "cache")
-    if c.dtype is not _U8 or c.dim() != 5:
-        raise ValueError("cache must be uint8 [planes, B, H, S, row]")
-    planes, B, H, S, R = c.shape
-    return planes, B, H, S, 2 * (R - 16)
+def _native():
+    global _native_module
+    if _native_module is None:
+        try:
+            from . import _binding
+        except ImportError as e:
+            raise RuntimeError(f"_binding.so cannot be loaded ({e}): build it with `python -m paper_2609_02514_gb300.build`") from e
+        _native_module = _binding
+    return _native_module
 
 
-def _rows(t, name, dev):
-    """[B, n, heads, D] numbers on dev whose last dimension is dense: their strides."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 4 or t.dtype not in _DTYPES:
-        raise ValueError(f"{name} must be float32 or bfloat16 [B, n, heads, D]")
-    b, i, h, d = t.stride()
-    if (d != 1 and t.shape[3] != 1) or t.device != dev:
-        raise ValueError(f"{name} must have a dense last dimension and lie on {dev}")
-    return _I64x3(b, i, h)
-
-
-def _out(t, name, shape, dtype, dev):
-    """The address of a dense tensor of that shape on dev."""
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} on {dev}")
-    return t.data_ptr()
+def _kv4_device(cache):
+    if not isinstance(cache, torch.Tensor) or not cache.is_cuda:
+        raise ValueError("cache must be a CUDA tensor")
+    return cache.device
 
 
 def kv4_cache(layers: int, B: int, H: int, S: int, D: int, device=None):
@@ -482,19 +472,8 @@ def kv4_append(cache, layer: int, k, v, start, count=None, out: torch.Tensor | N
     """Quantise k, v [B, n, H, D] into the cache at positions start[b] + i (in
     place; tokens i >= count[b] are padding); returns row_status [B, n] int32.
     k and v may be strided views with a dense last dimension."""
-    lib = _lib or load()
-    planes, B, H, S, D = _kv4_cache(cache)
-    dev = cache.device
-    ks, vs = _rows(k, "k", dev), _rows(v, "v", dev)
-    shape, dtype = k.shape, k.dtype
-    n = shape[1]
-    if shape != (B, n, H, D) or v.shape != shape or v.dtype is not dtype:
-        raise ValueError(f"k and v must be alike, [{B}, n, {H}, {D}]")
-    one = (B,)
-    st = _empty((B, n), dtype=_I32, device=dev) if out is None else out
-    code = lib.aces_kv4_append(cache.data_ptr(), planes, layer, B, H, S, D, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], ks, vs,
-                               _out(start, "start", one, _I32, dev), None if count is None else _out(count, "count", one, _I32, dev), n,
-                               st.data_ptr() if out is None else _out(out, "out", (B, n), _I32, dev), _stream(dev))
+    lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
+    code, st = native.append(lib.kv4_entries[0], cache, layer, k, v, start, count, out, _stream(dev))
     if code != 0:
         _check("aces_kv4_append", code)
     return st
@@ -503,19 +482,11 @@ def kv4_append(cache, layer: int, k, v, start, count=None, out: torch.Tensor | N
 def kv4_read(cache, layer: int, start, n: int, dtype=torch.bfloat16, out: dict | None = None):
     """Positions start[b] .. start[b] + n - 1 of the cache as numbers: a dict of
     k, v [B, n, H, D] (zeros outside the cache)."""
-    lib = _lib or load()
-    planes, B, H, S, D = _kv4_cache(cache)
-    dt = _DTYPES.get(dtype)
-    if dt is None:
+    lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
+    if dtype not in _DTYPES:
         raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
-    dev, shape = cache.device, (B, n, H, D)
-    if out is None:
-        k, v = _empty(shape, dtype=dtype, device=dev), _empty(shape, dtype=dtype, device=dev)
-        o, kp, vp = {"k": k, "v": v}, k.data_ptr(), v.data_ptr()
-    else:
-        o = _outputs(out, dev, ("k", shape, dtype), ("v", shape, dtype))
-        kp, vp = _out(o["k"], "k", shape, dtype, dev), _out(o["v"], "v", shape, dtype, dev)
-    code = lib.aces_kv4_read(cache.data_ptr(), planes, layer, B, H, S, D, _out(start, "start", (B,), _I32, dev), n, kp, vp, dt, _stream(dev))
+    o = {} if out is None else dict(out)
+    code, o["k"], o["v"] = native.read(lib.kv4_entries[1], cache, layer, start, n, dtype is _F32, o.get("k"), o.get("v"), _stream(dev))
     if code != 0:
         _check("aces_kv4_read", code)
     return o
@@ -529,14 +500,19 @@ _kv4_sizes = {}                # workspace bytes by shape
 _kv4_kept = threading.local()  # .ws: (address, bytes, tensor) by device and stream
 
 
-def _kv4_scratch(B, n, Hq, H, D, dev, stream):
+def _kv4_scratch(q, cache, dev, stream):
     """Address and bytes of the workspace that this thread keeps for a stream: its
     calls there come one after another.  (An allocation and its release take 3 us
     of the host.)  A call that is being captured gets one of its own."""
-    key = (B, n, Hq, H, D, dev)
+    key = (q.shape, cache.shape, dev)
     need = _kv4_sizes.get(key)
     if need is None:
-        need = _kv4_sizes[key] = max(kv4_workspace_bytes(B, n, Hq, H, D), 16)
+        if q.dim() != 4 or cache.dim() != 5:
+            return 0, 0, None  # refused by the call
+        _, n, Hq, D = q.shape
+        if len(_kv4_sizes) > 1000:
+            _kv4_sizes.clear()
+        need = _kv4_sizes[key] = max(kv4_workspace_bytes(cache.shape[1], n, Hq, cache.shape[2], D), 16)
     if torch.cuda.is_current_stream_capturing():
         ws = _empty(need, dtype=_U8, device=dev)
         return ws.data_ptr(), need, ws
@@ -564,44 +540,19 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
     [B, n, Hq, D], lse [B, n, Hq] and status [B] (ROW_RANGE: a sequence whose
     tokens do not lie in the cache).
     """
-    lib = _lib or load()
-    planes, B, H, S, D = _kv4_cache(cache)
-    dev = cache.device
-    qs = _rows(q, "q", dev)
-    shape, dtype = q.shape, q.dtype
-    _, n, Hq, _ = shape
-    if shape[0] != B or shape[3] != D:
-        raise ValueError(f"q must be [{B}, n, Hq, {D}]")
-    mp = dp = None
-    ms = ds = 0
-    if mask is not None or depth is not None:
-        if mask is None or depth is None:
-            raise ValueError("mask and depth go together")
-        words = (n + 31) // 32
-        ms = n * words if mask.dim() == 3 else 0
-        mp = _out(mask, "mask", (B, n, words) if ms else (n, words), _I32, dev)
-        ds = n if depth.dim() == 2 else 0
-        dp = _out(depth, "depth", (B, n) if ds else (n,), _I32, dev)
-    one = (B,)
-    if out is None:
-        r, lse, st = _empty(shape, dtype=dtype, device=dev), _empty((B, n, Hq), dtype=_F32, device=dev), _empty(one, dtype=_I32, device=dev)
-        o, rp, lp, sp = {"out": r, "lse": lse, "status": st}, r.data_ptr(), lse.data_ptr(), st.data_ptr()
-    else:
-        o = _outputs(out, dev, ("out", shape, dtype), ("lse", (B, n, Hq), _F32), ("status", one, _I32))
-        rp, lp = _out(o["out"], "out", shape, dtype, dev), _out(o["lse"], "lse", (B, n, Hq), _F32, dev)
-        sp = _out(o["status"], "status", one, _I32, dev)
+    lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
     stream = _stream(dev)
     if workspace is None:
-        wp, nbytes, _ = _kv4_scratch(B, n, Hq, H, D, dev, stream)
+        wp, nbytes, _ = _kv4_scratch(q, cache, dev, stream)
     else:
         ws = _cuda(workspace, "workspace")
         wp, nbytes = ws.data_ptr(), ws.numel() * ws.element_size()
         if ws.device != dev:
             raise ValueError(f"workspace must be on {dev}")
-    code = lib.aces_kv4_attention(q.data_ptr(), _DTYPES[dtype], qs, cache.data_ptr(), planes, layer, B, n, Hq, H, S, D,
-                                  _out(prefix_len, "prefix_len", one, _I32, dev),
-                                  None if count is None else _out(count, "count", one, _I32, dev), mp, ms, dp, ds,
-                                  D ** -0.5 if scale is None else scale, window, sinks, rp, lp, sp, wp, nbytes, stream)
+    o = {} if out is None else dict(out)
+    code, o["out"], o["lse"], o["status"] = native.attention(
+        lib.kv4_entries[2], q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, o.get("out"), o.get("lse"),
+        o.get("status"), wp, nbytes, stream)
     if code != 0:
         _check("aces_kv4_attention", code)
     return o

@@ -5,6 +5,8 @@ shared library (CUDA runtime linked statically).  Re-running is a no-op when
 the library is newer than every source.  build(checked=True) makes the
 checked test build instead, libacespec_checked.so (-DACES_CHECKED: every
 kernel records out-of-range indices instead of using them).
+The native half of the Python binding (csrc/binding.cpp, against torch's
+headers) is compiled alongside with the host compiler, into _binding.so.
 """
 from __future__ import annotations
 
@@ -20,6 +22,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libacespec.so")
 LIB_CHECKED = os.path.join(HERE, "libacespec_checked.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
+BINDING = os.path.join(HERE, "_binding.so")
+BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 
 
@@ -46,9 +50,41 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
+def _start_binding(force: bool):
+    """The compiler at work on _binding.so (its command and process), or None when it is newer than its sources."""
+    deps = [BINDING_SRC, os.path.join(ROOT, "include", "acespec.h")]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in deps):
+        return None
+    import sysconfig
+
+    import torch
+    cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        raise RuntimeError("g++ not found: a C++ compiler is required to build _binding.so")
+    base = os.path.dirname(torch.__file__)
+    inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"]]
+    cmd = [cxx, "-std=c++17", "-O1", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+    cmd += [f"-I{i}" for i in inc] + ["-o", BINDING + f".tmp{os.getpid()}", BINDING_SRC, "-L" + os.path.join(base, "lib"),
+                                      "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    return cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+
+
+def _finish_binding(started) -> None:
+    if started is None:
+        return
+    cmd, p = started
+    out, _ = p.communicate()
+    if p.returncode != 0:
+        raise RuntimeError("the binding does not compile: " + " ".join(cmd) + "\n" + out.decode(errors="replace"))
+    os.replace(cmd[cmd.index("-o") + 1], BINDING)
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     lib = LIB_CHECKED if checked else LIB
+    binding = _start_binding(force)
     if not force and up_to_date(lib):
+        _finish_binding(binding)
         return lib
     nvcc = _nvcc()
     bdir = os.path.join(HERE, "_build_checked" if checked else "_build")
@@ -72,6 +108,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     if r.returncode != 0:
         raise RuntimeError("link failed: " + " ".join(link) + "\n" + r.stdout.decode() + r.stderr.decode())
     os.replace(tmp, lib)
+    _finish_binding(binding)
     return lib
 
 
