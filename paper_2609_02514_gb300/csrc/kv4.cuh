@@ -39,17 +39,17 @@ __device__ __forceinline__ float kv4_t(float a) {
     return __uint_as_float((u & 0x80000000u) | m);
 }
 
-// Code of x for the step s (inv: 1 / s; h: |s| / 2; a step of 0: 0 and infinity).
-// Whole numbers live in the low bits of 1.5 * 2^23 + r: no conversions, which run
-// at a quarter of the rate.  |x| is at most 8.25 |s|, and above 8 |s| only on the
-// side of -8, so only the other end is cut.
+// x / s as a whole number r (inv: 1 / s; h: |s| / 2; a step of 0: 0 and infinity), in
+// the bits of 1.5 * 2^23 + r: no conversions, which run at a quarter of the rate,
+// and a word of codes is the sum of the bits, shifted, and KV4_BITS.  |x| is at most
+// 8.25 |s|, and above 8 |s| only on the side of -8, so only the other end is cut.
 //   bfloat16 x: the quotient after one Newton step is exact where it can be held,
 //   and a half can; any other is further from a half than that step's error.
 //   float32 x: the estimate may be a little off; the rest d = x - r s is exact (r s
 //   has at most nine bits, and d lies on x's grid below |x| or is x), so it
 //   decides, on a half to even.
 template <bool F32>
-__device__ __forceinline__ uint32_t kv4_code(float x, float s, float inv, float h) {
+__device__ __forceinline__ uint32_t kv4_round(float x, float s, float inv, float h) {
     constexpr float BIG = 12582912.0f;
     float e;
     if (F32) {
@@ -61,8 +61,10 @@ __device__ __forceinline__ uint32_t kv4_code(float x, float s, float inv, float 
         const float q = x * inv;
         e = fmaf(fmaf(-q, s, x), inv, q) + BIG;
     }
-    return (__float_as_uint(fminf(e, BIG + 7.0f)) ^ 8u) & 15u;
+    return __float_as_uint(fminf(e, BIG + 7.0f));
 }
+// turns the bits 0x4B400000 + r into the code r + 8, at each of a word's eight places
+constexpr uint32_t KV4_BITS = (8u - 0x4B400000u) * 0x11111111u;
 
 // The number of a sequence's cached positions and of its new ones.
 struct Kv4Seq {
