@@ -4,8 +4,12 @@
 // step and its codes need no other thread.  A CTA takes a few tokens of one
 // sequence with all their heads, keys and values, so one store of a token's
 // status follows; within a CTA the tokens of one head are neighbours, whose
-// cache rows are too.  What bounds both is memory: numbers one side, 5/8 (D =
-// 128) or 3/4 of a byte each on the other.
+// cache rows are too.  What a large call has to do is to move numbers on one side
+// and 5/8 (D = 128) or 3/4 of a byte each on the other.  Reading does so at 6.4
+// TB/s (704.6 MB in 109.9 us).  Writing one to two thousand tokens a sequence is one
+// or two waves of CTAs, and its time is their start, one load's way from memory and
+// back, and 17 (bfloat16) to 38 (float32) instructions a number: 48.5 MB in 11.5 us,
+// half the issue slots taken while CTAs run.
 #define ACES_FILE 7  // site numbers of the checked build
 #include "kv4.cuh"
 
@@ -171,13 +175,18 @@ __global__ void __launch_bounds__(NT4) k_kv4_read(Kv4Rows a, int lt) {
     }
 }
 
-// Tokens of a CTA (their logarithm): eight neighbours (rows of 640 or 384 bytes in a
-// piece) once that still gives every SM four CTAs, else one.
-static int tokens_per_cta(const Kv4Rows &a, int nsm) { return (long long)a.B * a.n >= 8ll * 4 * nsm ? 3 : 0; }
+// Tokens of a CTA (their logarithm): several neighbours, whose rows of 80 or 48 bytes
+// lie side by side, once that still gives every SM four CTAs, else one.  Eight when
+// reading (16384 tokens of 8 sequences, eight heads of 128: 109.9 us, by fours
+// 114.4), four when writing (80 tokens of 64 sequences: 11.5 us, by eights 12.7, one
+// at a time 16.4; 4099 of 3, float32, four heads of 64: 12.3, 12.1, 28.4).
+static int tokens_per_cta(const Kv4Rows &a, int lt, int nsm) {
+    return (long long)a.B * a.n >= (4ll * nsm) << lt ? lt : 0;
+}
 
 template <bool APPEND>
 static cudaError_t launch_rows(const Kv4Rows &a, int nsm, cudaStream_t s) {
-    const int lt = tokens_per_cta(a, nsm);
+    const int lt = tokens_per_cta(a, APPEND ? 2 : 3, nsm);
     const long long grid = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
     void (*fn)(Kv4Rows, int) = nullptr;
     if (APPEND)
