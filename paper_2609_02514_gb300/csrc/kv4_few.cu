@@ -463,9 +463,11 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // group c (Y blocks) takes the item in which the range of CTA c starts, when c is
 // the first to start inside it.  Block 0 writes the sequences' status.  The grid
 // is launched while the attention runs and waits for its end.
-// Two or three pieces (the rule): a warp takes two rows, all their loads under way
-// at once.  More (one long sequence): the block takes a row and its warps every
-// eighth piece.
+// A warp takes four rows, eight lanes each, three pieces at a time with all their
+// loads under way at once.  Many pieces of up to 16 rows (one long sequence): the
+// block takes a row and its warps every eighth piece.  What bounds it is its start
+// and two dependent loads: 10.5 us for the 23.5 MB of 152 items of 256 rows of 128
+// (a warp a row, two at a time: 14.1), 7.6 for 300 of four rows, with cold caches.
 constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32>
 __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
@@ -537,42 +539,51 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
             reinterpret_cast<uint2 *>(a.out)[orow * D4 + d4] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
         if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     };
-    float M, L;
-    if (pieces <= 3) {
-        constexpr int RW = 2 * PW;  // rows of a warp at a time (D = 64: a half warp a row)
+    if (pieces <= 3 || NR > 16) {
+        constexpr int LN = 8, RW = 32 / LN, V = D4 / LN;  // lanes of a row, rows of a warp
+        const int d4 = lane % LN;
         for (int row0 = (y * JW + warp) * RW; row0 < NR; row0 += Y * JW * RW) {
-            float4 v[2][3];
-            float m[2][3], l[2][3];
-            const int d4 = lane % D4;
+            const int row = row0 + lane / LN, rd = min(row, NR - 1);
+            float top = -INFINITY, sum = 0.0f;
+            float4 o[V];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int row = min(row0 + x * PW + lane / D4, NR - 1);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    const float *pc = piece(min(p, pieces - 1));
-                    v[x][p] = *reinterpret_cast<const float4 *>(pc + row * D + 4 * d4);
-                    m[x][p] = pc[R * D + row], l[x][p] = pc[R * D + R + row];
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int row = row0 + x * PW + lane / D4;
-                if (pieces < 3) m[x][2] = -INFINITY;
-                const float top = fmaxf(fmaxf(m[x][0], m[x][1]), m[x][2]), ref = top == -INFINITY ? 0.0f : top;
-                float sum = 0.0f;
-                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int x = 0; x < V; ++x) o[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int p0 = 0; p0 < pieces; p0 += 3) {
+                float4 v[3][V];
+                float m[3], l[3];
 #pragma unroll
                 for (int p = 0; p < 3; ++p) {
-                    if (p >= pieces) break;
-                    const float f = ex2(m[x][p] - ref);
-                    sum = fmaf(l[x][p], f, sum);
-                    o.x = fmaf(v[x][p].x, f, o.x), o.y = fmaf(v[x][p].y, f, o.y), o.z = fmaf(v[x][p].z, f, o.z), o.w = fmaf(v[x][p].w, f, o.w);
+                    const float *pc = piece(min(p0 + p, pieces - 1));
+                    m[p] = pc[R * D + rd], l[p] = pc[R * D + R + rd];
+#pragma unroll
+                    for (int x = 0; x < V; ++x) v[p][x] = *reinterpret_cast<const float4 *>(pc + rd * D + 4 * (d4 + x * LN));
                 }
-                if (row < NR) put(row, d4, o, top, sum);
+                const float was = top;
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    if (p0 + p < pieces) top = fmaxf(top, m[p]);
+                const float ref = top == -INFINITY ? 0.0f : top, old = ex2(was - ref);
+                sum *= old;
+#pragma unroll
+                for (int x = 0; x < V; ++x) o[x].x *= old, o[x].y *= old, o[x].z *= old, o[x].w *= old;
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    if (p0 + p >= pieces) break;
+                    const float f = ex2(m[p] - ref);
+                    sum = fmaf(l[p], f, sum);
+#pragma unroll
+                    for (int x = 0; x < V; ++x)
+                        o[x].x = fmaf(v[p][x].x, f, o[x].x), o[x].y = fmaf(v[p][x].y, f, o[x].y), o[x].z = fmaf(v[p][x].z, f, o[x].z),
+                        o[x].w = fmaf(v[p][x].w, f, o[x].w);
+                }
             }
+            if (row < NR)
+#pragma unroll
+                for (int x = 0; x < V; ++x) put(row, d4 + x * LN, o[x], top, sum);
         }
     } else {
         for (int row = y; row < NR; row += Y) {
+            float M, L;
             const float4 o = add(row, warp, JW, M, L);
             if (lane < D4) part[warp][lane] = o;
             if (lane == 0) part_m[warp] = M, part_l[warp] = L;
@@ -597,7 +608,7 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
 
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s) {
     const int rows = a.n * a.G < R ? a.n * a.G : R;
-    const int Y = rows < 16 ? rows : 16;  // blocks of an item
+    const int Y = rows <= 16 ? rows : (rows + 31) / 32;  // blocks of an item
     const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true> : k_kv4_join<64, false>) : (a.f32 ? k_kv4_join<128, true> : k_kv4_join<128, false>);
     return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
