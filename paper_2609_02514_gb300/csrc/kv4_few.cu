@@ -32,6 +32,12 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     return d;
 }
 
+// A wait that gave up: the ring's other copies (a place without one costs as long a wait)
+template <int ST>
+static __device__ __noinline__ void mbar_drain(uint32_t bar0, int seq) {
+    for (int z = seq; z < seq + ST; ++z) mbar_wait_slow(bar0 + 8 * (z % ST), (z / ST) & 1);
+}
+
 template <int D, bool F32, int NT>
 struct Few {
     static constexpr int RB = kv4_row_bytes(D), R = 8 * NT, KS = D / 16, JT = D / 16, WPT = D / 32;
@@ -91,7 +97,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     auto place_rows = [&](const Seg &g) { kb = a.k + g.row0(a) * RB, vb = a.v + g.row0(a) * RB; };
     place_rows(cur);
     auto issue = [&](const Seg &g, int y, int place) {
-        if (lane != 0) return;
+        if (lane != 0 || bad) return;
         const int j0 = kv4_tile<FKT>(g.key, (g.x0 + y) * FW + warp), rows = min(FKT, g.key.P + g.key.cnt - j0);
         if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
         const int s = place % ST;
@@ -209,7 +215,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         }
         for (int y = 0; y < mine; ++y, ++seq) {
             const int s = seq % ST;
-            if (!bad && !mbar_wait(bar0 + 8 * s, (seq / ST) & 1)) bad = true;
+            if (!bad && !mbar_wait(bar0 + 8 * s, (seq / ST) & 1)) {
+                bad = true;  // no more copies; those under way are waited for before the end
+                mbar_drain<ST>(bar0, seq);
+            }
             const uint8_t *kt = ringp + s * C::STAGE, *vt = kt + FKT * RB;
             const int j0 = kv4_tile<FKT>(key, (cur.x0 + y) * FW + warp);
             float S[NT][2][4];

@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 const int top = min(seg.x1, seg.key.tiles), end = seg.key.P + seg.key.cnt;
                 int ahead = seg.x0 + 1;
 #pragma unroll 1
-                for (int y = seg.x0; y < top; ++y) {
+                for (int y = seg.x0; y < top && !bad; ++y) {
                     for (; ahead < min(top, y + AHEAD); ++ahead) {
                         const int j0 = kv4_tile<MKT>(seg.key, ahead);
                         const uint32_t bytes = min(MKT, end - j0) * C::RB;
@@ -601,11 +601,15 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     for (int v = 0; v < 2; ++v, ++step) {
                         const uint32_t rs = step % C::NR;
                         wait(b_rfree + 8 * rs, step / C::NR + 1);
+                        if (bad) break;
                         mbar_expect(b_rfull + 8 * rs, in ? bytes : 0);
                         if (in) bulk_load(raw0 + rs * C::RAW, (v ? vb : kb) + off, bytes, b_rfull + 8 * rs);
                     }
                 }
-            } while (seg.next(a, R, RT));
+            } while (!bad && seg.next(a, R, RT));
+            // no copy is under way when the CTA ends, also after a wait that gave up
+            for (uint32_t z = step > C::NR ? step - C::NR : 0; z < step; ++z)
+                if (!mbar_wait(b_rfull + 8 * (z % C::NR), (z / C::NR) & 1)) bad = true;
         }
     } else {
         // -- products: the whole warp goes along, so that addresses stay in uniform
