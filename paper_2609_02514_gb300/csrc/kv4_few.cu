@@ -32,6 +32,27 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     return d;
 }
 
+// -- clusters -----------------------------------------------------------------
+constexpr int FCL = 8;  // CTAs of one, at most
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_map(uint32_t addr, int rank) {  // the same place in another CTA
+    uint32_t d;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
+    return d;
+}
+__device__ __forceinline__ float cluster_ld(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
 // A wait that gave up: the ring's other copies (a place without one costs as long a wait)
 template <int ST>
 static __device__ __noinline__ void mbar_drain(uint32_t bar0, int seq) {
@@ -62,8 +83,17 @@ struct Few {
 // channels of neighbouring keys: channels and keys come in whatever order the
 // words have, the same in both operands.  P' needs its pairs along the keys,
 // where S' has them along the rows: movmatrix turns the 8 x 8 blocks.
+// bfloat16 weights are rounded for their product; float32 queries and weights are
+// three bfloat16 parts each, all 24 bits.
+//
+// What bounds it is the codes' way into operands: some 780 warp instructions 32 keys
+// of 128, 60 of 100 issue slots taken.  One token, 32 heads over 8: 32 sequences of
+// 32768 positions 260 us, 5.16 TB/s; 64 of 200 to 8191 88 us, 4.0; one of 131071
+// 48 us, 3.5.  The rest of the shorter ones is a CTA's start (3 us: its share, its
+// first copies), its warps' merge (2.5 us an item) and the join.  mma.sync and not
+// the tcgen05 kernel: its rows are padded to 128 (the rule in kv4_abi.cu).
 template <int D, bool F32, int NT>
-__global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT, int direct) {
+__global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT, int CL) {
     using C = Few<D, F32, NT>;
     constexpr int RB = C::RB, R = C::R, KS = C::KS, JT = C::JT, WPT = C::WPT, ST = C::ST, SPL = C::SPL;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -80,15 +110,18 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (lane == 0)
         for (int s = 0; s < ST; ++s) mbar_init(bar0 + 8 * s, 1);
     if (tid == 0) any_timeout = 0;
+    const bool direct = CL > 0;  // clusters of CL CTAs an item, else shares
     if (!direct) pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
     using Seg = Kv4Seg<FKT, FW, FewCost>;
-    const Kv4Start at = direct ? kv4_whole<FKT, FW, FewCost>(a, R, RT) : kv4_start<FKT, FW, FewCost, FT>(a, R, RT);
+    const Kv4Start at = direct ? kv4_whole<FKT, FW, FewCost>(a, R, RT, CL) : kv4_start<FKT, FW, FewCost, FT>(a, R, RT);
     if (tid == 0 && !direct) kv4_put_info<FewCost>(ws, at);
     __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
     if (!cur.start(a, R, RT, at)) return;
+    const int rank = CL > 1 ? blockIdx.x % CL : 0;
+    if (CL > 1) cur.x0 = cur.key.units * rank / CL, cur.x1 = cur.key.units * (rank + 1) / CL;
 
     int seq = 0;       // tiles this warp has taken, of all segments
     bool bad = false;  // a wait gave up
@@ -380,7 +413,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
             if (y + ST < mine) issue(cur, y + ST, seq + ST);
         }
         // the next segment, whose first tiles are on their way while this one is merged
-        const bool whole = cur.whole();
+        const bool whole = CL <= 1 && cur.whole();
         const bool more = cur.next(a, R, RT);
         mine = more ? my_tiles(cur) : 0;
         if (more) {
@@ -401,7 +434,8 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
             }
         if (bad && lane == 0) any_timeout = 1;
         __syncthreads();
-        float *slot = ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
+        // (a cluster's parts stay in the rings, whose tiles are all used)
+        float *slot = CL > 1 ? reinterpret_cast<float *>(smem) : ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float M[2], L[2];
@@ -459,6 +493,48 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         first = false;
         info ^= 1;
         if (!more) break;
+    }
+    if (CL > 1) {  // the cluster's parts, in their order
+        constexpr int D4 = D / 4;
+        cluster_sync();
+        const int e = rank * FT + tid, row = e / D4, d4 = e % D4;
+        if (row < R) {
+            const uint32_t box = smem_u32(smem);
+            float4 v[FCL];
+            float m[FCL], l[FCL], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int c = 0; c < FCL; ++c) {
+                m[c] = -INFINITY, l[c] = 0.0f;
+                if (c >= CL) continue;
+                const uint32_t at_c = cluster_map(box, c);
+                m[c] = cluster_ld(at_c + 4 * (R * D + row)), l[c] = cluster_ld(at_c + 4 * (R * D + R + row));
+                v[c] = cluster_ld4(at_c + 16 * (row * D4 + d4));
+            }
+#pragma unroll
+            for (int c = 0; c < FCL; ++c) top = fmaxf(top, m[c]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int c = 0; c < FCL; ++c) {
+                if (c >= CL) continue;
+                const float f = ex2(m[c] - ref);
+                sum = fmaf(l[c], f, sum);
+                o.x = fmaf(v[c].x, f, o.x), o.y = fmaf(v[c].y, f, o.y), o.z = fmaf(v[c].z, f, o.z), o.w = fmaf(v[c].w, f, o.w);
+            }
+            const int r = at.rt * R + row, i = r / a.G;
+            if (r < a.n * a.G) {
+                const bool none = sum == 0.0f || rowinfo[0][row].x < 0;
+                const float k = none ? 0.0f : KV4_STEP / sum;
+                const size_t orow = ((size_t)at.b * a.n + i) * a.Hq + at.h * a.G + r % a.G;
+                if (none) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (F32)
+                    reinterpret_cast<float4 *>(a.out)[orow * D4 + d4] = make_float4(o.x * k, o.y * k, o.z * k, o.w * k);
+                else
+                    reinterpret_cast<uint2 *>(a.out)[orow * D4 + d4] = make_uint2(bf2_pack(o.x * k, o.y * k), bf2_pack(o.z * k, o.w * k));
+                if (d4 == 0 && a.lse) a.lse[orow] = none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+            }
+        }
+        cluster_sync();  // nobody leaves while its part is read
     }
     if (tid == 0 && any_timeout) {
         if (direct)
@@ -622,19 +698,39 @@ cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cuda
     return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
 
+// CTAs of a cluster that has an item to itself, or 0: shares and a join.  Clusters
+// while there is an SM for each of their CTAs (beyond, two on an SM take longer: four
+// sequences of 4000 positions, eight key heads, by fours 18.5 us, by eights 20.5) and
+// no CTA has more than KV4_DIRECT units, by the cache's or the window's length.
+// Against shares (us, eight key heads of 128): one sequence of 1000 positions 12.4 /
+// 14.3, of 4000 14.8 / 16.4, of 8000 16.9 / 20.5, of 16000 22.6 / 24.6 (by eights);
+// four of 8000 22.7 / 27.6 (by fours); 16 of 1000 18.4 / 24.6, of 2000 22.7 / 30.7 (one
+// CTA each).
+static int few_cluster(long long items, int most, int nsm) {
+    int cl = 1;
+    while (cl < FCL && cl < most && items * cl * 2 <= nsm) cl *= 2;
+    return items < (1ll << 30) && (most + cl - 1) / cl <= KV4_DIRECT ? cl : 0;
+}
+
 template <int D, bool F32, int NT>
 static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
     using C = Few<D, F32, NT>;
     const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
     const long long items = (long long)a.B * RT * a.H;
-    const bool direct = kv4_most_units(a, FW * FKT) <= KV4_DIRECT && items < (1ll << 30);
-    const int grid = direct ? (int)items : nsm * C::MINB;
+    const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, nsm);
+    const bool direct = CL > 0;
+    const int grid = direct ? (int)items * CL : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);
     static std::atomic<unsigned long long> allowed{0};
     cudaError_t e = allow_smem(k_kv4_few<D, F32, NT>, C::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    k_kv4_few<D, F32, NT><<<grid, FT, C::SMEM, s>>>(a, ws, RT, direct);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(FT), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = s;
+    cudaLaunchAttribute shape;
+    shape.id = cudaLaunchAttributeClusterDimension;
+    shape.val.clusterDim.x = direct ? CL : 1, shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
+    cfg.attrs = &shape, cfg.numAttrs = CL > 1 ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, k_kv4_few<D, F32, NT>, a, ws, RT, CL);
     return e != cudaSuccess || direct ? e : launch_kv4_join(a, ws, grid, C::R, s);
 }
 

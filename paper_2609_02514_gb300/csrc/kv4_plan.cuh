@@ -13,10 +13,9 @@
 // one CTA's range is written out by it; the pieces of one that several share go
 // to the workspace as sums not yet divided, with their reference maximum, and
 // k_kv4_join adds them in the CTAs' order.
-// Where no item can have more than KV4_DIRECT units (the cache is short, or the
-// window), each is one CTA's, and there is nothing to join (the few-row kernel;
-// measured at 1000 keys, with / without a split: 16 sequences of eight key heads
-// 25 / 17 us, 64 41 / 39; at 4000 keys one sequence 16 / 31).
+// Where no item can have more than KV4_DIRECT units for each CTA of a cluster (the
+// cache is short, or the window), a cluster takes it and adds its parts up in
+// shared memory: nothing to join (few rows only: few_cluster() and its figures).
 #pragma once
 #include <atomic>
 
@@ -151,17 +150,17 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     return s;
 }
 
-// Without a split: a CTA has the whole item.
+// Without shares: a cluster of CL CTAs has the whole item.
 template <int KT, int TPU, class Cost>
-__device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT) {
+__device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, int CL) {
     Kv4Start s;
-    const int e = blockIdx.x / a.H;
-    s.h = blockIdx.x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
+    const int x = blockIdx.x / CL, e = x / a.H;
+    s.h = x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
     s.off = 0;
     s.key = kv4_keys<KT, TPU>(a, R, s.b, s.rt);
     s.left = s.quantum = Cost::all(s.key);
     s.cnt = s.key.cnt;
-    if (threadIdx.x == 0 && s.h == 0 && s.rt == 0)
+    if (threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
         a.status[s.b] = kv4_seq(a.prefix, a.count, s.b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
     return s;
 }
