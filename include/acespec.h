@@ -69,8 +69,9 @@ typedef enum { ACES_F32 = 0, ACES_BF16 = 1 } aces_dtype;
 /* bits of row_status */
 #define ACES_ROW_NONFINITE 1 /* NaN / +inf logits, or all logits -inf      */
 #define ACES_ROW_BAD_Q 2     /* invalid draft probability or draft token   */
-#define ACES_ROW_TIMEOUT 4   /* reserved for a kernel that gives up a bounded
-                                wait; no current kernel waits on another */
+#define ACES_ROW_TIMEOUT 4   /* a wait for a kernel's own copies or products
+                                gave up after seconds (aces_kv4_attention):
+                                the results are not valid                */
 #define ACES_ROW_RANGE 8     /* positions outside the cache (aces_kv4_*)   */
 
 /* The CUDA runtime's cudaStream_t (NULL = legacy default stream). */
@@ -440,7 +441,7 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *                 k); -inf for those
  *   seq_status    [B] int32: ACES_ROW_RANGE where prefix_len or count is
  *                 negative, count above n, or prefix + count above S (the
- *                 sequence's tokens count as padding)
+ *                 sequence's tokens count as padding); ACES_ROW_TIMEOUT
  * Products are those of the cache's numbers and q's as they are, sums float32.
  * Weights are rounded to bfloat16 before they meet the values when q is
  * bfloat16, and are float32 when it is.

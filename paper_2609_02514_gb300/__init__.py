@@ -25,7 +25,7 @@ import torch
 
 __all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
            "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
-           "ROW_NONFINITE", "ROW_BAD_Q", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
+           "ROW_NONFINITE", "ROW_BAD_Q", "ROW_TIMEOUT", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libacespec.so")
@@ -40,6 +40,7 @@ COUNTERS_OFFSET = 256
 
 ROW_NONFINITE = 1
 ROW_BAD_Q = 2
+ROW_TIMEOUT = 4
 ROW_RANGE = 8
 ACES_F32 = 0
 ACES_BF16 = 1
@@ -538,7 +539,8 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
     above its own minus window, and those below sinks.  Tokens i >= count[b]
     are padding.  scale: 1 / sqrt(D) unless given.  Returns a dict of out
     [B, n, Hq, D], lse [B, n, Hq] and status [B] (ROW_RANGE: a sequence whose
-    tokens do not lie in the cache).
+    tokens do not lie in the cache; ROW_TIMEOUT: a wait in the kernel gave up,
+    the results are not valid).
     """
     lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
     stream = _stream(dev)
