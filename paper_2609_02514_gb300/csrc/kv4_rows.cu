@@ -8,7 +8,7 @@
 // and 5/8 (D = 128) or 3/4 of a byte each on the other.  Reading does so at 6.4
 // TB/s (704.6 MB in 109.9 us).  Writing one to two thousand tokens a sequence is one
 // or two waves of CTAs, and its time is their start, one load's way from memory and
-// back, and 17 (bfloat16) to 38 (float32) instructions a number: 48.5 MB in 11.5 us,
+// back, and 18 (bfloat16) to 43 (float32) instructions a number: 48.5 MB in 11.5 us,
 // half the issue slots taken while CTAs run.
 #define ACES_FILE 7  // site numbers of the checked build
 #include "kv4.cuh"
