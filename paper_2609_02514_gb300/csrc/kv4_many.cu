@@ -40,6 +40,7 @@
 #include <cuda_bf16.h>
 
 #include "kv4_plan.cuh"
+#include "warp_wait.cuh"
 
 namespace aces {
 
@@ -631,9 +632,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         const bool leader = elect_one();
         auto go = [&](uint32_t bar, uint32_t phase) {  // wait(), with one answer for the warp
             if (bad) return;
-            for (int t = 0; t < 16; ++t)
-                if (mbar_try(bar, phase & 1)) return;
-            bad = !__all_sync(0xffffffffu, mbar_wait_slow(bar, phase & 1));
+            bad = !warp_wait([&] { return mbar_try(bar, phase & 1); }, [&] { return mbar_wait_slow(bar, phase & 1); },
+                             [](bool ok) { return (bool)__all_sync(0xffffffffu, ok); });
         };
         uint32_t n = 0, segs = 0, n0 = 0, n1 = 0;  // tiles, segments and each group's tiles so far
         do {
