@@ -336,8 +336,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             const int all_see = a.mask || !warp_live ? P : P + imin + 1;
             const int T = min(seg.x1, key.tiles) - seg.x0;  // 0 for an item without keys
             const int mine = 2 * (single ? (T + 1 - x) >> 1 : T);  // of 64 keys
-            // queries (a row without one reads the first token's and keeps zeros)
-            {
+            // Queries (a row without one reads the first token's and keeps zeros), where the
+            // group has tiles: it then waits for their products below.  For a segment without
+            // any (padding) it waits for nothing, and words for two of those could both be
+            // there before the issuing warp looks: it would take the second for none.
+            if (mine > 0) {
                 const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + b * a.qb + (row_live ? i : 0) * a.qi +
                                           (long long)(h * a.G + (row_live ? gq : 0)) * a.qh;
                 const uint32_t keep = row_live ? 0xFFFFFFFFu : 0u;
@@ -363,11 +366,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                         *reinterpret_cast<uint4 *>(myq + swz(row, c)) = make_uint4(u[0], u[1], u[2], u[3]);
                     }
                 }
+                async_fence();
+                tc_before();  // the last segment's sums are read
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_q + 8 * x);
             }
-            async_fence();
-            tc_before();  // the last segment's sums are read
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_q + 8 * x);
             float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
 #pragma unroll 1
             for (int y = 0; y < mine; ++y) {
@@ -635,13 +638,13 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             bad = !warp_wait([&] { return mbar_try(bar, phase & 1); }, [&] { return mbar_wait_slow(bar, phase & 1); },
                              [](bool ok) { return (bool)__all_sync(0xffffffffu, ok); });
         };
-        uint32_t n = 0, segs = 0, n0 = 0, n1 = 0;  // tiles, segments and each group's tiles so far
+        uint32_t n = 0, n0 = 0, n1 = 0, q0s = 0, q1s = 0;  // tiles, each group's tiles and its queries so far
         do {
             const bool single = NR - seg.rt * R <= 128;
             const int T = __shfl_sync(0xffffffffu, min(seg.x1, seg.key.tiles) - seg.x0, 0);
             const int cnt0 = single ? (T + 1) >> 1 : T, cnt1 = single ? T >> 1 : T;
-            go(b_q, segs);
-            go(b_q + 8, segs);
+            if (cnt0 > 0) go(b_q, q0s++);
+            if (cnt1 > 0) go(b_q + 8, q1s++);
             // each group in turn: the values of its tile i, then the scores of i + 1
 #pragma unroll 1
             for (int u = -2; u < 2 * cnt0 && !bad; ++u) {
@@ -687,7 +690,6 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             }
             n += max(T, 0);
             n0 += max(cnt0, 0), n1 += max(cnt1, 0);
-            ++segs;
         } while (seg.next(a, R, RT));
         if (leader) tc_commit(b_end);  // nothing runs on when the columns are given back
         if (!mbar_wait(b_end, 0)) bad = true;
