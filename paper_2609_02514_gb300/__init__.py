@@ -173,8 +173,16 @@ def _ptr(o, key):
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream(dev) -> int:
-    """The current CUDA stream of the device."""
+    """The current CUDA stream of the device, which has to be the current one: the
+    library launches there, whichever GPU the pointers and the stream belong to
+    (every device's default stream has the same handle)."""
+    if dev.index is not None and dev.index != _current_device():
+        raise ValueError(f"the tensors are on {dev}, but cuda:{_current_device()} is the current device: "
+                         f"call under torch.cuda.device({dev.index})")
     if _raw_stream is not None and dev.index is not None:
         return _raw_stream(dev.index)
     return torch.cuda.current_stream(dev).cuda_stream
