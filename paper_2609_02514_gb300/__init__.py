@@ -138,7 +138,8 @@ def _open(path):
               lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention):
         f.restype = I
     # what the native half of the binding calls
-    lib.kv4_entries = tuple(ctypes.cast(f, P).value for f in (lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention))
+    lib.kv4_entries = tuple(ctypes.cast(f, P).value for f in (lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention,
+                                                                  lib.aces_kv4_workspace_bytes))
     if hasattr(lib, "aces_checked_violation"):
         lib.aces_checked_violation.argtypes = [P]
         lib.aces_checked_violation.restype = I
@@ -447,7 +448,6 @@ def tree_mask(F, branch_len: int, device=None):
 
 # The 4-bit cache's calls check their arguments, allocate and launch in the native
 # half of the binding (csrc/binding.cpp).
-_U8 = torch.uint8
 _native_module = None
 
 
@@ -505,37 +505,6 @@ def kv4_workspace_bytes(B: int, n: int, Hq: int, H: int, D: int) -> int:
     return int(load().aces_kv4_workspace_bytes(int(B), int(n), int(Hq), int(H), int(D)))
 
 
-_kv4_sizes = {}                # workspace bytes by shape
-_kv4_kept = threading.local()  # .ws: (address, bytes, tensor) by device and stream
-
-
-def _kv4_scratch(q, cache, dev, stream):
-    """Address and bytes of the workspace that this thread keeps for a stream: its
-    calls there come one after another.  (An allocation and its release take 3 us
-    of the host.)  A call that is being captured gets one of its own."""
-    key = (q.shape, cache.shape, dev)
-    need = _kv4_sizes.get(key)
-    if need is None:
-        if q.dim() != 4 or cache.dim() != 5:
-            return 0, 0, None  # refused by the call
-        _, n, Hq, D = q.shape
-        if len(_kv4_sizes) > 1000:
-            _kv4_sizes.clear()
-        need = _kv4_sizes[key] = max(kv4_workspace_bytes(cache.shape[1], n, Hq, cache.shape[2], D), 16)
-    if torch.cuda.is_current_stream_capturing():
-        ws = _empty(need, dtype=_U8, device=dev)
-        return ws.data_ptr(), need, ws
-    try:
-        kept = _kv4_kept.ws
-    except AttributeError:
-        kept = _kv4_kept.ws = {}
-    ws = kept.get((dev, stream))
-    if ws is None or ws[1] < need:
-        t = _empty(need, dtype=_U8, device=dev)
-        ws = kept[(dev, stream)] = (t.data_ptr(), need, t)
-    return ws
-
-
 def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count=None, scale: float | None = None,
                   window: int = 0, sinks: int = 0, out: dict | None = None, workspace: torch.Tensor | None = None):
     """Attention of q [B, n, Hq, D] over the layer's cache, whose positions
@@ -549,20 +518,16 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
     [B, n, Hq, D], lse [B, n, Hq] and status [B] (ROW_RANGE: a sequence whose
     tokens do not lie in the cache; ROW_TIMEOUT: a wait in the kernel gave up,
     the results are not valid).
+
+    The workspace (kv4_workspace_bytes(), up to 41 MB) is allocated for the call on
+    its stream and given back behind it, unless one is given: that one has to be on
+    the cache's device, contiguous, large enough and no other call's meanwhile.
     """
     lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
-    stream = _stream(dev)
-    if workspace is None:
-        wp, nbytes, _ = _kv4_scratch(q, cache, dev, stream)
-    else:
-        ws = _cuda(workspace, "workspace")
-        wp, nbytes = ws.data_ptr(), ws.numel() * ws.element_size()
-        if ws.device != dev:
-            raise ValueError(f"workspace must be on {dev}")
     o = {} if out is None else dict(out)
     code, o["out"], o["lse"], o["status"] = native.attention(
-        lib.kv4_entries[2], q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, o.get("out"), o.get("lse"),
-        o.get("status"), wp, nbytes, stream)
+        lib.kv4_entries[2], lib.kv4_entries[3], q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, o.get("out"),
+        o.get("lse"), o.get("status"), workspace, _stream(dev))
     if code != 0:
         _check("aces_kv4_attention", code)
     return o

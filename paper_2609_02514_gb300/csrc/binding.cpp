@@ -9,6 +9,7 @@
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <string>
@@ -107,6 +108,7 @@ PyObject *guarded(Py_ssize_t have, Py_ssize_t want, F f) {
 using Append = decltype(&aces_kv4_append);
 using Read = decltype(&aces_kv4_read);
 using Attention = decltype(&aces_kv4_attention);
+using Bytes = decltype(&aces_kv4_workspace_bytes);
 
 // append(entry, cache, layer, k, v, start, count, out, stream) -> (status code, row_status)
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
@@ -168,48 +170,59 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     });
 }
 
-// attention(entry, q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, out, lse, status, workspace, bytes,
-//           stream) -> (status code, out, lse, status)
+// attention(entry, workspace_bytes, q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, out, lse, status,
+//           workspace, stream) -> (status code, out, lse, status)
 PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     return guarded(n_args, 17, [&]() -> PyObject * {
-        const Cache c = cache_of(a[2]);
+        const Cache c = cache_of(a[3]);
         int64_t qs[3];
-        const Tensor &q = rows(a[1], "q", c, qs);
+        const Tensor &q = rows(a[2], "q", c, qs);
         const int n = (int)q.size(1), Hq = (int)q.size(2), words = (n + 31) / 32;
-        const void *prefix = dense(a[4], "prefix_len", {c.B}, at::kInt, c.t);
+        const void *prefix = dense(a[5], "prefix_len", {c.B}, at::kInt, c.t);
         const void *mask = nullptr, *depth = nullptr;
         int64_t ms = 0, ds = 0;
-        if ((a[5] == Py_None) != (a[6] == Py_None)) throw Refusal{"mask and depth go together"};
-        if (a[5] != Py_None) {
-            if (cuda(a[5], "mask").dim() == 3)
-                mask = dense(a[5], "mask", {c.B, n, words}, at::kInt, c.t), ms = (int64_t)n * words;
+        if ((a[6] == Py_None) != (a[7] == Py_None)) throw Refusal{"mask and depth go together"};
+        if (a[6] != Py_None) {
+            if (cuda(a[6], "mask").dim() == 3)
+                mask = dense(a[6], "mask", {c.B, n, words}, at::kInt, c.t), ms = (int64_t)n * words;
             else
-                mask = dense(a[5], "mask", {n, words}, at::kInt, c.t);
-            if (cuda(a[6], "depth").dim() == 2)
-                depth = dense(a[6], "depth", {c.B, n}, at::kInt, c.t), ds = n;
+                mask = dense(a[6], "mask", {n, words}, at::kInt, c.t);
+            if (cuda(a[7], "depth").dim() == 2)
+                depth = dense(a[7], "depth", {c.B, n}, at::kInt, c.t), ds = n;
             else
-                depth = dense(a[6], "depth", {n}, at::kInt, c.t);
+                depth = dense(a[7], "depth", {n}, at::kInt, c.t);
         }
-        const void *count = a[7] == Py_None ? nullptr : dense(a[7], "count", {c.B}, at::kInt, c.t);
+        const void *count = a[8] == Py_None ? nullptr : dense(a[8], "count", {c.B}, at::kInt, c.t);
         double scale = 1.0 / std::sqrt((double)(c.D > 0 ? c.D : 1));
-        if (a[8] != Py_None) {
-            scale = PyFloat_AsDouble(a[8]);
+        if (a[9] != Py_None) {
+            scale = PyFloat_AsDouble(a[9]);
             if (scale == -1.0 && PyErr_Occurred()) throw Refusal{""};
         }
         const Shape full{c.B, n, Hq, c.D}, row{c.B, n, Hq}, one{c.B};
         void *p[3] = {nullptr, nullptr, nullptr};
-        if (a[11] != Py_None) p[0] = dense(a[11], "out", full, q.scalar_type(), c.t);
-        if (a[12] != Py_None) p[1] = dense(a[12], "lse", row, at::kFloat, c.t);
-        if (a[13] != Py_None) p[2] = dense(a[13], "status", one, at::kInt, c.t);
-        const int layer = integer(a[3], "layer"), window = integer(a[9], "window"), sinks = integer(a[10], "sinks");
+        if (a[12] != Py_None) p[0] = dense(a[12], "out", full, q.scalar_type(), c.t);
+        if (a[13] != Py_None) p[1] = dense(a[13], "lse", row, at::kFloat, c.t);
+        if (a[14] != Py_None) p[2] = dense(a[14], "status", one, at::kInt, c.t);
+        const int layer = integer(a[4], "layer"), window = integer(a[10], "window"), sinks = integer(a[11], "sinks");
         const auto entry = reinterpret_cast<Attention>(address(a[0]));
         const auto stream = (aces_stream_t)address(a[16]);
-        void *ws = address(a[14]);
-        const size_t bytes = (size_t)whole(a[15]);
+        // The workspace is the call's own: given back on return, it is only used again
+        // behind the call's work on this stream.
+        Tensor scratch;
+        if (a[15] == Py_None) {
+            const size_t need = reinterpret_cast<Bytes>(address(a[1]))(c.B, n, Hq, c.H, c.D);
+            scratch = at::empty({(int64_t)std::max<size_t>(need, 16)}, c.t.options());
+        } else {
+            scratch = cuda(a[15], "workspace");
+            if (!scratch.is_contiguous() || scratch.device() != c.t.device())
+                throw Refusal{"workspace must be contiguous and on " + c.t.device().str()};
+        }
+        void *ws = scratch.data_ptr();
+        const size_t bytes = scratch.nbytes();
         PyObject *out[3];
         for (int x = 0; x < 3; ++x) {
-            if (a[11 + x] != Py_None) {
-                out[x] = a[11 + x];
+            if (a[12 + x] != Py_None) {
+                out[x] = a[12 + x];
                 Py_INCREF(out[x]);
                 continue;
             }
