@@ -7,6 +7,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -86,7 +87,26 @@ int integer(PyObject *o, const char *name) {
 }
 void *address(PyObject *o) { return reinterpret_cast<void *>((uintptr_t)whole(o)); }
 
-PyObject *wrap(const Tensor &t) { return THPVariable_Wrap(t); }
+// One output: the caller's object, or a tensor made here, which only becomes an object
+// on the way back to Python, so that what fails in between gives it back.
+struct Output {
+    PyObject *given = nullptr;
+    Tensor made;
+    void *p = nullptr;
+    void take(PyObject *o, const char *name, Shape shape, at::ScalarType type, const Tensor &cache) {
+        if (o != Py_None) given = o, p = dense(o, name, shape, type, cache);
+    }
+    void make(Shape shape, at::ScalarType type, const Tensor &cache) {
+        if (given) return;
+        made = at::empty(shape, cache.options().dtype(type));
+        p = made.data_ptr();
+    }
+    PyObject *object() const {
+        if (!given) return THPVariable_Wrap(made);
+        Py_INCREF(given);
+        return given;
+    }
+};
 
 // Runs f, and turns what it throws into a Python error.
 template <typename F>
@@ -99,8 +119,8 @@ PyObject *guarded(Py_ssize_t have, Py_ssize_t want, F f) {
         return f();
     } catch (const Refusal &r) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, r.why.c_str());
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {  // torch's own kinds stay what they are (out of memory, for one)
+        torch::translate_exception_to_python(std::current_exception());
     }
     return nullptr;
 }
@@ -123,19 +143,12 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         const auto stream = (aces_stream_t)address(a[8]);
         const void *start = dense(a[5], "start", {c.B}, at::kInt, c.t);
         const void *count = a[6] == Py_None ? nullptr : dense(a[6], "count", {c.B}, at::kInt, c.t);
-        PyObject *out = a[7];
-        void *st;
-        if (out == Py_None) {
-            const Tensor t = at::empty({c.B, n}, c.t.options().dtype(at::kInt));
-            st = t.data_ptr();
-            out = wrap(t);
-        } else {
-            st = dense(out, "out", {c.B, n}, at::kInt, c.t);
-            Py_INCREF(out);
-        }
+        Output st;
+        st.take(a[7], "out", {c.B, n}, at::kInt, c.t);
+        st.make({c.B, n}, at::kInt, c.t);
         const aces_status s = entry(c.t.data_ptr(), c.planes, layer, c.B, c.H, c.S, c.D, k.data_ptr(), v.data_ptr(), code(k.scalar_type()), ks,
-                                    vs, (const int32_t *)start, (const int32_t *)count, n, (int32_t *)st, stream);
-        return Py_BuildValue("(iN)", (int)s, out);
+                                    vs, (const int32_t *)start, (const int32_t *)count, n, (int32_t *)st.p, stream);
+        return Py_BuildValue("(iN)", (int)s, st.object());
     });
 }
 
@@ -149,24 +162,12 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         const at::ScalarType type = a[5] == Py_True ? at::kFloat : at::kBFloat16;
         const void *start = dense(a[3], "start", {c.B}, at::kInt, c.t);
         if (n < 1) return Py_BuildValue("(iOO)", (int)ACES_ERR_INVALID_ARG, Py_None, Py_None);
-        PyObject *out[2];
-        void *p[2];
-        for (int x = 0; x < 2; ++x) {
-            if (a[6 + x] == Py_None) continue;
-            p[x] = dense(a[6 + x], x ? "v" : "k", {c.B, n, c.H, c.D}, type, c.t);
-        }
-        for (int x = 0; x < 2; ++x) {
-            if (a[6 + x] != Py_None) {
-                out[x] = a[6 + x];
-                Py_INCREF(out[x]);
-                continue;
-            }
-            const Tensor t = at::empty({c.B, n, c.H, c.D}, c.t.options().dtype(type));
-            p[x] = t.data_ptr();
-            out[x] = wrap(t);
-        }
-        const aces_status s = entry(c.t.data_ptr(), c.planes, layer, c.B, c.H, c.S, c.D, (const int32_t *)start, n, p[0], p[1], code(type), stream);
-        return Py_BuildValue("(iNN)", (int)s, out[0], out[1]);
+        Output out[2];
+        for (int x = 0; x < 2; ++x) out[x].take(a[6 + x], x ? "v" : "k", {c.B, n, c.H, c.D}, type, c.t);
+        for (int x = 0; x < 2; ++x) out[x].make({c.B, n, c.H, c.D}, type, c.t);
+        const aces_status s = entry(c.t.data_ptr(), c.planes, layer, c.B, c.H, c.S, c.D, (const int32_t *)start, n, out[0].p, out[1].p, code(type),
+                                    stream);
+        return Py_BuildValue("(iNN)", (int)s, out[0].object(), out[1].object());
     });
 }
 
@@ -199,10 +200,10 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
             if (scale == -1.0 && PyErr_Occurred()) throw Refusal{""};
         }
         const Shape full{c.B, n, Hq, c.D}, row{c.B, n, Hq}, one{c.B};
-        void *p[3] = {nullptr, nullptr, nullptr};
-        if (a[12] != Py_None) p[0] = dense(a[12], "out", full, q.scalar_type(), c.t);
-        if (a[13] != Py_None) p[1] = dense(a[13], "lse", row, at::kFloat, c.t);
-        if (a[14] != Py_None) p[2] = dense(a[14], "status", one, at::kInt, c.t);
+        Output out, lse, status;
+        out.take(a[12], "out", full, q.scalar_type(), c.t);
+        lse.take(a[13], "lse", row, at::kFloat, c.t);
+        status.take(a[14], "status", one, at::kInt, c.t);
         const int layer = integer(a[4], "layer"), window = integer(a[10], "window"), sinks = integer(a[11], "sinks");
         const auto entry = reinterpret_cast<Attention>(address(a[0]));
         const auto stream = (aces_stream_t)address(a[16]);
@@ -219,23 +220,14 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         }
         void *ws = scratch.data_ptr();
         const size_t bytes = scratch.nbytes();
-        PyObject *out[3];
-        for (int x = 0; x < 3; ++x) {
-            if (a[12 + x] != Py_None) {
-                out[x] = a[12 + x];
-                Py_INCREF(out[x]);
-                continue;
-            }
-            const Tensor t = at::empty(x == 0 ? full : x == 1 ? row : one,
-                                       c.t.options().dtype(x == 0 ? q.scalar_type() : x == 1 ? at::kFloat : at::kInt));
-            p[x] = t.data_ptr();
-            out[x] = wrap(t);
-        }
+        out.make(full, q.scalar_type(), c.t);
+        lse.make(row, at::kFloat, c.t);
+        status.make(one, at::kInt, c.t);
         const aces_status s = entry(
             q.data_ptr(), code(q.scalar_type()), qs, c.t.data_ptr(), c.planes, layer, c.B, n, Hq, c.H, c.S, c.D, (const int32_t *)prefix,
-            (const int32_t *)count, (const uint32_t *)mask, ms, (const int32_t *)depth, ds, (float)scale, window, sinks, p[0], (float *)p[1],
-            (int32_t *)p[2], ws, bytes, stream);
-        return Py_BuildValue("(iNNN)", (int)s, out[0], out[1], out[2]);
+            (const int32_t *)count, (const uint32_t *)mask, ms, (const int32_t *)depth, ds, (float)scale, window, sinks, out.p, (float *)lse.p,
+            (int32_t *)status.p, ws, bytes, stream);
+        return Py_BuildValue("(iNNN)", (int)s, out.object(), lse.object(), status.object());
     });
 }
 
