@@ -6,7 +6,8 @@ the library is newer than every source.  build(checked=True) makes the
 checked test build instead, libacespec_checked.so (-DACES_CHECKED: every
 kernel records out-of-range indices instead of using them).
 The native half of the Python binding (csrc/binding.cpp, against torch's
-headers) is compiled alongside with the host compiler, into _binding.so.
+headers) is compiled alongside with the host compiler, into _binding.so, where
+there are torch, Python's headers and a C++ compiler.
 """
 from __future__ import annotations
 
@@ -50,27 +51,43 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
+def _binding_tools():
+    """(torch's directory, its ABI flag, Python's headers, the C++ compiler) for _binding.so, or the
+    reason why it cannot be built here."""
+    import sysconfig
+    try:
+        import torch
+    except Exception as e:  # not installed, or not loadable on this machine
+        return f"torch cannot be imported ({e})"
+    cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        return "no C++ compiler"
+    headers = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(headers, "Python.h")):
+        return f"no Python.h in {headers}"
+    return os.path.dirname(torch.__file__), int(torch.compiled_with_cxx11_abi()), headers, cxx
+
+
 def _start_binding(force: bool):
-    """The compiler at work on _binding.so (its command and process), or None when it is newer than its sources."""
+    """The compiler at work on _binding.so (its command and process), or None when it is newer than its
+    sources, or when it cannot be built here: a C caller needs libacespec.so alone."""
     deps = [BINDING_SRC, os.path.join(ROOT, "include", "acespec.h")]
     if not force and os.path.exists(BINDING) and all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in deps):
         return None
-    import sysconfig
-
-    import torch
-    cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
-    if cxx is None:
-        raise RuntimeError("g++ not found: a C++ compiler is required to build _binding.so")
-    base = os.path.dirname(torch.__file__)
-    inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           sysconfig.get_paths()["include"]]
-    cmd = [cxx, "-std=c++17", "-O1", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+    tools = _binding_tools()
+    if isinstance(tools, str):
+        print(f"{os.path.basename(BINDING)} (the Python calls of the 4-bit cache) is not built: {tools}", file=sys.stderr)
+        return None
+    base, abi, headers, cxx = tools
+    inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), headers]
+    cmd = [cxx, "-std=c++17", "-O1", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}"]
     cmd += [f"-I{i}" for i in inc] + ["-o", BINDING + f".tmp{os.getpid()}", BINDING_SRC, "-L" + os.path.join(base, "lib"),
                                       "-ltorch_python", "-ltorch_cpu", "-lc10"]
     return cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
 
 
 def _finish_binding(started) -> None:
+    """Waits for the compiler; an error of its own is raised when the library is there."""
     if started is None:
         return
     cmd, p = started
