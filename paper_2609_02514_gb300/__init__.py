@@ -454,11 +454,17 @@ _native_module = None
 def _native():
     global _native_module
     if _native_module is None:
+        import importlib.util
+        from . import build
+        path = build.binding_path(torch.__version__)
+        name = __name__ + "._binding"
         try:
-            from . import _binding
+            spec = importlib.util.spec_from_file_location(name, path)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
         except ImportError as e:
-            raise RuntimeError(f"_binding.so cannot be loaded ({e}): build it with `python -m paper_2609_02514_gb300.build`") from e
-        _native_module = _binding
+            raise RuntimeError(f"{path} cannot be loaded ({e}): build it with `python -m paper_2609_02514_gb300.build`") from e
+        _native_module = module
     return _native_module
 
 

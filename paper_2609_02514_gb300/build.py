@@ -6,8 +6,9 @@ the library is newer than every source.  build(checked=True) makes the
 checked test build instead, libacespec_checked.so (-DACES_CHECKED: every
 kernel records out-of-range indices instead of using them).
 The native half of the Python binding (csrc/binding.cpp, against torch's
-headers) is compiled alongside with the host compiler, into _binding.so, where
-there are torch, Python's headers and a C++ compiler.
+headers) is compiled alongside with the host compiler, into a file named
+after Python's and torch's versions, where there are torch, Python's headers
+and a C++ compiler.
 """
 from __future__ import annotations
 
@@ -23,9 +24,14 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libacespec.so")
 LIB_CHECKED = os.path.join(HERE, "libacespec_checked.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
+
+
+def binding_path(torch_version: str) -> str:
+    """The binding for this Python and a version of torch: built against one of each, it must not be
+    loaded by another."""
+    return os.path.join(HERE, f"_binding.{sys.implementation.cache_tag}.torch-{torch_version}.so")
 
 
 def _nvcc() -> str:
@@ -51,50 +57,45 @@ def up_to_date(lib: str = LIB) -> bool:
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
-def _binding_tools():
-    """(torch's directory, its ABI flag, Python's headers, the C++ compiler) for _binding.so, or the
-    reason why it cannot be built here."""
+def _no_binding(why: str) -> None:
+    print(f"the binding (the Python calls of the 4-bit cache) is not built: {why}", file=sys.stderr)
+
+
+def _start_binding(force: bool):
+    """The compiler at work on the binding (its command, process and result), or None when it is newer than
+    its sources, or when it cannot be built here: a C caller needs libacespec.so alone."""
     import sysconfig
     try:
         import torch
     except Exception as e:  # not installed, or not loadable on this machine
-        return f"torch cannot be imported ({e})"
+        return _no_binding(f"torch cannot be imported ({e})")
+    path = binding_path(torch.__version__)
+    deps = [BINDING_SRC, os.path.join(ROOT, "include", "acespec.h")]
+    if not force and os.path.exists(path) and all(os.path.getmtime(p) <= os.path.getmtime(path) for p in deps):
+        return None
     cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
     if cxx is None:
-        return "no C++ compiler"
+        return _no_binding("no C++ compiler")
     headers = sysconfig.get_paths()["include"]
     if not os.path.exists(os.path.join(headers, "Python.h")):
-        return f"no Python.h in {headers}"
-    return os.path.dirname(torch.__file__), int(torch.compiled_with_cxx11_abi()), headers, cxx
-
-
-def _start_binding(force: bool):
-    """The compiler at work on _binding.so (its command and process), or None when it is newer than its
-    sources, or when it cannot be built here: a C caller needs libacespec.so alone."""
-    deps = [BINDING_SRC, os.path.join(ROOT, "include", "acespec.h")]
-    if not force and os.path.exists(BINDING) and all(os.path.getmtime(p) <= os.path.getmtime(BINDING) for p in deps):
-        return None
-    tools = _binding_tools()
-    if isinstance(tools, str):
-        print(f"{os.path.basename(BINDING)} (the Python calls of the 4-bit cache) is not built: {tools}", file=sys.stderr)
-        return None
-    base, abi, headers, cxx = tools
+        return _no_binding(f"no Python.h in {headers}")
+    base, abi = os.path.dirname(torch.__file__), int(torch.compiled_with_cxx11_abi())
     inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), headers]
     cmd = [cxx, "-std=c++17", "-O1", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={abi}"]
-    cmd += [f"-I{i}" for i in inc] + ["-o", BINDING + f".tmp{os.getpid()}", BINDING_SRC, "-L" + os.path.join(base, "lib"),
+    cmd += [f"-I{i}" for i in inc] + ["-o", path + f".tmp{os.getpid()}", BINDING_SRC, "-L" + os.path.join(base, "lib"),
                                       "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    return cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    return cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT), path
 
 
 def _finish_binding(started) -> None:
     """Waits for the compiler; an error of its own is raised when the library is there."""
     if started is None:
         return
-    cmd, p = started
+    cmd, p, path = started
     out, _ = p.communicate()
     if p.returncode != 0:
         raise RuntimeError("the binding does not compile: " + " ".join(cmd) + "\n" + out.decode(errors="replace"))
-    os.replace(cmd[cmd.index("-o") + 1], BINDING)
+    os.replace(cmd[cmd.index("-o") + 1], path)
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:

@@ -15,7 +15,6 @@ def small(tmp_path, monkeypatch):
     src.write_text('extern "C" int one() { return 1; }\n')
     monkeypatch.setattr(b, "HERE", str(tmp_path))
     monkeypatch.setattr(b, "LIB", str(tmp_path / "libone.so"))
-    monkeypatch.setattr(b, "BINDING", str(tmp_path / "_binding.so"))
     monkeypatch.setattr(b, "_sources", lambda: [str(src)])
     return tmp_path
 
@@ -40,7 +39,7 @@ def _no_compiler(monkeypatch, tmp_path):
 def test_the_library_builds_without(small, monkeypatch, capfd, without):
     without(monkeypatch, small)
     assert b.build() == b.LIB and os.path.exists(b.LIB)
-    assert not os.path.exists(b.BINDING)
+    assert not list(small.glob("_binding*"))
     assert "is not built" in capfd.readouterr().err
 
 
@@ -51,4 +50,25 @@ def test_the_library_is_there_when_the_binding_does_not_compile(small, monkeypat
     monkeypatch.setattr(b, "BINDING_SRC", str(bad))
     with pytest.raises(RuntimeError, match="the binding does not compile"):
         b.build()
-    assert os.path.exists(b.LIB) and not os.path.exists(b.BINDING)
+    assert os.path.exists(b.LIB) and not list(small.glob("_binding*.so"))
+
+
+def test_a_binding_of_other_versions_is_not_loaded(monkeypatch):
+    torch = pytest.importorskip("torch")
+    import paper_2609_02514_gb300 as A
+    b.build()
+    monkeypatch.setattr(A, "_native_module", None)
+    assert A._native().__file__ == b.binding_path(torch.__version__)
+    monkeypatch.setattr(A, "_native_module", None)
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    with pytest.raises(RuntimeError, match="build it with"):
+        A._native()
+
+
+def test_a_built_binding_needs_no_compiler(small, monkeypatch, capfd):
+    torch = pytest.importorskip("torch")
+    with open(b.binding_path(torch.__version__), "w"):
+        pass
+    _no_compiler(monkeypatch, small)
+    b.build()
+    assert "is not built" not in capfd.readouterr().err
