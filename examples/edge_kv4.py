@@ -3,8 +3,10 @@
 The prompt's keys and values are quantised as they are written and attended to;
 the draft tree is run in one packed forward with the tree mask; the cloud's
 verdict is looked up in the branch cache; the hit branch's rows move behind the
-accepted tokens; and the next token attends to what is left.  A toy model of a
-few layers (random projections) stands where the draft model would.
+accepted tokens.  A hit branch begins with the verdict's token, so nothing is run
+again: the tree's forward has the state after it.  Elsewhere (a miss, or a chain
+accepted whole) the verdict's token is run, and those sequences alone get its row.
+A toy model of a few layers (random projections) stands where the draft model would.
 
     python examples/edge_kv4.py
 """
@@ -23,13 +25,14 @@ class Layer:
         self.qkv = torch.randn(width, (Hq + 2 * H) * D, generator=gen, device="cuda").bfloat16() * width ** -0.5
         self.out = torch.randn(Hq * D, width, generator=gen, device="cuda").bfloat16() * (Hq * D) ** -0.5
 
-    def __call__(self, x, cache, layer, start, **seen):
-        """x [B, n, width] -> x plus the layer's attention; its keys and values go into the cache."""
+    def __call__(self, x, cache, layer, start, count=None, **seen):
+        """x [B, n, width] -> x plus the layer's attention; its keys and values go into the cache
+        (those of count[b] tokens)."""
         B, n, _ = x.shape
         p = (x @ self.qkv).view(B, n, self.Hq + 2 * self.H, self.D)
         q, k, v = p.split([self.Hq, self.H, self.H], dim=2)        # views: nothing is copied
-        A.kv4_append(cache, layer, k, v, start)
-        return x + A.kv4_attention(q, cache, layer, start, **seen)["out"].flatten(2) @ self.out
+        A.kv4_append(cache, layer, k, v, start, count=count)
+        return x + A.kv4_attention(q, cache, layer, start, count=count, **seen)["out"].flatten(2) @ self.out
 
 
 def forward(layers, x, cache, start, **seen):
@@ -60,7 +63,7 @@ def cycle(B=4, prompt=300, K=4, F=(3, 2, 1, 1), branch_len=2, V=1000, width=256,
     mask, depths = A.tree_mask(F, branch_len)
     follow = torch.randint(V, (B, sum(F), branch_len - 1), generator=gen, device="cuda")
     tree = torch.cat([chain.long(), torch.cat([branches.long()[..., None], follow], -1).flatten(1)], 1)
-    forward(layers, embed[tree], cache, prefix, mask=mask, depth=depths, **seen)
+    state = forward(layers, embed[tree], cache, prefix, mask=mask, depth=depths, **seen)
 
     # the cloud's verdict on the chain (target logits that agree in part)
     z = torch.log(q)
@@ -71,12 +74,18 @@ def cycle(B=4, prompt=300, K=4, F=(3, 2, 1, 1), branch_len=2, V=1000, width=256,
 
     # the hit branch moves behind the accepted tokens; a rejected tail is dropped
     new_len = A.compact_kv(cache, prefix, verdict["accept_len"], slot, K, branch_len)
-    x = forward(layers, embed[verdict["out_token"].long()][:, None], cache, new_len, **seen)
-    return dict(cache=cache, prefix=prefix, new_len=new_len, slot=slot, accept_len=verdict["accept_len"], hidden=x, tree=tree)
+    # what there is to run: the verdict's token, where no branch held it
+    fed = (slot < 0).int()
+    x = forward(layers, embed[verdict["out_token"].long()][:, None], cache, new_len, count=fed, **seen)
+    last = K + slot.clamp(min=0).long() * branch_len + branch_len - 1          # a hit branch's last row in the tree
+    hidden = torch.where(fed[:, None].bool(), x[:, 0], state[torch.arange(B, device="cuda"), last])[:, None]
+    return dict(cache=cache, prefix=prefix, new_len=new_len, length=new_len + fed, slot=slot, accept_len=verdict["accept_len"],
+                out_token=verdict["out_token"], hidden=hidden, prompt=tokens, tree=tree, embed=embed, layers=layers)
 
 
 if __name__ == "__main__":
     r = cycle()
     torch.cuda.synchronize()
     for b in range(len(r["slot"])):
-        print(f"sequence {b}: accepted {int(r['accept_len'][b])}, slot {int(r['slot'][b])}, cache {int(r['prefix'][b])} -> {int(r['new_len'][b])}")
+        print(f"sequence {b}: accepted {int(r['accept_len'][b])}, slot {int(r['slot'][b])}, "
+              f"cache {int(r['prefix'][b])} -> {int(r['length'][b])}")
