@@ -175,11 +175,12 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
             for (int j = 0; j < 8; ++j) v[j] = __ldg(f + j);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                // cut off, not rounded: the largest float32 would become infinities
                 float v0 = v[2 * j], v1 = v[2 * j + 1];
-                uint32_t w = bf2_pack(v0, v1);
+                uint32_t w = __byte_perm(__float_as_uint(v0), __float_as_uint(v1), 0x7632);
                 for (int x = 0; x < sp; ++x) {
                     v0 -= bf_lo(w), v1 -= bf_hi(w);
-                    w = bf2_pack(v0, v1);
+                    w = __byte_perm(__float_as_uint(v0), __float_as_uint(v1), 0x7632);
                 }
                 o[j] = w;
             }
