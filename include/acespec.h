@@ -431,7 +431,7 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *                 lets it see new token j, and its position is prefix +
  *                 depth[i].  mask_stride (words) and depth_stride (entries)
  *                 between two sequences' arrays; 0: shared
- *   scale > 0     of q . k (1 / sqrt(D) as a rule)
+ *   scale > 0     of q . k (1 / sqrt(D) as a rule; at most 2^110)
  *   window, sinks window > 0: of what it sees otherwise a token at position p
  *                 sees positions above p - window and those below sinks
  * Outputs:

@@ -1,6 +1,5 @@
 // C entry points of the 4-bit KV cache: argument checks and launches.
 #include <climits>
-#include <cmath>
 
 #include "kv4_plan.cuh"
 
@@ -128,7 +127,7 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
     const int words = (n + 31) / 32;
     if (mask && ((mask_stride != 0 && mask_stride < (int64_t)n * words) || (depth_stride != 0 && depth_stride < n)))
         return ACES_ERR_INVALID_ARG;
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return ACES_ERR_INVALID_ARG;
+    if (!(scale > 0.0f && scale <= 0x1p110f)) return ACES_ERR_INVALID_ARG;  // a.scale below is finite
     if (window < 0 || sinks < 0) return ACES_ERR_INVALID_ARG;
     a.k = pk, a.v = pv;
     a.q = q;
