@@ -699,18 +699,31 @@ cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cuda
     return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
 }
 
-// CTAs of a cluster that has an item to itself, or 0: shares and a join.  Clusters
-// while there is an SM for each of their CTAs (beyond, two on an SM take longer: four
-// sequences of 4000 positions, eight key heads, by fours 18.5 us, by eights 20.5) and
-// no CTA has more than KV4_DIRECT units, by the cache's or the window's length.
-// Against shares (us, eight key heads of 128): one sequence of 1000 positions 12.4 /
-// 14.3, of 4000 14.8 / 16.4, of 8000 16.9 / 20.5, of 16000 22.6 / 24.6 (by eights);
-// four of 8000 22.7 / 27.6 (by fours); 16 of 1000 18.4 / 24.6, of 2000 22.7 / 30.7 (one
-// CTA each).
-static int few_cluster(long long items, int most, int nsm) {
+// CTAs of a cluster that has an item to itself, or 0: shares and a join.  An item's
+// units are counted by the cache's length or the window's (the sequences' lengths lie
+// on the device): in a cache that is longer than it needs to be, shares come sooner.
+//   Two to eight CTAs, while there is an SM for each (beyond, two on an SM take longer:
+// four sequences of 4000 positions, eight key heads, by fours 18.5 us, by eights 20.5)
+// and none has more than KV4_DIRECT units.  Against shares (us, eight key heads of 128):
+// one sequence of 1000 positions 12.4 / 14.3, of 4000 14.8 / 16.4, of 8000 16.9 / 20.5,
+// of 16000 22.6 / 24.6 (by eights); four of 8000 22.7 / 27.6 (by fours).
+//   One CTA, up to KV4_DIRECT units, for any number of items of bfloat16.  Against
+// shares (key heads of 128, sequences as long as the cache, and in brackets of all
+// lengths up to it): four rows, 152 items of eight units 20.6 / 28.6 (20.6 / 24.0), 320
+// 41.0 / 40.9 (29.5 / 30.9), 640 63.5 / 64.7 (47.9 / 48.0), 1216 98.8 / 100.5 (77.9 /
+// 76.0), 320 of two units 20.6 / 24.5; 16 rows, one CTA an SM, 160 of eight 49.1 / 40.9
+// (28.7 / 34.8), 320 73.5 / 64.0 (47.3 / 53.0).  Float32's products are three times as
+// many, and a last wave that is nearly empty costs more than a join: beyond the SMs'
+// number up to FEW_ONE units.  160 of eight 46.0 / 34.9 (26.1 / 29.7), 320 69.7 / 59.4
+// (43.0 / 43.1), 512 92.9 / 85.8 (65.6 / 61.5); of four 160 30.7 / 26.9 (19.7 / 23.0),
+// 320 45.1 / 40.8 (31.9 / 34.9); of two 22.1 / 22.6 (18.5 / 22.3), 31.3 / 31.3 (26.8 /
+// 30.8).
+constexpr int FEW_ONE = 4;
+static int few_cluster(long long items, int most, bool f32, int nsm) {
     int cl = 1;
     while (cl < FCL && cl < most && items * cl * 2 <= nsm) cl *= 2;
-    return items < (1ll << 30) && (most + cl - 1) / cl <= KV4_DIRECT ? cl : 0;
+    if (items >= (1ll << 30) || (most + cl - 1) / cl > KV4_DIRECT) return 0;
+    return f32 && items > nsm && most > FEW_ONE ? 0 : cl;
 }
 
 template <int D, bool F32, int NT>
@@ -718,7 +731,7 @@ static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
     using C = Few<D, F32, NT>;
     const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
     const long long items = (long long)a.B * RT * a.H;
-    const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, nsm);
+    const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
     const bool direct = CL > 0;
     const int grid = direct ? (int)items * CL : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);

@@ -13,8 +13,8 @@
 // one CTA's range is written out by it; the pieces of one that several share go
 // to the workspace as sums not yet divided, with their reference maximum, and
 // k_kv4_join adds them in the CTAs' order.
-// Where no item can have more than KV4_DIRECT units for each CTA of a cluster (the
-// cache is short, or the window), a cluster takes it and adds its parts up in
+// Where no item can have more than KV4_DIRECT units for each CTA of a cluster, or one
+// CTA (the cache is short, or the window), it takes the item and adds its parts up in
 // shared memory: nothing to join (few rows only: few_cluster() and its figures).
 #pragma once
 #include <atomic>
