@@ -525,7 +525,7 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
     tokens do not lie in the cache; ROW_TIMEOUT: a wait in the kernel gave up,
     the results are not valid).
 
-    The workspace (kv4_workspace_bytes(), up to 41 MB) is allocated for the call on
+    The workspace (kv4_workspace_bytes(), up to 61 MB) is allocated for the call on
     its stream and given back behind it, unless one is given: that one has to be on
     the cache's device, contiguous, large enough and no other call's meanwhile.
     """

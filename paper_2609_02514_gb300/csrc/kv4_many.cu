@@ -23,7 +23,8 @@
 // Sums are rescaled only when a row's maximum grew by more than 2^8 (in the
 // weights' scale); weights stay below that and lose nothing by it.  Weights are
 // rounded to bfloat16 for their product (the sums of weights take them as they
-// were); scores and sums are float32.
+// were); scores and sums are float32, the sums by the tensor cores for as many keys as
+// FOLD allows.
 //
 // What bounds it is a group's chain (scores out of TMEM, maximum, exponentials,
 // weights back in, 64 keys at a time): a tile of 256 rows of 128 takes 4.1 thousand
@@ -59,6 +60,11 @@ struct ManyCost {
     static __device__ __forceinline__ int all(const Kv4Keys &k) { return FIX + k.units * weight(k); }
 };
 constexpr float M_LAZY = 8.0f;
+// Tiles of a group after which its sums leave TMEM for float32 totals in the workspace:
+// the tensor cores' adds (one for 16 keys) cut off up to a unit each, so sums of one sign
+// lie up to 2^-13 low then.  Without totals, values of one sign behind 600000 positions
+// came out 3.6e-3 low, twice the rounding of the result; with them 1e-4.
+constexpr int FOLD = 128;
 // -- tcgen05 ------------------------------------------------------------------
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -256,6 +262,29 @@ __device__ __forceinline__ void store_piece(uint8_t *tile, int p, const Piece<D>
     }
 }
 
+// Adds a row's sums in TMEM to its totals (256 floats apart, their maximum behind
+// them; the first time there are none) and leaves zeros.
+template <int D>
+static __device__ __noinline__ void fold_sums(float *tot, uint32_t tO, float m, bool first) {
+    const float was = first ? -INFINITY : tot[256 * D], keep = was == -INFINITY ? 0.0f : ex2(was - m);
+    tot[256 * D] = m;
+#pragma unroll 1
+    for (int w = 0; w < D / 16; ++w) {
+        float o[16];
+        uint32_t zero[16];
+        tc_ld16(tO + 16 * w, o);
+        tc_wait_ld(o);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            float *to = tot + 256 * (16 * w + c);
+            *to = first ? o[c] : fmaf(*to, keep, o[c]);
+            zero[c] = 0u;
+        }
+        tc_st16(tO + 16 * w, zero);
+    }
+    tc_wait_st();
+}
+
 template <int D>
 __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, int RT) {
     using C = Many<D>;
@@ -372,84 +401,92 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 if (lane == 0) mbar_arrive(b_q + 8 * x);
             }
             float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-#pragma unroll 1
-            for (int y = 0; y < mine; ++y) {
-                const int half = y & 1;
-                if (half == 0) {
+            for (int y = 0; y < mine;) {
+                if (y > 0) {  // to the totals: the last tile's product is over before these scores are made
                     wait(b_s + 8 * x, n_s);
                     tc_after();
+                    if (warp_live) fold_sums<D>(ws.total + (size_t)blockIdx.x * 256 * (D + 1) + x * 128 + row, tO, m, y == 2 * FOLD);
                 }
-                if (warp_live) {
-                    const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + half * MKH;
-                    const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > a.sinks);
-                    const uint32_t at = tS + half * MKH;
-                    float v[2][32];
-                    tc_ld32(at, v[0]);
-                    tc_ld32(at + 32, v[1]);
-                    tc_wait_ld(v[0]);
-                    tc_wait_ld(v[1]);
-                    if (masked) {
-                        uint32_t see0 = 0u, see1 = 0u;
-                        if (row_live) see0 = seen_word(a, b, P, key.cnt, j0, i, pos), see1 = seen_word(a, b, P, key.cnt, j0 + 32, i, pos);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
-                            if (!(see1 >> c & 1u)) v[1][c] = -INFINITY;
-                        }
-                        __syncwarp();
-                    }
-                    float m0 = v[0][0], m1 = v[0][31], m2 = v[1][0], m3 = v[1][31];
-#pragma unroll
-                    for (int c = 1; c < 15; c += 2) {
-                        m0 = max3(m0, v[0][c], v[0][c + 1]), m1 = max3(m1, v[0][c + 15], v[0][c + 16]);
-                        m2 = max3(m2, v[1][c], v[1][c + 1]), m3 = max3(m3, v[1][c + 15], v[1][c + 16]);
-                    }
-                    m0 = max3(m0, v[0][15], v[0][30]), m2 = max3(m2, v[1][15], v[1][30]);
-                    const float mx = fmaxf(max3(m0, m1, m2), m3) * a.scale;
-                    const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
-                    if (__any_sync(0xffffffffu, grew)) {
-                        const float f = grew ? ex2(m - mx) : 1.0f;
-                        if (grew) m = mx;
-                        l0 *= f, l1 *= f;
-                        if (y > 0) {
-                            // what was added last is there: before these scores were
-                            // made, or (the first half's) by a word of its own
-                            if (half == 1) wait(b_f + 8 * x, n_s);
-                            tc_after();
+                const int stop = min(mine, y + 2 * FOLD);
 #pragma unroll 1
-                            for (int w = 0; w < D / 16; ++w) {
-                                float o[16];
-                                tc_ld16(tO + 16 * w, o);
-                                tc_wait_ld(o);
-                                uint32_t u[16];
+                for (; y < stop; ++y) {
+                    const int half = y & 1;
+                    if (half == 0) {
+                        wait(b_s + 8 * x, n_s);
+                        tc_after();
+                    }
+                    if (warp_live) {
+                        const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + half * MKH;
+                        const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > a.sinks);
+                        const uint32_t at = tS + half * MKH;
+                        float v[2][32];
+                        tc_ld32(at, v[0]);
+                        tc_ld32(at + 32, v[1]);
+                        tc_wait_ld(v[0]);
+                        tc_wait_ld(v[1]);
+                        if (masked) {
+                            uint32_t see0 = 0u, see1 = 0u;
+                            if (row_live) see0 = seen_word(a, b, P, key.cnt, j0, i, pos), see1 = seen_word(a, b, P, key.cnt, j0 + 32, i, pos);
 #pragma unroll
-                                for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(o[c] * f);
-                                tc_st16(tO + 16 * w, u);
+                            for (int c = 0; c < 32; ++c) {
+                                if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
+                                if (!(see1 >> c & 1u)) v[1][c] = -INFINITY;
+                            }
+                            __syncwarp();
+                        }
+                        float m0 = v[0][0], m1 = v[0][31], m2 = v[1][0], m3 = v[1][31];
+#pragma unroll
+                        for (int c = 1; c < 15; c += 2) {
+                            m0 = max3(m0, v[0][c], v[0][c + 1]), m1 = max3(m1, v[0][c + 15], v[0][c + 16]);
+                            m2 = max3(m2, v[1][c], v[1][c + 1]), m3 = max3(m3, v[1][c + 15], v[1][c + 16]);
+                        }
+                        m0 = max3(m0, v[0][15], v[0][30]), m2 = max3(m2, v[1][15], v[1][30]);
+                        const float mx = fmaxf(max3(m0, m1, m2), m3) * a.scale;
+                        const bool grew = mx > m + M_LAZY || (m == -INFINITY && mx > m);
+                        if (__any_sync(0xffffffffu, grew)) {
+                            const float f = grew ? ex2(m - mx) : 1.0f;
+                            if (grew) m = mx;
+                            l0 *= f, l1 *= f;
+                            if (y > 0) {
+                                // what was added last is there: before these scores were
+                                // made, or (the first half's) by a word of its own
+                                if (half == 1) wait(b_f + 8 * x, n_s);
+                                tc_after();
+#pragma unroll 1
+                                for (int w = 0; w < D / 16; ++w) {
+                                    float o[16];
+                                    tc_ld16(tO + 16 * w, o);
+                                    tc_wait_ld(o);
+                                    uint32_t u[16];
+#pragma unroll
+                                    for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(o[c] * f);
+                                    tc_st16(tO + 16 * w, u);
+                                }
                             }
                         }
-                    }
-                    const float ref = m == -INFINITY ? 0.0f : -m;
+                        const float ref = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        uint32_t pk[16];
-                        float s0 = 0.0f, s1 = 0.0f;
+                        for (int w = 0; w < 2; ++w) {
+                            uint32_t pk[16];
+                            float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) {
-                            float *e = v[w] + 2 * c;
-                            fma2(e[0], e[1], a.scale, ref);
-                            e[0] = ex2(e[0]), e[1] = ex2(e[1]);
-                            add2(s0, s1, e[0], e[1]);
-                            pk[c] = bf2_pack(e[0], e[1]);
+                            for (int c = 0; c < 16; ++c) {
+                                float *e = v[w] + 2 * c;
+                                fma2(e[0], e[1], a.scale, ref);
+                                e[0] = ex2(e[0]), e[1] = ex2(e[1]);
+                                add2(s0, s1, e[0], e[1]);
+                                pk[c] = bf2_pack(e[0], e[1]);
+                            }
+                            l0 += s0, l1 += s1;
+                            tc_st16(at + C::TP + 16 * w, pk);
                         }
-                        l0 += s0, l1 += s1;
-                        tc_st16(at + C::TP + 16 * w, pk);
+                        tc_wait_st();
                     }
-                    tc_wait_st();
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_p + 8 * (2 * x + half));
+                    n_s += half;
                 }
-                tc_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_p + 8 * (2 * x + half));
-                n_s += half;
             }
             if (mine > 0) {
                 wait(b_o + 8 * x, n_o++);
@@ -465,7 +502,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             const bool whole = seg.whole();
             float *slot = ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);
             const int orow = (seg.b * a.n + ri) * a.Hq + seg.h * a.G + (r - ri * a.G);  // at most 2^30
-            float f = 1.0f;
+            // what the totals count for, those of the rows' weights being to m
+            const bool folded = mine > 2 * FOLD && warp_live;
+            const float *tot = ws.total + (size_t)blockIdx.x * 256 * (D + 1) + x * 128 + row;
+            float f = 1.0f, ft = 0.0f;
+            if (folded && tot[256 * D] != -INFINITY) ft = ex2(tot[256 * D] - m);
             if (single) {  // both groups have the rows
                 sm_m[x][row] = m, sm_l[x][row] = l;
                 asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -484,6 +525,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 if (mine > 0 && warp_live) {
                     tc_ld32(tO + 32 * w, v);
                     tc_wait_ld(v);
+                    if (folded) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] = fmaf(tot[256 * (32 * w + c)], ft, v[c]);
+                    }
                 } else {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[c] = 0.0f;
@@ -708,12 +753,14 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
 // Rows of an item.
 static int many_rows_of(int n, int G) { return (long long)n * G <= 128 ? 128 : 256; }
 
-size_t kv4_many_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(nsm, many_rows_of(n, G), D); }
+// (after the pieces: a CTA's totals, [D] by 256 rows and their maximum)
+size_t kv4_many_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(nsm, many_rows_of(n, G), D) + (size_t)nsm * 256 * (D + 1) * 4; }
 
 template <int D>
 static cudaError_t run_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
     const int R = many_rows_of(a.n, a.G), RT = (int)(((long long)a.n * a.G + R - 1) / R);
-    const Kv4Ws ws = kv4_ws_carve(workspace, nsm);
+    Kv4Ws ws = kv4_ws_carve(workspace, nsm);
+    ws.total = ws.piece + (size_t)2 * nsm * R * (D + 2);
     static std::atomic<unsigned long long> allowed{0};
     cudaError_t e = allow_smem(k_kv4_many<D>, Many<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;

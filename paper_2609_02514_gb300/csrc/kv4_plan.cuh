@@ -41,12 +41,14 @@ static_assert(sizeof(Kv4Info) == 48, "Kv4Info layout");
 struct Kv4Ws {
     Kv4Info *info;
     float *piece;
+    float *total;  // k_kv4_many's own
 };
 inline size_t kv4_ws_bytes(int C, int R, int D) { return sizeof(Kv4Info) * (size_t)C + (size_t)2 * C * R * (D + 2) * 4; }
 inline Kv4Ws kv4_ws_carve(void *p, int C) {
     Kv4Ws w;
     w.info = reinterpret_cast<Kv4Info *>(p);
     w.piece = reinterpret_cast<float *>(w.info + C);
+    w.total = nullptr;
     return w;
 }
 
