@@ -83,14 +83,17 @@ struct Few {
 // channels of neighbouring keys: channels and keys come in whatever order the
 // words have, the same in both operands.  P' needs its pairs along the keys,
 // where S' has them along the rows: movmatrix turns the 8 x 8 blocks.
-// bfloat16 weights are rounded for their product; float32 queries and weights are
-// three bfloat16 parts each, all 24 bits.
+// With bfloat16 queries the weights are rounded to bfloat16 for their product (half a
+// unit of eight bits, what the result's own rounding costs; all 24 bits would be three
+// products), and the tensor cores add a warp's eighth of the keys up, an add for 16 of
+// them, which cuts off up to a unit: 1e-4 for 131072 positions that one CTA has alone.
+// Float32 queries and weights are three bfloat16 parts each, all 24 bits.
 //
-// What bounds it is the codes' way into operands: some 780 warp instructions 32 keys
-// of 128, 60 of 100 issue slots taken.  One token, 32 heads over 8: 32 sequences of
-// 32768 positions 260 us, 5.16 TB/s; 64 of 200 to 8191 88 us, 4.0; one of 131071
-// 48 us, 3.5.  The rest of the shorter ones is a CTA's start (3 us: its share, its
-// first copies), its warps' merge (2.5 us an item) and the join.  mma.sync and not
+// Most of its time is the codes' way into operands: some 780 warp instructions 32 keys
+// of 128, 60 of 100 issue slots taken (and of the ALU's).  One token, 32 heads over 8:
+// 32 sequences of 32768 positions 260 us, 5.16 TB/s; 64 of 200 to 8191 88 us, 4.0; one
+// of 131071 48 us, 3.5.  The rest of the shorter ones is a CTA's start (3 us: its share,
+// its first copies), its warps' merge (2.5 us an item) and the join.  mma.sync and not
 // the tcgen05 kernel: its rows are padded to 128 (the rule in kv4_abi.cu).
 template <int D, bool F32, int NT>
 __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att a, Kv4Ws ws, int RT, int CL) {

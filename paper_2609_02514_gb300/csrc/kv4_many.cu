@@ -22,16 +22,17 @@
 // made in the place of a P whose product is under way.
 // Sums are rescaled only when a row's maximum grew by more than 2^8 (in the
 // weights' scale); weights stay below that and lose nothing by it.  Weights are
-// rounded to bfloat16 for their product (the sums of weights take them as they
-// were); scores and sums are float32, the sums by the tensor cores for as many keys as
+// rounded to bfloat16 for their product, as the tensor cores take them: all 24 bits
+// would be three products, and half a unit of eight bits is what the result's own
+// rounding costs (the sums of weights take them as they were); scores and sums are float32, the sums by the tensor cores for as many keys as
 // FOLD allows.
 //
 // What bounds it is a group's chain (scores out of TMEM, maximum, exponentials,
 // weights back in, 64 keys at a time): a tile of 256 rows of 128 takes 4.1 thousand
-// cycles, its products alone 2.6, and 45 of 100 issue slots are taken.  128 keys in
+// cycles, its products alone 2.6, and 45 to 55 of 100 issue slots are taken.  128 keys in
 // one product of scores and weights by halves instead of 64 of each: 1003 -> 770 us
-// (4096 tokens of two sequences behind 4000, 32 heads over 8).  That call: 729 us,
-// 1.10 PFLOP/s; trees of 80 tokens, 16 sequences: 125 us, 0.60; 2048 tokens of four
+// (4096 tokens of two sequences behind 4000, 32 heads over 8).  That call: 740 us,
+// 1.09 PFLOP/s; trees of 80 tokens, 16 sequences: 127 us, 0.59; 2048 tokens of four
 // sequences behind a window of 1024, 16 heads of 64: 127 us, 0.27.  Beside the
 // tiles an item pays for its queries, its pipeline's start and its way out, two to
 // four tiles' time, a fifth of the last one's.

@@ -6,10 +6,12 @@
 // status follows; within a CTA the tokens of one head are neighbours, whose
 // cache rows are too.  What a large call has to do is to move numbers on one side
 // and 5/8 (D = 128) or 3/4 of a byte each on the other.  Reading does so at 6.4
-// TB/s (704.6 MB in 109.9 us).  Writing one to two thousand tokens a sequence is one
-// or two waves of CTAs, and its time is their start, one load's way from memory and
-// back, and 18 (bfloat16) to 43 (float32) instructions a number: 48.5 MB in 11.5 us,
-// half the issue slots taken while CTAs run.
+// TB/s (704.6 MB in 109.9 us).  Writing is 18 (bfloat16) to 43 (float32)
+// instructions a number and a few waves of CTAs, each a start and one or two loads'
+// way from memory and back: 80 tokens of 64 sequences (eight heads of 128, bfloat16)
+// 11.5 us, three waves of 608 CTAs, the last of 64, with two groups a thread, the
+// second's load behind the first's store; 4099 of 3 (four of 64, float32) 12.3 us, five
+// waves of 760, the last of 35.  Half the issue slots are taken while CTAs run.
 #define ACES_FILE 7  // site numbers of the checked build
 #include "kv4.cuh"
 
