@@ -442,7 +442,9 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *   seq_status    [B] int32: ACES_ROW_RANGE where prefix_len or count is
  *                 negative, count above n, or prefix + count above S (the
  *                 sequence's tokens count as padding); ACES_ROW_TIMEOUT
- * Products are those of the cache's numbers and q's as they are, sums float32.
+ * Products are those of the cache's numbers and q's as they are, sums float32
+ * (for bfloat16 q by the tensor cores, whose adds cut off: 2^-13 at most, or
+ * for up to 16 query rows a key head 1e-9 of the result for each position).
  * Weights are rounded to bfloat16 before they meet the values when q is
  * bfloat16, and are float32 when it is.
  * workspace: aces_kv4_workspace_bytes(B, n, Hq, H, D) bytes, 16-byte aligned,
