@@ -329,7 +329,7 @@ def _turned(s, x, weight, kind):
     c = s["case"]
     x = x.to(kind)
     if c["norm"]:
-        x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS) * weight.to(kind)
+        x = x * weight.to(kind) * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)       # (equal products stay equal)
     angle = _angles(s)
     cos, sin = torch.cos(angle).to(kind), torch.sin(angle).to(kind)
     y, rest = x[..., :c["R"]], x[..., c["R"]:]
@@ -423,7 +423,7 @@ def _turned64(s, x, weight):
     c = s["case"]
     x = x.double().clone()
     if weight is not None:
-        x = x / torch.sqrt(x.square().sum(-1, keepdim=True) / c["D"] + EPS) * weight.double()
+        x = x * weight.double() / torch.sqrt(x.square().sum(-1, keepdim=True) / c["D"] + EPS)
     out = x.clone()
     half = c["R"] // 2
     for j in range(half):
