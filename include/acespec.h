@@ -416,6 +416,71 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
                           const int32_t *start, int n, void *k, void *v, aces_dtype dt, aces_stream_t stream);
 
 /*
+ * How queries and keys are normed and turned by their positions, head by head.
+ * With x a head's D numbers and w its weights:
+ *   y = x w / sqrt(mean(x^2) + eps)         where norm is set, else y = x
+ *   z_u = scale (y_u cos t - y_v sin t), z_v = scale (y_v cos t + y_u sin t)
+ *   t = p * inv_freq[j] in 64 bits, p the token's position on the pair's axis
+ * for the pairs j < rot_dim / 2 of channels (u, v): (j, j + rot_dim / 2), or
+ * with interleaved (2 j, 2 j + 1).  Channels from rot_dim on stay y.
+ *   inv_freq     [rot_dim / 2] float32
+ *   rot_dim      a multiple of D / 4, at most D
+ *   axes         [rot_dim / 2] int32 or NULL: the pairs' axes (beyond 0 ..
+ *                n_axes - 1 the nearest; needed with more than one)
+ *   positions    [n_axes, B, n] int32 dense, n_axes <= ACES_MAX_AXES, or NULL:
+ *                token i of sequence b is at start[b] + base[b] + i on every
+ *                axis, or + depth[i] (aces_tree_mask's; depth_stride entries
+ *                between two sequences', 0: shared) in place of i
+ *   start        [B] int32 (aces_rotate_qk, without positions); NULL in
+ *                aces_kv4_append_rotated, which has its own
+ *   base         [B] int32 or NULL: positions before the cache's first (a shared
+ *                prefix)
+ *   q_weight, k_weight   float32 or bfloat16, [D] (stride 0) or a row for each
+ *                head (stride D or more), or NULL: ones; only with norm
+ *   eps          1e-30 .. 1e30
+ *   scale        2^-20 .. 2^20 (1 as a rule; of scaled position schemes)
+ * Numbers are float32 inside (angles 64 bits); each result is rounded once.
+ */
+#define ACES_MAX_AXES 4
+typedef struct {
+    const float *inv_freq;
+    int rot_dim, interleaved;
+    const int32_t *axes, *positions;
+    int n_axes;
+    const int32_t *start, *base, *depth;
+    int64_t depth_stride;
+    const void *q_weight, *k_weight;
+    aces_dtype q_weight_dt, k_weight_dt;
+    int64_t q_weight_stride, k_weight_stride;
+    int norm;
+    double eps, scale;
+} aces_turn;
+
+/*
+ * Norms and rotation of queries [B, n, Hq, D] and keys [B, n, H, D], float32 or
+ * bfloat16 (dt), D = 64 or 128; the last dimension is dense, the others' strides
+ * are host arrays in elements (multiples of 16 bytes on 16-byte aligned arrays
+ * are read and written in vectors).  q_out and k_out, of the same type, may be
+ * q and k themselves with the same strides; otherwise they overlap neither.
+ */
+aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const int64_t *q_strides,
+                           const int64_t *k_strides, int B, int n, int Hq, int H, int D, const aces_turn *turn,
+                           void *q_out, void *k_out, const int64_t *q_out_strides, const int64_t *k_out_strides,
+                           aces_stream_t stream);
+
+/*
+ * The same for new tokens of a cache in 4 bits, whose keys, so turned, and
+ * values are quantised as they are written (aces_kv4_append's arguments and
+ * status; the keys are not rounded to dt before: their codes are those of the
+ * numbers in 64 bits).  q_out has every token, padding too.
+ */
+aces_status aces_kv4_append_rotated(void *cache, int planes, int layer, int B, int H, int S, int D, const void *q,
+                                    const void *k, const void *v, aces_dtype dt, const int64_t *q_strides,
+                                    const int64_t *k_strides, const int64_t *v_strides, int Hq, const int32_t *start,
+                                    const int32_t *count, int n, const aces_turn *turn, void *q_out,
+                                    const int64_t *q_out_strides, int32_t *row_status, aces_stream_t stream);
+
+/*
  * Attention of n new tokens of every sequence over a cache in 4 bits (Sec.
  * III-C: the packed branch forward; n = 1: one token; any n: a prompt, in one
  * piece or several).  The new tokens' keys and values are in the cache

@@ -14,6 +14,8 @@ without the built library, or with host tensors, raises.
     cache_lookup(branch_tok, F, pi, tok)  Algorithm 1 state recovery
     kv4_cache, kv4_append, kv4_read       a KV cache in 4 bits
     kv4_attention(q, cache, ...)          tokens, trees and prompts against it
+    rotate_qk(q, k, inv_freq, ...)        norms and positions of queries and keys
+    kv4_append_rotated(cache, ...)        the same, the keys going into that cache
 """
 from __future__ import annotations
 
@@ -25,6 +27,7 @@ import torch
 
 __all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
            "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
+           "rotate_qk", "kv4_append_rotated",
            "ROW_NONFINITE", "ROW_BAD_Q", "ROW_TIMEOUT", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -131,15 +134,19 @@ def _open(path):
     lib.aces_kv4_append.argtypes = [P, I, I, I, I, I, I, P, P, I, P, P, P, P, I, P, P]
     lib.aces_kv4_read.argtypes = [P, I, I, I, I, I, I, P, I, P, P, I, P]
     lib.aces_kv4_attention.argtypes = [P, I, P, P, I, I, I, I, I, I, I, I, P, P, P, L, P, L, F, I, I, P, P, P, P, S, P]
+    lib.aces_rotate_qk.argtypes = [P, P, I, P, P, I, I, I, I, I, P, P, P, P, P, P]
+    lib.aces_kv4_append_rotated.argtypes = [P, I, I, I, I, I, I, P, P, P, I, P, P, P, I, P, P, I, P, P, P, P, P]
     lib.aces_status_string.argtypes = [I]
     lib.aces_status_string.restype = ctypes.c_char_p
     for f in (lib.aces_verify, lib.aces_verify_exact, lib.aces_sparsify, lib.aces_cache_build,
               lib.aces_cache_lookup, lib.aces_resample_sparse, lib.aces_tree_budget, lib.aces_branch_alloc,
-              lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention):
+              lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention,
+              lib.aces_rotate_qk, lib.aces_kv4_append_rotated):
         f.restype = I
     # what the native half of the binding calls
     lib.kv4_entries = tuple(ctypes.cast(f, P).value for f in (lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention,
-                                                                  lib.aces_kv4_workspace_bytes))
+                                                                  lib.aces_kv4_workspace_bytes,
+                                                                  lib.aces_rotate_qk, lib.aces_kv4_append_rotated))
     if hasattr(lib, "aces_checked_violation"):
         lib.aces_checked_violation.argtypes = [P]
         lib.aces_checked_violation.restype = I
@@ -536,4 +543,48 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
         o.get("lse"), o.get("status"), workspace, _stream(dev))
     if code != 0:
         _check("aces_kv4_attention", code)
+    return o
+
+
+def rotate_qk(q, k, inv_freq, start=None, depth=None, positions=None, axes=None, q_weight=None, k_weight=None, eps: float | None = None,
+              interleaved: bool = False, scale: float = 1.0, out: dict | None = None):
+    """Queries q [B, n, Hq, D] and keys k [B, n, H, D] normed head by head (eps given; q_weight,
+    k_weight: [D], or [heads, D], or none) and turned by their positions; returns a dict of q, k.
+
+    inv_freq [R / 2] float32: the first R channels turn (a multiple of D / 4), pairs j and j + R / 2,
+    or interleaved 2 j and 2 j + 1, by the angle position * inv_freq[j].  Token i of sequence b is at
+    start[b] + i, or with tree_mask()'s depth at start[b] + depth[i]; or at positions [B, n], or
+    [A, B, n] with up to four axes, of which pair j turns by axes[j] ([R / 2] int32).  scale multiplies
+    the turned channels.  q and k may be strided views with a dense last dimension, and `out` may
+    hold q and k themselves (in place); anything else in it overlaps neither.
+    """
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    lib, native, dev = _lib or load(), _native_module or _native(), q.device
+    o = {} if out is None else dict(out)
+    code, o["q"], o["k"] = native.rotate(lib.kv4_entries[4], q, k, inv_freq, start, None, depth, positions, axes, q_weight, k_weight, eps,
+                                         interleaved, scale, o.get("q"), o.get("k"), _stream(dev))
+    if code != 0:
+        _check("aces_rotate_qk", code)
+    return o
+
+
+def kv4_append_rotated(cache, layer: int, q, k, v, start, inv_freq, base=None, depth=None, count=None, positions=None, axes=None,
+                       q_weight=None, k_weight=None, eps: float | None = None, interleaved: bool = False, scale: float = 1.0,
+                       out: dict | None = None):
+    """rotate_qk() of q and k, with the keys so turned and v [B, n, H, D] quantised into the cache at
+    start[b] + i as kv4_append() does (tokens i >= count[b] are padding and not written); returns a
+    dict of q [B, n, Hq, D] (every token's) and status [B, n] int32.
+
+    Without positions token i is at base[b] + start[b] + i, or + depth[i]; base [B]: positions before
+    the cache's first, as of a prefix that is shared.  The keys are not rounded to their type before
+    they are quantised.
+    """
+    lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
+    o = {} if out is None else dict(out)
+    code, o["q"], o["status"] = native.append_rotated(lib.kv4_entries[5], cache, layer, q, k, v, start, count, inv_freq, None, base, depth,
+                                                      positions, axes, q_weight, k_weight, eps, interleaved, scale, o.get("q"),
+                                                      o.get("status"), _stream(dev))
+    if code != 0:
+        _check("aces_kv4_append_rotated", code)
     return o

@@ -231,7 +231,158 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     });
 }
 
-PyMethodDef methods[] = {{"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append)), METH_FASTCALL, nullptr},
+using Rotate = decltype(&aces_rotate_qk);
+using AppendRotated = decltype(&aces_kv4_append_rotated);
+
+double real(PyObject *o) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Refusal{""};
+    return x;
+}
+// heads [B, n, heads, D] of a type on a device, the last dimension dense
+struct Heads {
+    void *p = nullptr;
+    PyObject *given = nullptr;
+    Tensor made;
+    int64_t stride[3];
+    void take(PyObject *o, const char *name, const Tensor &q, int64_t n_heads) {
+        const Tensor &t = cuda(o, name);
+        if (t.scalar_type() != q.scalar_type() || t.dim() != 4 || t.device() != q.device() || t.size(0) != q.size(0) || t.size(1) != q.size(1) ||
+            (n_heads >= 0 && t.size(2) != n_heads) || t.size(2) > INT32_MAX || t.size(3) != q.size(3))
+            throw Refusal{std::string(name) + " must be a " + c10::toString(q.scalar_type()) + " [" + std::to_string(q.size(0)) + ", " +
+                          std::to_string(q.size(1)) + ", " + (n_heads < 0 ? "heads" : std::to_string(n_heads)) + ", " + std::to_string(q.size(3)) +
+                          "] on " + q.device().str()};
+        if (t.stride(3) != 1 && t.size(3) != 1) throw Refusal{std::string(name) + " must have a dense last dimension"};
+        given = o, p = t.data_ptr();
+        for (int i = 0; i < 3; ++i) stride[i] = t.stride(i);
+    }
+    // an output: the caller's (`in` itself, or something that does not overlap it) or a new one
+    void put(PyObject *o, const char *name, const Tensor &q, const Heads &in, int64_t n_heads) {
+        if (o != Py_None) {
+            take(o, name, q, n_heads);
+            if (p == in.p && !std::equal(stride, stride + 3, in.stride)) throw Refusal{std::string(name) + " overlaps its input in another layout"};
+            return;
+        }
+        made = at::empty({q.size(0), q.size(1), n_heads, q.size(3)}, q.options());
+        p = made.data_ptr();
+        for (int i = 0; i < 3; ++i) stride[i] = made.stride(i);
+    }
+    PyObject *object() const {
+        if (!given) return THPVariable_Wrap(made);
+        Py_INCREF(given);
+        return given;
+    }
+};
+const Tensor &queries(PyObject *o) {
+    const Tensor &q = cuda(o, "q");
+    if (q.dim() != 4 || (q.scalar_type() != at::kFloat && q.scalar_type() != at::kBFloat16))
+        throw Refusal{"q must be float32 or bfloat16 [B, n, heads, D]"};
+    for (int i = 0; i < 4; ++i)
+        if (q.size(i) > INT32_MAX) throw Refusal{"q has a dimension above 2^31"};
+    return q;
+}
+// a[0..10]: inv_freq, start, base, depth, positions, axes, q_weight, k_weight, eps, interleaved, scale
+aces_turn turn_of(PyObject *const *a, const Tensor &q, int64_t Hq, int64_t H) {
+    const int64_t B = q.size(0), n = q.size(1), D = q.size(3);
+    aces_turn t = {};
+    const Tensor &f = cuda(a[0], "inv_freq");
+    if (f.dim() != 1 || f.size(0) > D / 2) throw Refusal{"inv_freq must be float32 [R / 2] with R at most " + std::to_string(D)};
+    t.inv_freq = (const float *)dense(a[0], "inv_freq", {f.size(0)}, at::kFloat, q);
+    t.rot_dim = 2 * (int)f.size(0);
+    if (a[1] != Py_None) t.start = (const int32_t *)dense(a[1], "start", {B}, at::kInt, q);
+    if (a[2] != Py_None) t.base = (const int32_t *)dense(a[2], "base", {B}, at::kInt, q);
+    if (a[3] != Py_None) {
+        if (cuda(a[3], "depth").dim() == 2)
+            t.depth = (const int32_t *)dense(a[3], "depth", {B, n}, at::kInt, q), t.depth_stride = n;
+        else
+            t.depth = (const int32_t *)dense(a[3], "depth", {n}, at::kInt, q);
+    }
+    t.n_axes = 1;
+    if (a[4] != Py_None) {
+        const Tensor &p = cuda(a[4], "positions");
+        if (p.dim() == 3) {
+            if (p.size(0) < 1 || p.size(0) > ACES_MAX_AXES) throw Refusal{"positions must have 1 to " + std::to_string(ACES_MAX_AXES) + " axes"};
+            t.n_axes = (int)p.size(0);
+            t.positions = (const int32_t *)dense(a[4], "positions", {t.n_axes, B, n}, at::kInt, q);
+        } else {
+            t.positions = (const int32_t *)dense(a[4], "positions", {B, n}, at::kInt, q);
+        }
+        if (a[2] != Py_None || a[3] != Py_None) throw Refusal{"positions stand for base and depth, not beside them"};
+    }
+    if (a[5] != Py_None) t.axes = (const int32_t *)dense(a[5], "axes", {f.size(0)}, at::kInt, q);
+    if (t.n_axes > 1 && !t.axes) throw Refusal{"positions of several axes need axes"};
+    for (int i = 0; i < 2; ++i) {
+        if (a[6 + i] == Py_None) continue;
+        const char *name = i ? "k_weight" : "q_weight";
+        const Tensor &w = cuda(a[6 + i], name);
+        if (w.scalar_type() != at::kFloat && w.scalar_type() != at::kBFloat16) throw Refusal{std::string(name) + " must be float32 or bfloat16"};
+        const bool each = w.dim() == 2;
+        const void *p = each ? dense(a[6 + i], name, {i ? H : Hq, D}, w.scalar_type(), q) : dense(a[6 + i], name, {D}, w.scalar_type(), q);
+        (i ? t.k_weight : t.q_weight) = p;
+        (i ? t.k_weight_dt : t.q_weight_dt) = code(w.scalar_type());
+        (i ? t.k_weight_stride : t.q_weight_stride) = each ? D : 0;
+        if (a[8] == Py_None) throw Refusal{std::string(name) + " goes with eps"};
+    }
+    if (a[8] != Py_None) t.norm = 1, t.eps = real(a[8]);
+    const int turned = PyObject_IsTrue(a[9]);
+    if (turned < 0) throw Refusal{""};
+    t.interleaved = turned;
+    t.scale = real(a[10]);
+    return t;
+}
+
+// rotate(entry, q, k, the eleven of turn_of, q_out, k_out, stream) -> (status code, q, k)
+PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+    return guarded(n_args, 17, [&]() -> PyObject * {
+        const Tensor &q = queries(a[1]);
+        Heads in[2], out[2];
+        in[0].take(a[1], "q", q, -1);
+        in[1].take(a[2], "k", q, -1);
+        const int64_t Hq = q.size(2), H = cuda(a[2], "k").size(2);
+        const aces_turn t = turn_of(a + 3, q, Hq, H);
+        if (!t.positions && !t.start) throw Refusal{"start or positions must be given"};
+        const auto entry = reinterpret_cast<Rotate>(address(a[0]));
+        const auto stream = (aces_stream_t)address(a[16]);
+        out[0].put(a[14], "q of out", q, in[0], Hq);
+        out[1].put(a[15], "k of out", q, in[1], H);
+        const aces_status s = entry(in[0].p, in[1].p, code(q.scalar_type()), in[0].stride, in[1].stride, (int)q.size(0), (int)q.size(1), (int)Hq,
+                                    (int)H, (int)q.size(3), &t, out[0].p, out[1].p, out[0].stride, out[1].stride, stream);
+        return Py_BuildValue("(iNN)", (int)s, out[0].object(), out[1].object());
+    });
+}
+
+// append_rotated(entry, cache, layer, q, k, v, start, count, the eleven of turn_of, q_out, status, stream) -> (status code, q, status)
+PyObject *append_rotated(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+    return guarded(n_args, 22, [&]() -> PyObject * {
+        const Cache c = cache_of(a[1]);
+        const Tensor &q = queries(a[3]);
+        if (q.device() != c.t.device() || q.size(0) != c.B || q.size(3) != c.D)
+            throw Refusal{"q must be [" + std::to_string(c.B) + ", n, heads, " + std::to_string(c.D) + "] on " + c.t.device().str()};
+        Heads in[3], out;
+        in[0].take(a[3], "q", q, -1);
+        in[1].take(a[4], "k", q, c.H);
+        in[2].take(a[5], "v", q, c.H);
+        const int64_t Hq = q.size(2);
+        const int n = (int)q.size(1), layer = integer(a[2], "layer");
+        const void *start = dense(a[6], "start", {c.B}, at::kInt, c.t);
+        const void *count = a[7] == Py_None ? nullptr : dense(a[7], "count", {c.B}, at::kInt, c.t);
+        const aces_turn t = turn_of(a + 8, q, Hq, c.H);
+        const auto entry = reinterpret_cast<AppendRotated>(address(a[0]));
+        const auto stream = (aces_stream_t)address(a[21]);
+        Output st;
+        st.take(a[20], "status of out", {c.B, n}, at::kInt, c.t);
+        out.put(a[19], "q of out", q, in[0], Hq);
+        st.make({c.B, n}, at::kInt, c.t);
+        const aces_status s = entry(c.t.data_ptr(), c.planes, layer, c.B, c.H, c.S, c.D, in[0].p, in[1].p, in[2].p, code(q.scalar_type()),
+                                    in[0].stride, in[1].stride, in[2].stride, (int)Hq, (const int32_t *)start, (const int32_t *)count, n, &t, out.p,
+                                    out.stride, (int32_t *)st.p, stream);
+        return Py_BuildValue("(iNN)", (int)s, out.object(), st.object());
+    });
+}
+
+PyMethodDef methods[] = {{"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotate)), METH_FASTCALL, nullptr},
+                         {"append_rotated", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_rotated)), METH_FASTCALL, nullptr},
+                         {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append)), METH_FASTCALL, nullptr},
                          {"read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(read)), METH_FASTCALL, nullptr},
                          {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

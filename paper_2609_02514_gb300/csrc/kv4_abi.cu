@@ -2,6 +2,7 @@
 #include <climits>
 
 #include "kv4_plan.cuh"
+#include "turn.cuh"
 
 using namespace aces;
 
@@ -49,6 +50,58 @@ bool many_rows(int f32, int B, int H, int n, int G) {
     const long long rows = (long long)n * G;
     return !f32 && rows > ((long long)B * H <= 32 ? 32 : 16);
 }
+
+// Checks of what a rotation is, and its part of the kernel's arguments.
+aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, const void *q, const void *k, aces_dtype dt, Turn *a) {
+    if (D != 64 && D != 128) return D < 1 ? ACES_ERR_INVALID_ARG : ACES_ERR_UNSUPPORTED;
+    if (dt != ACES_F32 && dt != ACES_BF16) return ACES_ERR_UNSUPPORTED;
+    if (!t || !q || !k || !t->inv_freq || B < 1 || n < 1 || Hq < 1 || H < 1) return ACES_ERR_INVALID_ARG;
+    if (n > INT_MAX / 4 || (long long)B * n > INT_MAX / 2 || Hq > INT_MAX / 64 || H > INT_MAX / 64) return ACES_ERR_INVALID_ARG;
+    if (t->rot_dim < 1 || t->rot_dim > D) return ACES_ERR_INVALID_ARG;
+    if (t->rot_dim % (D / 4) != 0) return ACES_ERR_UNSUPPORTED;
+    if (t->positions && (t->n_axes < 1 || t->n_axes > ACES_MAX_AXES || (t->n_axes > 1 && !t->axes))) return ACES_ERR_INVALID_ARG;
+    if (t->depth && t->depth_stride != 0 && t->depth_stride < n) return ACES_ERR_INVALID_ARG;
+    if (!(t->scale >= 0x1p-20 && t->scale <= 0x1p20)) return ACES_ERR_INVALID_ARG;
+    if (t->norm ? !(t->eps >= 1e-30 && t->eps <= 1e30) : (t->q_weight || t->k_weight)) return ACES_ERR_INVALID_ARG;
+    const size_t es = dt == ACES_F32 ? 4 : 2;
+    if ((uintptr_t)q % es || (uintptr_t)k % es) return ACES_ERR_INVALID_ARG;
+    const void *w[2] = {t->q_weight, t->k_weight};
+    const aces_dtype wt[2] = {t->q_weight_dt, t->k_weight_dt};
+    const int64_t ws[2] = {t->q_weight_stride, t->k_weight_stride};
+    for (int i = 0; i < 2; ++i) {
+        TurnWeight &o = i ? a->kw : a->qw;
+        o = {w[i], ws[i], wt[i] == ACES_F32};
+        if (!w[i]) {
+            o.h = 0;
+            continue;
+        }
+        if (wt[i] != ACES_F32 && wt[i] != ACES_BF16) return ACES_ERR_UNSUPPORTED;
+        if ((uintptr_t)w[i] % (o.f32 ? 4 : 2) || (ws[i] != 0 && ws[i] < D)) return ACES_ERR_INVALID_ARG;
+    }
+    a->freq = t->inv_freq, a->axes = t->axes, a->positions = t->positions;
+    a->start = t->start, a->base = t->base, a->depth = t->depth, a->depth_b = t->depth_stride;
+    a->R = t->rot_dim, a->n_axes = t->positions ? t->n_axes : 1, a->norm = t->norm;
+    a->eps = t->eps, a->scale = t->scale;
+    a->B = B, a->n = n, a->Hq = Hq, a->H = H;
+    return ACES_OK;
+}
+// whether no two numbers of strided outputs [B, n, heads, D] share a place
+bool apart(const int64_t *stride, int B, int n, int H, int D) {
+    int64_t st[3] = {stride[0], stride[1], stride[2]}, size[3] = {B, n, H};
+    int64_t least = D;
+    for (int left = 3; left > 0; --left) {  // the smallest stride of what is left
+        int at = -1;
+        for (int i = 0; i < 3; ++i)
+            if (size[i] > 0 && (at < 0 || st[i] < st[at])) at = i;
+        if (size[at] > 1) {
+            if (st[at] < least || st[at] > INT64_MAX / 4 / size[at]) return false;
+            least = st[at] * size[at];
+        }
+        size[at] = 0;
+    }
+    return true;
+}
+TurnHeads heads(const void *p, const int64_t *s) { return {const_cast<void *>(p), s[0], s[1], s[2]}; }
 
 }  // namespace
 
@@ -142,6 +195,50 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
     a.scale = (float)((double)scale * 1.4426950408889634 * (double)KV4_STEP);
     const auto launch = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many : launch_kv4_few;
     return launch(a, workspace, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
+}
+
+aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const int64_t *q_strides, const int64_t *k_strides, int B, int n,
+                           int Hq, int H, int D, const aces_turn *turn, void *q_out, void *k_out, const int64_t *q_out_strides,
+                           const int64_t *k_out_strides, aces_stream_t stream) {
+    Turn a = {};
+    const aces_status st = check_turn(turn, D, B, n, Hq, H, q, k, dt, &a);
+    if (st != ACES_OK) return st;
+    const size_t es = dt == ACES_F32 ? 4 : 2;
+    if (!q_out || !k_out || !q_strides || !k_strides || !q_out_strides || !k_out_strides) return ACES_ERR_INVALID_ARG;
+    if ((uintptr_t)q_out % es || (uintptr_t)k_out % es) return ACES_ERR_INVALID_ARG;
+    if (!apart(q_out_strides, B, n, Hq, D) || !apart(k_out_strides, B, n, H, D)) return ACES_ERR_INVALID_ARG;
+    if (!turn->positions && !turn->start) return ACES_ERR_INVALID_ARG;
+    a.q = heads(q, q_strides), a.k = heads(k, k_strides);
+    a.oq = heads(q_out, q_out_strides), a.ok = heads(k_out, k_out_strides);
+    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es);
+    a.ovec = on_grid(q_out, q_out_strides, es) && on_grid(k_out, k_out_strides, es);
+    return launch_turn(a, D, dt == ACES_F32, false, turn->interleaved != 0, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? ACES_OK
+               : ACES_ERR_CUDA;
+}
+
+aces_status aces_kv4_append_rotated(void *cache, int planes, int layer, int B, int H, int S, int D, const void *q, const void *k,
+                                    const void *v, aces_dtype dt, const int64_t *q_strides, const int64_t *k_strides,
+                                    const int64_t *v_strides, int Hq, const int32_t *start, const int32_t *count, int n,
+                                    const aces_turn *turn, void *q_out, const int64_t *q_out_strides, int32_t *row_status,
+                                    aces_stream_t stream) {
+    Turn a = {};
+    aces_status st = check_cache(cache, planes, layer, B, H, S, D, &a.ck, &a.cv);
+    if (st != ACES_OK) return st;
+    st = check_turn(turn, D, B, n, Hq, H, q, k, dt, &a);
+    if (st != ACES_OK) return st;
+    st = check_rows(k, v, dt, start, B, n, H);
+    if (st != ACES_OK) return st;
+    const size_t es = dt == ACES_F32 ? 4 : 2;
+    if (!q_out || !row_status || !q_strides || !k_strides || !v_strides || !q_out_strides || turn->start) return ACES_ERR_INVALID_ARG;
+    if ((uintptr_t)q_out % es || !apart(q_out_strides, B, n, Hq, D)) return ACES_ERR_INVALID_ARG;
+    a.start = start, a.count = count, a.status = row_status, a.S = S;
+    a.q = heads(q, q_strides), a.k = heads(k, k_strides), a.v = heads(v, v_strides), a.oq = heads(q_out, q_out_strides);
+    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es) && on_grid(v, v_strides, es);
+    a.ovec = on_grid(q_out, q_out_strides, es);
+    return launch_turn(a, D, dt == ACES_F32, true, turn->interleaved != 0, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? ACES_OK
+               : ACES_ERR_CUDA;
 }
 
 }  // extern "C"
