@@ -70,7 +70,7 @@ aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, c
     const int64_t ws[2] = {t->q_weight_stride, t->k_weight_stride};
     for (int i = 0; i < 2; ++i) {
         TurnWeight &o = i ? a->kw : a->qw;
-        o = {w[i], ws[i], wt[i] == ACES_F32};
+        o = {w[i], ws[i], wt[i] == ACES_F32, aligned16(w[i]) && ws[i] * (wt[i] == ACES_F32 ? 4 : 2) % 16 == 0};
         if (!w[i]) {
             o.h = 0;
             continue;
@@ -82,6 +82,7 @@ aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, c
     a->start = t->start, a->base = t->base, a->depth = t->depth, a->depth_b = t->depth_stride;
     a->R = t->rot_dim, a->n_axes = t->positions ? t->n_axes : 1, a->norm = t->norm;
     a->eps = t->eps, a->scale = t->scale;
+    a->eps32 = (float)t->eps, a->scale32 = (float)t->scale;
     a->B = B, a->n = n, a->Hq = Hq, a->H = H;
     return ACES_OK;
 }
@@ -210,8 +211,7 @@ aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const in
     if (!turn->positions && !turn->start) return ACES_ERR_INVALID_ARG;
     a.q = heads(q, q_strides), a.k = heads(k, k_strides);
     a.oq = heads(q_out, q_out_strides), a.ok = heads(k_out, k_out_strides);
-    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es);
-    a.ovec = on_grid(q_out, q_out_strides, es) && on_grid(k_out, k_out_strides, es);
+    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es) && on_grid(q_out, q_out_strides, es) && on_grid(k_out, k_out_strides, es);
     return launch_turn(a, D, dt == ACES_F32, false, turn->interleaved != 0, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
                ? ACES_OK
                : ACES_ERR_CUDA;
@@ -234,8 +234,7 @@ aces_status aces_kv4_append_rotated(void *cache, int planes, int layer, int B, i
     if ((uintptr_t)q_out % es || !apart(q_out_strides, B, n, Hq, D)) return ACES_ERR_INVALID_ARG;
     a.start = start, a.count = count, a.status = row_status, a.S = S;
     a.q = heads(q, q_strides), a.k = heads(k, k_strides), a.v = heads(v, v_strides), a.oq = heads(q_out, q_out_strides);
-    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es) && on_grid(v, v_strides, es);
-    a.ovec = on_grid(q_out, q_out_strides, es);
+    a.vec = on_grid(q, q_strides, es) && on_grid(k, k_strides, es) && on_grid(v, v_strides, es) && on_grid(q_out, q_out_strides, es);
     return launch_turn(a, D, dt == ACES_F32, true, turn->interleaved != 0, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
                ? ACES_OK
                : ACES_ERR_CUDA;

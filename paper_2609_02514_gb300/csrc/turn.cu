@@ -5,93 +5,78 @@
 //   z_u = y_u c_j - y_v s_j, z_v = y_v c_j + y_u s_j     c_j, s_j = scale (cos, sin)(p f_j)
 //
 // for the pairs j < R / 2 of channels (u, v) = (j, j + R / 2), or (2 j, 2 j + 1); p is the
-// position on the pair's axis.  Four lanes have a head's row, two of its eight groups
-// each, both channels of every pair among them: no number changes lanes, and a lane that
-// writes the cache has whole groups to quantise.  A CTA has some tokens of a sequence with
-// all their heads; their cosines and sines are made once and lie in shared memory.
+// position on the pair's axis.  As many warps as fit take the tokens in turns, one (or
+// some, where there are few heads) at a time, and wait for nobody; a token's cosines and
+// sines are made once, into shared memory.  A lane has both channels of its pairs, so no
+// number changes lanes:
+//   - of rows that stay numbers 16 channels, eight or four lanes a row, each with every
+//     so many 16 bytes of it (a load or store of the warp covers whole sectors) and with
+//     its weights, cosines and sines in registers for all heads;
+//   - of rows that go to the cache two whole groups, four lanes a row, to be quantised.
 //
-// The angle p f is taken in 64 bits (a position of 2^20 has no fraction left in 32), as
-// turns: its whole turns go before it is rounded to float32.
+// The angle p f is taken as turns, a 64-bit fraction f / (2 pi) times p (a position of 2^20
+// has no fraction left in float32): whole turns fall off by themselves.
 //
 // The cache's codes are those of z in 64 bits, so that they do not depend on how sums and
 // products were ordered here.  Float32's z is within E of that; where a quotient lies
-// closer than that to a border, or the step could be another, the row's lanes do the row
-// again in 64 bits (four rows of a thousand).
+// closer than that to a border, or the step could be another, the whole warp does the
+// row again in 64 bits (three rows of a thousand).
 #define ACES_FILE 10  // site numbers of the checked build
 #include "kv4_quant.cuh"
 #include "turn.cuh"
 
 namespace aces {
 
-constexpr int TN = 256, TW = TN / 32;
-constexpr int TOKENS = 8;  // of a CTA, at most
+constexpr int TW = 4, TN = TW * 32;
+constexpr int TOKENS = 8;  // of a warp, at most
+constexpr long long SLICE_WARPS = 24;  // an SM's warps, below which units are cut
 
 // ---------------------------------------------------------------------------
-// loads and stores of one group
-template <int G, bool F32>
-struct Raw {
-    static constexpr int N = G * (F32 ? 4 : 2) / 16;
-    uint4 w[N];
-};
+// loads and stores
 // (in place, a row is read by the lanes that write it, before they do: a plain load)
 __device__ __forceinline__ uint4 load16(const void *p) {
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
-template <int G, bool F32>
-__device__ __forceinline__ void load_raw(const void *base, long long at, bool vec, Raw<G, F32> &r) {
-    constexpr int ES = F32 ? 4 : 2;
-    const char *p = reinterpret_cast<const char *>(base) + at * ES;
-    if (vec) {
+// 16 bytes of a row: its numbers, whatever the alignment
+template <bool VEC, bool F32>
+__device__ __forceinline__ uint4 load_word(const void *base, int at) {  // at: in numbers
+    const char *p = reinterpret_cast<const char *>(base) + at * (F32 ? 4 : 2);
+    uint32_t u[4];
+    if (VEC) return load16(p);
 #pragma unroll
-        for (int i = 0; i < Raw<G, F32>::N; ++i) r.w[i] = load16(p + 16 * i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < Raw<G, F32>::N; ++i) {
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (F32) {
-                    u[j] = reinterpret_cast<const volatile uint32_t *>(p)[4 * i + j];
-                } else {
-                    const volatile unsigned short *h = reinterpret_cast<const volatile unsigned short *>(p) + 8 * i + 2 * j;
-                    u[j] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
-                }
-            }
-            r.w[i] = make_uint4(u[0], u[1], u[2], u[3]);
+    for (int j = 0; j < 4; ++j) {
+        if (F32) {
+            u[j] = reinterpret_cast<const volatile uint32_t *>(p)[j];
+        } else {
+            const volatile unsigned short *h = reinterpret_cast<const volatile unsigned short *>(p) + 2 * j;
+            u[j] = (uint32_t)h[0] | (uint32_t)h[1] << 16;
         }
     }
-}
-template <int G, bool F32>
-__device__ __forceinline__ float raw_get(const Raw<G, F32> &r, int e) {
-    return F32 ? Elem<ACES_F32>::get(r.w[e / 4], e % 4) : Elem<ACES_BF16>::get(r.w[F32 ? 0 : e / 8], e % 8);
+    return make_uint4(u[0], u[1], u[2], u[3]);
 }
 __device__ __forceinline__ uint32_t bf2_round(float a, float b) {  // low half from a
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
     return d;
 }
-template <int G, bool F32>
-__device__ __forceinline__ void store_group(void *base, long long at, bool vec, const float (&y)[G]) {
-    constexpr int ES = F32 ? 4 : 2;
-    char *p = reinterpret_cast<char *>(base) + at * ES;
+template <bool VEC, bool F32>
+__device__ __forceinline__ void store_word(void *base, int at, const float *y) {
+    char *p = reinterpret_cast<char *>(base) + at * (F32 ? 4 : 2);
+    uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < Raw<G, F32>::N; ++i) {
-        uint32_t u[4];
+    for (int j = 0; j < 4; ++j) u[j] = F32 ? __float_as_uint(y[j]) : bf2_round(y[2 * j], y[2 * j + 1]);
+    if (VEC) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) u[j] = F32 ? __float_as_uint(y[F32 ? 4 * i + j : 0]) : bf2_round(y[F32 ? 0 : 8 * i + 2 * j], y[F32 ? 0 : 8 * i + 2 * j + 1]);
-        if (vec) {
-            reinterpret_cast<uint4 *>(p)[i] = make_uint4(u[0], u[1], u[2], u[3]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (F32) {
-                    reinterpret_cast<uint32_t *>(p)[4 * i + j] = u[j];
-                } else {
-                    unsigned short *h = reinterpret_cast<unsigned short *>(p) + 8 * i + 2 * j;
-                    h[0] = (unsigned short)u[j], h[1] = (unsigned short)(u[j] >> 16);
-                }
+        for (int j = 0; j < 4; ++j) {
+            if (F32) {
+                reinterpret_cast<uint32_t *>(p)[j] = u[j];
+            } else {
+                unsigned short *h = reinterpret_cast<unsigned short *>(p) + 2 * j;
+                h[0] = (unsigned short)u[j], h[1] = (unsigned short)(u[j] >> 16);
             }
         }
     }
@@ -101,6 +86,31 @@ __device__ __forceinline__ float weight_at(const TurnWeight &w, long long at) {
     if (!w.p) return 1.0f;
     return w.f32 ? __ldg(reinterpret_cast<const float *>(w.p) + at)
                  : __uint_as_float((uint32_t)__ldg(reinterpret_cast<const unsigned short *>(w.p) + at) << 16);
+}
+
+// two float32 at once
+__device__ __forceinline__ void mul2(float &x, float &y, float a, float b) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmul.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void fma2(float &x, float &y, float a, float b, float c, float d) {  // x += a c, y += b d
+    asm("{\n\t.reg .b64 u, v, w;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\tmov.b64 w, {%4, %5};\n\t"
+        "fma.rn.f32x2 u, v, w, u;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+}
+
+// four neighbouring weights (vec: of a row on the 16-byte grid)
+__device__ __forceinline__ float4 weight4(const TurnWeight &w, long long at) {
+    if (!w.p) return make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    if (w.vec && w.f32) return __ldg(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(w.p) + at));
+    if (w.vec) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(reinterpret_cast<const unsigned short *>(w.p) + at));
+        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                           __uint_as_float(v.y & 0xFFFF0000u));
+    }
+    return make_float4(weight_at(w, at), weight_at(w, at + 1), weight_at(w, at + 2), weight_at(w, at + 3));
 }
 
 // Position of token i of sequence b on an axis.
@@ -114,16 +124,25 @@ __device__ __forceinline__ int turn_axis(const Turn &a, int j) {
     return a.axes && a.positions ? min(max(__ldg(a.axes + j), 0), a.n_axes - 1) : 0;
 }
 
-// The two groups of lane l of a row's four, and whether they turn.  Half-split pairs: one
-// group of the first half of the turned channels and its partner of the second; then
-// neighbours.
-template <int D, bool INTER>
-__device__ __forceinline__ void lane_groups(int R, int l, int &c0, int &c1) {
-    constexpr int G = D / KV4_GROUPS;
-    const int half = R / (2 * G);
-    c0 = !INTER && l < half ? l : 2 * l;
-    c1 = !INTER && l < half ? l + half : 2 * l + 1;
-}
+// Where the numbers of lane l of a row's LN lie: y[c][w * PC ..] are the PC channels from
+// chan(c, w) on, 16 bytes of a row, w < W.  Half-split pairs have their channels at one
+// place of y[0] and y[1].  GROUPS: whole groups.  FULL: all channels turn.
+template <int D, bool F32, bool INTER, bool FULL, bool GROUPS>
+struct Lane {
+    static constexpr int G = D / KV4_GROUPS, PC = F32 ? 4 : 8, LN = GROUPS ? 4 : D / 16, HC = D / (2 * LN), W = HC / PC;
+    int l, R;
+    __device__ __forceinline__ int chan(int c, int w) const {
+        const int half = FULL ? D / 2 : R / 2;
+        if (GROUPS) {
+            const int h = half / G;
+            return (!INTER && (FULL || l < h) ? l + (c ? h : 0) : 2 * l + c) * G + w * PC;
+        }
+        const int k = (l + LN * w) * PC;
+        if (INTER) return k + (c ? D / 2 : 0);
+        return FULL || k < half ? k + (c ? half : 0) : k + (c ? D / 2 : half);
+    }
+    __device__ __forceinline__ bool turns(int c, int w) const { return FULL || chan(c, w) < R; }
+};
 
 // ---------------------------------------------------------------------------
 // Codes of a group of z whose numbers are within E of the 64-bit ones: false where those
@@ -166,351 +185,511 @@ __device__ __forceinline__ bool quantise_near(float (&z)[G], float E, uint32_t (
     return none || (sure && far < 0.5f - fmaf(E, fabsf(inv), 1.0e-6f));
 }
 
-// One number of a row in 64 bits.
+// A row in 64 bits, and into the cache, by a whole warp: a lane has D / 32 neighbouring
+// channels, four lanes a group.
 template <int D, bool F32, bool INTER>
-struct Exact {
-    const Turn &a;
-    const void *x;
-    long long at;   // of the row
-    TurnWeight wt;  // and of its weights
-    long long wat;
-    int b, i;
-    double r;       // 1 / the norm
-    __device__ __forceinline__ double in(int d) const {
-        const long long j = at + d;
-        return F32 ? reinterpret_cast<const float *>(x)[j]
-                   : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(x)[j] << 16);
+static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h, uint8_t *row) {
+    constexpr int G = D / KV4_GROUPS, CH = D / 32;
+    constexpr uint32_t ALL = 0xffffffffu;
+    const int lane = threadIdx.x & 31, d0 = lane * CH, half = a.R / 2;
+    const long long at = b * a.k.b + i * a.k.i + h * a.k.h + d0;
+    double y[CH], ss = 0.0;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        y[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
+                   : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
+        ss = fma(y[e], y[e], ss);
     }
-    __device__ __forceinline__ double y(int d) const { return a.norm ? in(d) * weight_at(wt, wat + d) * r : in(d); }  // (x w is exact: equal ones stay equal)
-    __device__ __forceinline__ double z(int d) const {
-        if (d >= a.R) return y(d);
-        const int half = a.R / 2, j = INTER ? d >> 1 : d % half;
-        const bool second = INTER ? d & 1 : d >= half;
-        const double u = y(INTER ? 2 * j : j), v = y(INTER ? 2 * j + 1 : j + half);
-        double sn, cs;
-        sincos((double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j), &sn, &cs);
-        return (second ? v * cs + u * sn : u * cs - v * sn) * a.scale;
+    if (a.norm) {
+        for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(ALL, ss, x);
+        const double r = 1.0 / sqrt(ss / D + a.eps);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) y[e] = y[e] * weight_at(a.kw, h * a.kw.h + d0 + e) * r;  // (x w is exact: equal ones stay equal)
     }
-};
-
-// Codes of a row's groups g[0], g[1] whose float32 numbers z (within E of the 64-bit ones)
-// leave them open: the numbers that may be a group's first of largest magnitude, and those
-// next to a border, are worked out in 64 bits.  By the row's four lanes, which share its
-// sum of squares.
-template <int D, bool F32, bool INTER>
-static __device__ __noinline__ void exact_groups(Exact<D, F32, INTER> row, uint32_t mask, const int *g, const float *z, const float *E,
-                                                 uint32_t *w, float *t_out) {
-    constexpr int G = D / KV4_GROUPS;
-    if (row.a.norm) {
-        double ss = 0.0;
-        for (int c = 0; c < 2; ++c)
-            for (int e = 0; e < G; ++e) {
-                const double f = row.in(g[c] * G + e);
-                ss = fma(f, f, ss);
-            }
-        ss += __shfl_xor_sync(mask, ss, 1);
-        ss += __shfl_xor_sync(mask, ss, 2);
-        row.r = 1.0 / sqrt(ss / D + row.a.eps);
+    // A lane works out half of its pairs' cosines and sines: interleaved pairs are its own,
+    // the others are shared with the lane that has their other channels.
+    const bool turns = d0 < a.R, second = !INTER && d0 >= half;
+    const int other = INTER || !turns ? lane : second ? lane - half / CH : lane + half / CH;
+    double sn[CH / 2], cn[CH / 2];
+#pragma unroll
+    for (int x = 0; x < CH / 2; ++x) {
+        sn[x] = 0.0, cn[x] = 1.0;
+        if (!turns) continue;
+        const int j = INTER ? d0 / 2 + x : second ? d0 - half + CH / 2 + x : d0 + x;
+        sincos((double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j), &sn[x], &cn[x]);
+    }
+    double z[CH];
+    if (INTER) {
+#pragma unroll
+        for (int x = 0; x < CH / 2; ++x) {
+            const double u = y[2 * x], v = y[2 * x + 1];
+            z[2 * x] = u * cn[x] - v * sn[x];
+            z[2 * x + 1] = v * cn[x] + u * sn[x];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+            const int x = e % (CH / 2);
+            const bool mine = (e >= CH / 2) == second;
+            const double yo = __shfl_sync(ALL, y[e], other), so = __shfl_sync(ALL, sn[x], other), co = __shfl_sync(ALL, cn[x], other);
+            const double s = mine ? sn[x] : so, c = mine ? cn[x] : co;
+            z[e] = second ? y[e] * c + yo * s : y[e] * c - yo * s;
+        }
     }
     constexpr double CAP = (double)KV4_CAP;
-    for (int c = 0; c < 2; ++c) {
-        const float *zc = z + c * G;
-        float big = 0.0f;
-        bool fine = true;
-        for (int e = 0; e < G; ++e) {
-            big = fmaxf(big, fabsf(zc[e]));
-            fine &= fabsf(zc[e]) <= FLT_MAX;
-        }
-        if (!fine) continue;  // what is not finite is not open
-        double top = 0.0;
-        for (int e = 0; e < G; ++e)
-            if (fabsf(zc[e]) >= fminf(big, KV4_CAP) - 2.0f * E[c]) {
-                const double v = fmin(fmax(row.z(g[c] * G + e), -CAP), CAP);
-                if (fabs(v) > fabs(top)) top = v;
-            }
-        // -top / 2^19 in five significant bits, ties to even
-        double t = 0.0;
-        if (fabs(top) >= (double)KV4_TINY) {
-            const unsigned long long bits = (unsigned long long)__double_as_longlong(-top * 1.9073486328125e-06);
-            unsigned long long m = bits & 0x7FFFFFFFFFFFFFFFull;
-            m = (m + 0x7FFFFFFFFFFFull + ((m >> 48) & 1ull)) & ~0xFFFFFFFFFFFFull;
-            t = __longlong_as_double((long long)((bits & 0x8000000000000000ull) | m));
-        }
-        t_out[c] = (float)t;
-        const float s = (float)t * KV4_STEP, inv = s == 0.0f ? 0.0f : __frcp_rn(s);
-        for (int j = 0; j < G / 8; ++j) {
-            uint32_t word = 0u;
-            for (int e = 0; e < 8; ++e) {
-                const float x = fminf(fmaxf(zc[8 * j + e], -KV4_CAP), KV4_CAP), q = x * inv;
-                float r = rintf(q);
-                if (s != 0.0f && fabsf(q - r) >= 0.5f - fmaf(E[c], fabsf(inv), 1.5e-6f))
-                    r = (float)rint(fmin(fmax(row.z(g[c] * G + 8 * j + e), -CAP), CAP) / (double)s);
-                word |= (uint32_t)((int)fminf(fmaxf(r, -8.0f), 7.0f) + 8) << (4 * (e >> 1) + 16 * (e & 1));
-            }
-            w[c * (G / 8) + j] = word;
-        }
+    double top = 0.0;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        z[e] = turns ? z[e] * a.scale : y[e];
+        z[e] = z[e] == z[e] ? fmin(fmax(z[e], -CAP), CAP) : 0.0;
+        if (fabs(z[e]) > fabs(top)) top = z[e];  // the first of the largest
     }
+#pragma unroll
+    for (int x = 1; x < 4; x <<= 1) {
+        const double o = __shfl_xor_sync(ALL, top, x);
+        if (lane & x ? fabs(o) >= fabs(top) : fabs(o) > fabs(top)) top = o;
+    }
+    // -top / 2^19 in five significant bits, ties to even
+    double t = 0.0;
+    if (fabs(top) >= (double)KV4_TINY) {
+        const unsigned long long bits = (unsigned long long)__double_as_longlong(-top * 1.9073486328125e-06);
+        unsigned long long m = bits & 0x7FFFFFFFFFFFFFFFull;
+        m = (m + 0x7FFFFFFFFFFFull + ((m >> 48) & 1ull)) & ~0xFFFFFFFFFFFFull;
+        t = __longlong_as_double((long long)((bits & 0x8000000000000000ull) | m));
+    }
+    const double s = t * (double)KV4_STEP;
+    uint32_t w = 0u;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        const int c = (d0 + e) & 7;  // of its word
+        const double r = s == 0.0 ? 0.0 : fmin(fmax(rint(z[e] / s), -8.0), 7.0);
+        w |= (uint32_t)((int)r + 8) << (4 * (c >> 1) + 16 * (c & 1));
+    }
+#pragma unroll
+    for (int x = 1; x < 8 / CH; x <<= 1) w |= __shfl_xor_sync(ALL, w, x);
+    if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = w;
+    if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint((float)t) >> 16);
 }
 
 // ---------------------------------------------------------------------------
-template <int D, bool F32, bool APPEND, bool INTER>
-__global__ void __launch_bounds__(TN) k_turn(Turn a, int lt) {
-    constexpr int G = D / KV4_GROUPS, RB = kv4_row_bytes(D), P = G + 4;  // a group's place in shared memory: no two lanes on a bank
-    __shared__ __align__(16) float cs[TOKENS][2][4 * P], wts[2][KV4_GROUPS * P];
-    __shared__ int st[TOKENS];
-    const int T = 1 << lt, per = (a.n + T - 1) >> lt;  // CTAs of a sequence
-    const int b = blockIdx.x / per, i0 = (blockIdx.x - b * per) * T, tokens = min(T, a.n - i0);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l = lane & 3;
-    const uint32_t mask = 0xFu << (lane & ~3);
-    // eight rows of one kind a warp: queries, then keys, then values
-    const int oq = (tokens * a.Hq + 7) >> 3, ok = (tokens * a.H + 7) >> 3, octets = oq + (APPEND ? 2 : 1) * ok;
-    int c0, c1;
-    lane_groups<D, INTER>(a.R, l, c0, c1);
+template <bool VEC, bool F32, class My>
+__device__ __forceinline__ void load_row(const My my, const TurnHeads &from, int b, int i, int h, uint4 (&raw)[2][My::W]) {
+    const char *p = reinterpret_cast<const char *>(from.p) + (b * from.b + i * from.i + h * from.h) * (F32 ? 4 : 2);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int w = 0; w < My::W; ++w) raw[c][w] = load_word<VEC, F32>(p, my.chan(c, w));
+}
+template <bool F32, int W, int HC>
+__device__ __forceinline__ void numbers(const uint4 (&raw)[2][W], float (&y)[2][HC]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < HC; ++e) y[c][e] = Elem<F32 ? ACES_F32 : ACES_BF16>::get(raw[c][e / (F32 ? 4 : 8)], e % (F32 ? 4 : 8));
+}
 
-    // the row of this lane in an octet: kind, token, head; false for none
-    auto place = [&](int o, int &kind, int &tok, int &h) {
-        kind = o < oq ? 0 : o < oq + ok ? 1 : 2;
-        const int r = (o - (kind == 0 ? 0 : kind == 1 ? oq : oq + ok)) * 8 + (lane >> 2), heads = kind == 0 ? a.Hq : a.H;
-        tok = r / heads;
-        h = r - tok * heads;
-        return tok < tokens;
-    };
-    Raw<G, F32> raw[2];
-    auto fetch = [&](int o) {
-        int kind, tok, h;
-        if (o >= octets || !place(o, kind, tok, h)) return;
-        const TurnHeads &x = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-        const long long at = b * x.b + (i0 + tok) * x.i + h * x.h;
-        load_raw<G, F32>(x.p, at + c0 * G, a.vec, raw[0]);
-        load_raw<G, F32>(x.p, at + c1 * G, a.vec, raw[1]);
-    };
-    fetch(warp);
-
-    for (int x = tid; x < tokens * (a.R / 2); x += TN) {
-        const int tok = x / (a.R / 2), j = x - tok * (a.R / 2);
-        const double p = turn_position(a, b, i0 + tok, turn_axis(a, j));
-        const double angle = p * (double)__ldg(a.freq + j);
-        // turns: 1 / (2 pi) in two parts
-        const double hi = angle * 0.15915494309189535, lo = fma(angle, 0.15915494309189535, -hi) + angle * -9.839338337591493e-18;
-        float sn, cn;
-        sincospif(2.0f * (float)(hi - rint(hi) + lo), &sn, &cn);
-        const int at = j / G * P + j % G;
-        cs[tok][0][at] = cn * (float)a.scale, cs[tok][1][at] = sn * (float)a.scale;
+// 1 / the norm of a row, whose lanes are LN neighbours.  Numbers whose squares pass
+// float32 become 2^-70 of themselves.
+template <int D, int LN, int HC>
+__device__ __forceinline__ float inv_norm(const Turn &a, float (&y)[2][HC]) {
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = y[0][e];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) mul2(p[e], p[e + 1], p[e], p[e + 1]);
+#pragma unroll
+    for (int e = 8; e < 2 * HC; e += 2) {
+        const float *v = &y[e / HC][e % HC];
+        fma2(p[e % 8], p[e % 8 + 1], v[0], v[1], v[0], v[1]);
     }
-    if (a.norm)
-        for (int x = tid; x < 2 * D; x += TN) {
-            const int which = x / D, d = x - which * D;
-            const TurnWeight &w = which ? a.kw : a.qw;
-            if (w.h == 0) wts[which][d / G * P + d % G] = weight_at(w, d);
-        }
-    if (APPEND && tid < T) st[tid] = 0;
-    __syncthreads();
-    const int start = APPEND ? a.start[b] : 0, cnt = APPEND && a.count ? a.count[b] : a.n;
-
-    for (int o = warp; o < octets; o += TW) {
-        int kind, tok, h;
-        const bool live = place(o, kind, tok, h);
-        const int i = i0 + tok;
-        float y[2][G];
+    float ss = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+#pragma unroll
+    for (int x = 1; x < LN; x <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
+    const bool huge = !(ss < 1e37f);
+    float eps = a.eps32;
+    if (__any_sync(0xffffffffu, huge)) {
+        float s2 = 0.0f;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int e = 0; e < G; ++e) y[c][e] = live ? raw_get<G, F32>(raw[c], e) : 0.0f;
-        fetch(o + TW);
-        bool bad = false;
-        uint32_t w[2][G / 8];
-        float t[2];
-        const long long pos = APPEND ? (long long)start + i : 0;
-        const bool in = APPEND && live && i < cnt && pos >= 0 && pos < a.S;
-        if (APPEND && kind == 2) {
-            if (!in) {
-                if (live && i < cnt && h == 0 && l == 0) atomicOr(&st[tok], ACES_ROW_RANGE);
-                continue;
+            for (int e = 0; e < HC; ++e) {
+                if (huge) y[c][e] *= 0x1p-70f;
+                s2 = fmaf(y[c][e], y[c][e], s2);
             }
-            bool bad1;
-            quantise<G, F32>(y[0], w[0], &t[0], &bad);
-            quantise<G, F32>(y[1], w[1], &t[1], &bad1);
-            bad |= bad1;
-        } else {
-            const int tk = live ? tok : 0;
+#pragma unroll
+        for (int x = 1; x < LN; x <<= 1) s2 += __shfl_xor_sync(0xffffffffu, s2, x);
+        if (huge) ss = s2, eps = 0.0f;
+    }
+    // (a Newton step behind the approximation: within 1.5 * 2^-24)
+    const float m = fmaf(ss, 1.0f / D, eps), r = rsqrtf(m);
+    return m <= FLT_MAX ? fmaf(-0.5f * r, fmaf(m * r, r, -1.0f), r) : r;
+}
+
+// Turns four numbers of y[c] from e on: half-split pairs with those of y[1] (c = 0), or
+// interleaved among themselves; cc and sc: their four or two cosines and sines.
+template <bool INTER, int HC>
+__device__ __forceinline__ void turn4(float (&y)[2][HC], int c, int e, const float *cc, const float *sc) {
+    if (INTER) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float u = y[c][e + 2 * x], v = y[c][e + 2 * x + 1];
+            y[c][e + 2 * x] = fmaf(u, cc[x], -(v * sc[x]));
+            y[c][e + 2 * x + 1] = fmaf(v, cc[x], u * sc[x]);
+        }
+    } else {
+#pragma unroll
+        for (int x = 0; x < 4; x += 2) {
+            const float u0 = y[0][e + x], u1 = y[0][e + x + 1], v0 = y[1][e + x], v1 = y[1][e + x + 1];
+            float m0 = v0, m1 = v1, n0 = u0, n1 = u1;
+            mul2(m0, m1, sc[x], sc[x + 1]);
+            mul2(n0, n1, sc[x], sc[x + 1]);
+            y[0][e + x] = fmaf(u0, cc[x], -m0), y[0][e + x + 1] = fmaf(u1, cc[x + 1], -m1);
+            fma2(n0, n1, v0, v1, cc[x], cc[x + 1]);
+            y[1][e + x] = n0, y[1][e + x + 1] = n1;
+        }
+    }
+}
+
+// Heads of one token that stay numbers, steps [s0, s1) of 32 / LN heads each, the next
+// but one step's loads under way.  ws: weights that all heads share; cs: the token's cosines
+// and sines.
+template <int D, bool F32, bool INTER, bool VEC, bool FULL>
+__device__ __forceinline__ void turn_heads(const Turn &a, const TurnHeads &from, const TurnHeads &to, const TurnWeight &wt, const float *ws,
+                                           const float *cs, int b, int i, int heads, int s0, int s1) {
+    using My = Lane<D, F32, INTER, FULL, false>;
+    constexpr int HC = My::HC, PC = My::PC, LN = My::LN, RW = 32 / LN, W = My::W;
+    static_assert(HC == 8, "16 channels a lane");
+    const int lane = threadIdx.x & 31;
+    const My my{lane % LN, FULL ? D : a.R};
+    constexpr int DEPTH = F32 ? 1 : 2;  // steps under way
+    constexpr int ES = F32 ? 4 : 2;
+    uint4 raw[DEPTH][2][W];
+    const int row = lane / LN;
+    const char *src = reinterpret_cast<const char *>(from.p) + (b * from.b + i * from.i) * ES;
+    char *dst = reinterpret_cast<char *>(to.p) + (b * to.b + i * to.i) * ES;
+    // (lanes without a head have the last one's numbers, and write nothing)
+    auto fetch = [&](int s, uint4 (&r)[2][W]) {
+        if (s >= s1) return;
+        const char *p = src + min(s * RW + row, heads - 1) * from.h * ES;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int w = 0; w < W; ++w) r[c][w] = load_word<VEC, F32>(p, my.chan(c, w));
+    };
+#pragma unroll
+    for (int p = 0; p < DEPTH; ++p) fetch(s0 + p, raw[p]);
+    // A pair's turn and weights in one: z_u = x_u ta + x_v tb, z_v = x_v tc + x_u td.  Pair
+    // e: y[0][e], y[1][e], or interleaved y[e / 4][2 (e % 4)] and its neighbour.  Numbers
+    // that do not turn have ta and tc, their weights.
+    float ta[HC], tb[HC], tc[HC], td[HC];
+    auto tables = [&](int h) {
+#pragma unroll
+        for (int e = 0; e < HC; e += 4) {
+            float wu[4] = {1.0f, 1.0f, 1.0f, 1.0f}, wv[4] = {1.0f, 1.0f, 1.0f, 1.0f}, cc[4] = {1.0f, 1.0f, 1.0f, 1.0f}, sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const int c = INTER ? e / 4 : 0, n0 = INTER ? 0 : e;  // numbers y[c][n0 ..]
+            const int d = my.chan(c, n0 / PC) + n0 % PC, dv = INTER ? my.chan(c, 4 / PC) + 4 % PC : my.chan(1, n0 / PC) + n0 % PC;
             if (a.norm) {
-                float p[8];
+                const float4 p = wt.h == 0 ? *reinterpret_cast<const float4 *>(ws + d) : weight4(wt, h * wt.h + d);
+                const float4 q = wt.h == 0 ? *reinterpret_cast<const float4 *>(ws + dv) : weight4(wt, h * wt.h + dv);
+                if (INTER) {
+                    wu[0] = p.x, wv[0] = p.y, wu[1] = p.z, wv[1] = p.w, wu[2] = q.x, wv[2] = q.y, wu[3] = q.z, wv[3] = q.w;
+                } else {
+                    wu[0] = p.x, wu[1] = p.y, wu[2] = p.z, wu[3] = p.w, wv[0] = q.x, wv[1] = q.y, wv[2] = q.z, wv[3] = q.w;
+                }
+            }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = y[0][e] * y[0][e];
+            for (int x = 0; x < 4; x += 2) {  // (interleaved pairs of float32 may have one 16 bytes that turn and one that do not)
+                const int n = INTER ? 2 * x : e + x, at = my.chan(c, n / PC) + n % PC;
+                if (!my.turns(c, n / PC)) continue;
+                const float2 cv = *reinterpret_cast<const float2 *>(cs + (INTER ? at / 2 : at));
+                const float2 sv = *reinterpret_cast<const float2 *>(cs + D / 2 + (INTER ? at / 2 : at));
+                cc[x] = cv.x, cc[x + 1] = cv.y, sc[x] = sv.x, sc[x + 1] = sv.y;
+            }
 #pragma unroll
-                for (int e = 8; e < 2 * G; ++e) p[e % 8] = fmaf(y[e / G][e % G], y[e / G][e % G], p[e % 8]);
-                float ss = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                ss += __shfl_xor_sync(0xffffffffu, ss, 1);
-                ss += __shfl_xor_sync(0xffffffffu, ss, 2);
-                const bool huge = !(ss < 1e37f);
-                float eps = (float)a.eps;
-                if (__any_sync(0xffffffffu, huge)) {  // squares beyond float32: of numbers times 2^-70
-                    float s2 = 0.0f;
+            for (int x = 0; x < 4; ++x) ta[e + x] = wu[x] * cc[x], tb[e + x] = -(wv[x] * sc[x]), tc[e + x] = wv[x] * cc[x], td[e + x] = wu[x] * sc[x];
+        }
+    };
+    if (!a.norm || wt.h == 0) tables(0);
+    auto step = [&](int s, uint4 (&r)[2][W]) {
+        const int h = s * RW + row;
+        float y[2][HC];
+        numbers<F32>(r, y);
+        fetch(s + DEPTH, r);
+        float in = 1.0f;
+        if (a.norm) {
+            in = inv_norm<D, LN>(a, y);
+            if (wt.h != 0) tables(min(h, heads - 1));
+        }
+#pragma unroll
+        for (int e = 0; e < HC; e += 2) {
+            const int c = INTER ? e / 4 : 0, n = INTER ? 2 * (e % 4) : e;
+            float &u0 = y[c][n], &u1 = INTER ? y[c][n + 2] : y[0][n + 1], &v0 = INTER ? y[c][n + 1] : y[1][n], &v1 = INTER ? y[c][n + 3] : y[1][n + 1];
+            float p0 = u0, p1 = u1, q0 = v0, q1 = v1;
+            mul2(p0, p1, ta[e], ta[e + 1]);
+            mul2(q0, q1, tc[e], tc[e + 1]);
+            if (my.turns(c, n / PC)) {
+                fma2(p0, p1, v0, v1, tb[e], tb[e + 1]);
+                fma2(q0, q1, u0, u1, td[e], td[e + 1]);
+            }
+            if (a.norm) {
+                mul2(p0, p1, in, in);
+                mul2(q0, q1, in, in);
+            }
+            u0 = p0, u1 = p1, v0 = q0, v1 = q1;
+        }
+        if (h >= heads) return;
+        char *p = dst + h * to.h * ES;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int w = 0; w < W; ++w) store_word<VEC, F32>(p, my.chan(c, w), y[c] + w * PC);
+    };
+#pragma unroll 1
+    for (int s = s0; s < s1; s += DEPTH) {
+#pragma unroll
+        for (int p = 0; p < DEPTH; ++p)
+            if (p == 0 || s + p < s1) step(s + p, raw[p]);
+    }
+}
+
+constexpr int TURN_CTAS = 4;  // an SM
+
+// VEC: every 16 bytes lie on their grid; FULL: all channels turn.
+template <int D, bool F32, bool APPEND, bool INTER, bool VEC, bool FULL>
+__global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slices) {
+    constexpr int G = D / KV4_GROUPS, RB = kv4_row_bytes(D), RW = 512 / D;  // RW: heads of a step that stay numbers
+    using My = Lane<D, F32, INTER, FULL, true>;
+    constexpr int PC = My::PC;
+    extern __shared__ __align__(16) float tables[];  // [warp]: weights of queries and keys [D], then [token] cosines, sines [D / 2]
+    __shared__ int sts[TW][TOKENS];
+    const int T = 1 << lt, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, R = FULL ? D : a.R;
+    float *ws = tables, *cs = tables + 2 * D + warp * (T * D);
+    int *st = sts[warp];
+    const My my{lane & 3, R};
+
+    // The lane's pairs, lane and lane + 32: 2^64 f / (2 pi), whose whole turns do not count
+    uint32_t fh[2] = {0u, 0u}, fl[2] = {0u, 0u};
+    int axis[2] = {0, 0};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int j = lane + 32 * x;
+        if (j >= R / 2) continue;
+        const double f = __ldg(a.freq + j), hi = f * 0.15915494309189535;
+        const double lo = fma(f, 0.15915494309189535, -hi) + f * -9.839338337591493e-18;
+        const unsigned long long u = __double2ull_rz((hi - floor(hi)) * 0x1p64) + (unsigned long long)__double2ll_rn(lo * 0x1p64);
+        fh[x] = (uint32_t)(u >> 32), fl[x] = (uint32_t)u;
+        axis[x] = turn_axis(a, j);
+    }
+    if (a.norm)  // weights that all heads share
+        for (int y = 4 * threadIdx.x; y < 2 * D; y += 4 * TN) {
+            const TurnWeight &w = y < D ? a.qw : a.kw;
+            if (w.h == 0) *reinterpret_cast<float4 *>(ws + y) = weight4(w, y % D);
+        }
+    __syncthreads();
+
+    // units: some tokens of a sequence, and a share of their rows
+    const uint32_t per = (uint32_t)(a.n + T - 1) >> lt, units = (uint32_t)a.B * per * slices;
+#pragma unroll 1
+    for (uint32_t x = blockIdx.x * TW + warp; x < units; x += gridDim.x * TW) {
+        const uint32_t unit = slices > 1 ? x / slices : x;
+        const int slice = (int)(x - unit * slices), b = (int)(unit / per), i0 = (int)(unit - b * per) * T, tokens = min(T, a.n - i0);
+        // The warp's share: of rows for the cache, eight at a time, keys then values, all in the
+        // first slice, which has the tokens' status; of the others steps of every token.
+        const int ok = (tokens * a.H + 7) >> 3, ks = APPEND ? 0 : (a.H + RW - 1) / RW, steps = ks + (a.Hq + RW - 1) / RW;
+        int s0 = 0, s1 = steps;
+        if (slices > 1) {
+            const int first = APPEND ? 1 : 0;  // slices without steps
+            s0 = slice < first ? 0 : steps * (slice - first) / (slices - first);
+            s1 = slice < first ? 0 : steps * (slice - first + 1) / (slices - first);
+        }
+        const int octets = APPEND && slice == 0 ? 2 * ok : 0;
+
+        // The row of this lane in an octet: token, head.  Lanes without one (false) have the
+        // last one's numbers, and write nothing.
+        auto place = [&](int o, int &tok, int &h) {
+            const int r = (o < ok ? o : o - ok) * 8 + (lane >> 2), rr = min(r, tokens * a.H - 1);
+            tok = tokens == 1 ? 0 : rr / a.H;
+            h = rr - tok * a.H;
+            return r == rr;
+        };
+        uint4 raw[2][My::W];
+        auto fetch = [&](int o) {
+            int tok, h;
+            if (o >= octets) return;
+            place(o, tok, h);
+            load_row<VEC, F32>(my, o < ok ? a.k : a.v, b, i0 + tok, h, raw);
+        };
+        if (APPEND) fetch(0);
+
+        __syncwarp();  // the last unit's tables are read
+#pragma unroll 1
+        for (int tok = 0; tok < tokens; ++tok)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int j = lane + 32 * y;
+                if (j >= R / 2) continue;
+                const uint32_t p = (uint32_t)turn_position(a, b, i0 + tok, axis[y]);
+                const uint32_t turns = p * fh[y] + __umulhi(p, fl[y]) - (p >> 31 ? fl[y] : 0u);
+                float sn, cn;
+                sincospif((float)(int)turns * 0x1p-31f, &sn, &cn);
+                cs[tok * D + j] = cn * a.scale32, cs[tok * D + D / 2 + j] = sn * a.scale32;
+            }
+        if (APPEND && lane < TOKENS) st[lane] = 0;
+        __syncwarp();
+
+        // (keys, then queries; of a token after another)
+#pragma unroll 1
+        for (int y = APPEND ? 1 : 0; y < 2 * tokens; y += APPEND ? 2 : 1) {
+            const int q = y & 1, tok = y >> 1, from = q ? max(s0 - ks, 0) : s0, to = q ? s1 - ks : min(s1, ks);
+            if (from < to)
+                turn_heads<D, F32, INTER, VEC, FULL>(a, q ? a.q : a.k, q ? a.oq : a.ok, q ? a.qw : a.kw, ws + (q ? 0 : D), cs + tok * D, b, i0 + tok,
+                                                     q ? a.Hq : a.H, from, to);
+        }
+        if (!APPEND) continue;
+
+        const int start = a.start[b], cnt = a.count ? a.count[b] : a.n;
+#pragma unroll 1
+        for (int o = 0; o < octets; ++o) {
+            int tok, h;
+            const bool live = place(o, tok, h), keys = o < ok;
+            const int i = i0 + tok;
+            float y[2][G];
+            numbers<F32>(raw, y);
+            fetch(o + 1);
+            bool bad = false, bad1 = false, sure = true;
+            uint32_t w[2][G / 8];
+            float t[2];
+            const long long pos = (long long)start + i;
+            const bool mine = live && i < cnt, in = mine && pos >= 0 && pos < a.S;
+            if (!keys) {
+                quantise<G, F32>(y[0], w[0], &t[0], &bad);
+                quantise<G, F32>(y[1], w[1], &t[1], &bad1);
+            } else {
+                if (a.norm) {
+                    const float r = inv_norm<D, 4>(a, y);
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
-                        for (int e = 0; e < G; ++e) {
-                            if (huge) y[c][e] *= 0x1p-70f;
-                            s2 = fmaf(y[c][e], y[c][e], s2);
+                        for (int e = 0; e < G; e += 4) {
+                            const int d = my.chan(c, e / PC) + e % PC;
+                            float4 v = a.kw.h == 0 ? *reinterpret_cast<const float4 *>(ws + D + d) : weight4(a.kw, h * a.kw.h + d);
+                            mul2(v.x, v.y, r, r);
+                            mul2(v.z, v.w, r, r);
+                            mul2(y[c][e], y[c][e + 1], v.x, v.y);
+                            mul2(y[c][e + 2], y[c][e + 3], v.z, v.w);
                         }
-                    s2 += __shfl_xor_sync(0xffffffffu, s2, 1);
-                    s2 += __shfl_xor_sync(0xffffffffu, s2, 2);
-                    if (huge) ss = s2, eps = 0.0f;
                 }
-                const float r = __frsqrt_rn(fmaf(ss, 1.0f / D, eps));
-                const TurnWeight &wt = kind ? a.kw : a.qw;
-                const float *ws = wts[kind];
+                // Float32's z is within 14 u = 14 * 2^-24 of the 64-bit one, relative to the length h
+                // of its pair: the sum of squares 9 u (four in a row, three and two levels more), half
+                // of which shows in the root, the mean with eps 0.5 u, the root, r w and its product
+                // with x 1 u each: 8 u; a product of the two and their sum 2 u; cosine and sine 1 u and
+                // 2 pi 2^-26 < 1.6 u of their angle, absolute, for both together 2^0.5 as much of h:
+                // 3.7 u.  With the scale's two roundings below 16 u.
+                // (E: the largest square of a group, or of what turns of pairs among both)
+                float E[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int g = c ? c1 : c0;
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < G; e += 2) {
+                        if (INTER || !my.turns(c, e / PC))
+                            E[c] = fmaxf(E[c], fmaf(y[c][e], y[c][e], y[c][e + 1] * y[c][e + 1]));
+                        else if (c == 0)
+                            E[0] = fmaxf(E[0], fmaxf(fmaf(y[0][e], y[0][e], y[1][e] * y[1][e]), fmaf(y[0][e + 1], y[0][e + 1], y[1][e + 1] * y[1][e + 1])));
+                    }
+                if (!INTER && my.turns(0, 0)) E[1] = E[0];
+#pragma unroll
+                for (int c = 0; c < (INTER ? 2 : 1); ++c)
 #pragma unroll
                     for (int e = 0; e < G; e += 4) {
-                        float4 v;
-                        if (wt.h == 0) {
-                            v = *reinterpret_cast<const float4 *>(ws + g * P + e);
+                        if (!my.turns(c, e / PC)) continue;
+                        const float *cp = cs + tok * D + (my.chan(c, e / PC) + e % PC) / (INTER ? 2 : 1);
+                        float cc[4], sc[4];
+                        if (INTER) {
+                            const float2 cv = *reinterpret_cast<const float2 *>(cp), sv = *reinterpret_cast<const float2 *>(cp + D / 2);
+                            cc[0] = cv.x, cc[1] = cv.y, sc[0] = sv.x, sc[1] = sv.y;
                         } else {
-                            const long long at = (live ? h : 0) * wt.h + g * G + e;
-                            v = make_float4(weight_at(wt, at), weight_at(wt, at + 1), weight_at(wt, at + 2), weight_at(wt, at + 3));
+                            const float4 cv = *reinterpret_cast<const float4 *>(cp), sv = *reinterpret_cast<const float4 *>(cp + D / 2);
+                            cc[0] = cv.x, cc[1] = cv.y, cc[2] = cv.z, cc[3] = cv.w, sc[0] = sv.x, sc[1] = sv.y, sc[2] = sv.z, sc[3] = sv.w;
                         }
-                        y[c][e] *= r * v.x, y[c][e + 1] *= r * v.y, y[c][e + 2] *= r * v.z, y[c][e + 3] *= r * v.w;
+                        turn4<INTER>(y, c, e, cc, sc);
                     }
-                }
-            }
-            float E[2] = {0.0f, 0.0f};  // the largest square (of a pair that turns: of both its numbers)
-            auto largest = [&](float &m, float u, float v) { m = fmaxf(m, fmaf(u, u, v * v)); };
-            const bool keys = APPEND && kind == 1;
-            if (!INTER) {
-                if (c0 < a.R / (2 * G)) {
-                    const float *cp = cs[tk][0] + c0 * P, *sp = cs[tk][1] + c0 * P;
+                float near[2];
 #pragma unroll
-                    for (int e = 0; e < G; e += 4) {
-                        const float4 cv = *reinterpret_cast<const float4 *>(cp + e), sv = *reinterpret_cast<const float4 *>(sp + e);
-                        const float cc[4] = {cv.x, cv.y, cv.z, cv.w}, sc[4] = {sv.x, sv.y, sv.z, sv.w};
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const float u = y[0][e + x], v = y[1][e + x];
-                            if (keys) largest(E[0], u, v);
-                            y[0][e + x] = fmaf(u, cc[x], -(v * sc[x]));
-                            y[1][e + x] = fmaf(v, cc[x], u * sc[x]);
-                        }
-                    }
-                    E[1] = E[0];
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int g = c ? c1 : c0;
-                    if (g * G >= a.R) continue;
-                    const int j0 = g * (G / 2);
-                    const float *cp = cs[tk][0] + j0 / G * P + j0 % G, *sp = cs[tk][1] + j0 / G * P + j0 % G;
-#pragma unroll
-                    for (int e = 0; e < G; e += 8) {
-                        const float4 cv = *reinterpret_cast<const float4 *>(cp + e / 2), sv = *reinterpret_cast<const float4 *>(sp + e / 2);
-                        const float cc[4] = {cv.x, cv.y, cv.z, cv.w}, sc[4] = {sv.x, sv.y, sv.z, sv.w};
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const float u = y[c][e + 2 * x], v = y[c][e + 2 * x + 1];
-                            if (keys) largest(E[c], u, v);
-                            y[c][e + 2 * x] = fmaf(u, cc[x], -(v * sc[x]));
-                            y[c][e + 2 * x + 1] = fmaf(v, cc[x], u * sc[x]);
-                        }
-                    }
-                }
-            }
-            if (!APPEND || kind == 0) {
-                if (live) {
-                    const TurnHeads &x = kind == 0 ? a.oq : a.ok;
-                    const long long at = b * x.b + i * x.i + h * x.h;
-                    store_group<G, F32>(x.p, at + c0 * G, a.ovec, y[0]);
-                    store_group<G, F32>(x.p, at + c1 * G, a.ovec, y[1]);
-                }
-                continue;
-            }
-            // Float32's z is within 14 u = 14 * 2^-24 of the 64-bit one, relative to the length h
-            // of its pair: the sum of squares 9 u (four in a row, three and two levels more), half
-            // of which shows in the root, the mean with eps 0.5 u, the root, r w and its product
-            // with x 1 u each: 8 u; a product of the two and their sum 2 u; cosine and sine 1 u and
-            // 2 pi 2^-26 < 1.6 u of their angle, absolute, for both together 2^0.5 as much of h:
-            // 3.7 u.  With the scale's two roundings below 16 u.
-            bool sure = true, bad1 = false;
-            float near[2] = {0.0f, 0.0f};
-            if (in) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if ((c ? c1 : c0) * G >= a.R) {
-#pragma unroll
-                        for (int e = 0; e < G; ++e) E[c] = fmaxf(E[c], y[c][e] * y[c][e]);
-                    }
-                    // (the least length: of squares below float32)
-                    near[c] = fmaxf(__fsqrt_rn(E[c]), 1e-22f) * ((c ? c1 : c0) * G < a.R ? (float)a.scale : 1.0f) * 0x1p-20f;
-                }
+                for (int c = 0; c < 2; ++c)  // (the least length: of squares below float32)
+                    near[c] = fmaxf(__fsqrt_rn(E[c]), 1e-22f) * (my.turns(c, 0) ? a.scale32 : 1.0f) * 0x1p-20f;
                 sure = quantise_near<G>(y[0], near[0], w[0], &t[0], &bad);
                 sure &= quantise_near<G>(y[1], near[1], w[1], &t[1], &bad1);
-                bad |= bad1;
             }
-            const uint32_t again = __ballot_sync(0xffffffffu, !sure) & mask;
-            if (again) {  // (all four lanes of the row)
-                const int g[2] = {c0, c1};
-                float z[2 * G], tt[2] = {t[0], t[1]};
-                uint32_t ww[2 * (G / 8)];
+            if (mine && !in) atomicOr(&st[tok], ACES_ROW_RANGE);
+            if (in && (bad || bad1)) atomicOr(&st[tok], ACES_ROW_NONFINITE);
+            // rows to be done again: one bit for each of the eight
+            uint32_t again = __ballot_sync(0xffffffffu, in && !sure);
+            again = (again | again >> 1 | again >> 2 | again >> 3) & 0x11111111u;
+            uint8_t *row = nullptr;
+            if (in && ACES_IN(pos, a.S)) {
+                row = (keys ? a.ck : a.cv) + ((size_t)((size_t)b * a.H + h) * a.S + (size_t)pos) * RB;
+                if (!(again >> (lane & ~3) & 1u)) {
 #pragma unroll
-                for (int e = 0; e < 2 * G; ++e) z[e] = y[e / G][e % G];
-#pragma unroll
-                for (int e = 0; e < 2 * (G / 8); ++e) ww[e] = w[e / (G / 8)][e % (G / 8)];
-                exact_groups<D, F32, INTER>(Exact<D, F32, INTER>{a, a.k.p, b * a.k.b + i * a.k.i + h * a.k.h, a.kw, h * a.kw.h, b, i, 1.0}, mask, g, z,
-                                            near, ww, tt);
-                t[0] = tt[0], t[1] = tt[1];
-#pragma unroll
-                for (int e = 0; e < 2 * (G / 8); ++e) w[e / (G / 8)][e % (G / 8)] = ww[e];
+                    for (int c = 0; c < 2; ++c) {
+                        const int g = my.chan(c, 0) / G;
+                        uint32_t *to = reinterpret_cast<uint32_t *>(row) + g * (G / 8);
+                        if (G == 16)
+                            *reinterpret_cast<uint2 *>(to) = make_uint2(w[c][0], w[c][G / 8 - 1]);
+                        else
+                            *to = w[c][0];
+                        reinterpret_cast<unsigned short *>(row + D / 2)[g] = (unsigned short)(__float_as_uint(t[c]) >> 16);
+                    }
+                }
             }
-            if (!in) continue;
+            for (; again; again &= again - 1) {
+                const int from = __ffs(again) - 1;
+                uint8_t *to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, (unsigned long long)row, from));
+                const int ri = __shfl_sync(0xffffffffu, i, from), rh = __shfl_sync(0xffffffffu, h, from);
+                if (to) exact_row<D, F32, INTER>(a, b, ri, rh, to);
+            }
         }
-        if (!APPEND) continue;
-        if (bad) atomicOr(&st[tok], ACES_ROW_NONFINITE);
-        if (!ACES_IN(pos, a.S)) continue;
-        uint8_t *row = (kind == 2 ? a.cv : a.ck) + ((size_t)((size_t)b * a.H + h) * a.S + (size_t)pos) * RB;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int g = c ? c1 : c0;
-            uint32_t *to = reinterpret_cast<uint32_t *>(row) + g * (G / 8);
-            if (G == 16)
-                *reinterpret_cast<uint2 *>(to) = make_uint2(w[c][0], w[c][G / 8 - 1]);
-            else
-                *to = w[c][0];
-            reinterpret_cast<unsigned short *>(row + D / 2)[g] = (unsigned short)(__float_as_uint(t[c]) >> 16);
+        if (slice == 0) {
+            __syncwarp();
+            if (lane < tokens) a.status[(size_t)b * a.n + i0 + lane] = st[lane];
         }
-    }
-    if (APPEND) {
-        __syncthreads();
-        if (tid < tokens) a.status[(size_t)b * a.n + i0 + tid] = st[tid];
     }
 }
 
-// Tokens of a CTA (their logarithm): several once that still gives every SM four CTAs.
-static int turn_tokens(const Turn &a, int nsm) {
+// Tokens of a warp (their logarithm): with few key heads several, so that the eight rows
+// that go to the cache at a time are not mostly none, while there are warps enough.
+static int turn_tokens(const Turn &a, bool append, int nsm) {
     int lt = 0;
-    while ((2 << lt) <= TOKENS && (long long)a.B * a.n >= (8ll * nsm) << lt) ++lt;
+    while (append && (2 << lt) <= TOKENS && (a.H << lt) < 8 && (long long)a.B * a.n >= (16ll * nsm) << lt) ++lt;
     return lt;
 }
 
-template <int D, bool F32, bool APPEND>
-static cudaError_t run_turn(const Turn &a, bool interleaved, int nsm, cudaStream_t s) {
-    const int lt = turn_tokens(a, nsm);
-    const long long grid = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
-    if (interleaved)
-        k_turn<D, F32, APPEND, true><<<(unsigned)grid, TN, 0, s>>>(a, lt);
-    else
-        k_turn<D, F32, APPEND, false><<<(unsigned)grid, TN, 0, s>>>(a, lt);
+template <int D, bool F32, bool APPEND, bool INTER>
+static cudaError_t run_turn(const Turn &a, int nsm, cudaStream_t s) {
+    const int lt = turn_tokens(a, APPEND, nsm);
+    const long long units = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
+    // A unit's rows go to several warps while those are few.
+    constexpr int RW = 512 / D;
+    const int most = APPEND ? 1 + (a.Hq + RW - 1) / RW : (a.H + RW - 1) / RW + (a.Hq + RW - 1) / RW;
+    int slices = 1;
+    while (slices < most && units * slices < SLICE_WARPS * nsm) ++slices;
+    const long long want = (units * slices + TW - 1) / TW;
+    const unsigned grid = (unsigned)(want < (long long)TURN_CTAS * nsm ? want : (long long)TURN_CTAS * nsm);
+    const size_t tables = (size_t)((TW << lt) + 2) * (D * 4);
+    const auto fn = !a.vec ? k_turn<D, F32, APPEND, INTER, false, false>
+                  : a.R == D ? k_turn<D, F32, APPEND, INTER, true, true>
+                             : k_turn<D, F32, APPEND, INTER, true, false>;
+    fn<<<grid, TN, tables, s>>>(a, lt, slices);
     return cudaGetLastError();
 }
 
+template <int D, bool F32>
+static cudaError_t run_kind(const Turn &a, bool append, bool interleaved, int nsm, cudaStream_t s) {
+    if (append) return interleaved ? run_turn<D, F32, true, true>(a, nsm, s) : run_turn<D, F32, true, false>(a, nsm, s);
+    return interleaved ? run_turn<D, F32, false, true>(a, nsm, s) : run_turn<D, F32, false, false>(a, nsm, s);
+}
 cudaError_t launch_turn(const Turn &a, int D, bool f32, bool append, bool interleaved, int nsm, cudaStream_t s) {
-    if (D == 64) {
-        if (append) return f32 ? run_turn<64, true, true>(a, interleaved, nsm, s) : run_turn<64, false, true>(a, interleaved, nsm, s);
-        return f32 ? run_turn<64, true, false>(a, interleaved, nsm, s) : run_turn<64, false, false>(a, interleaved, nsm, s);
-    }
-    if (append) return f32 ? run_turn<128, true, true>(a, interleaved, nsm, s) : run_turn<128, false, true>(a, interleaved, nsm, s);
-    return f32 ? run_turn<128, true, false>(a, interleaved, nsm, s) : run_turn<128, false, false>(a, interleaved, nsm, s);
+    if (D == 64) return f32 ? run_kind<64, true>(a, append, interleaved, nsm, s) : run_kind<64, false>(a, append, interleaved, nsm, s);
+    return f32 ? run_kind<128, true>(a, append, interleaved, nsm, s) : run_kind<128, false>(a, append, interleaved, nsm, s);
 }
 
 #ifdef ACES_CHECKED

@@ -11,12 +11,12 @@ struct TurnHeads {  // [B, n, heads, D] numbers, the last dimension dense; strid
 struct TurnWeight {
     const void *p;   // null: ones
     long long h;     // between two heads' (0: shared)
-    int f32;
+    int f32, vec;    // vec: every head's start on 16 bytes
 };
 
 struct Turn {
     TurnHeads q, k, v, oq, ok;         // v: append only; ok: rotation only
-    int vec, ovec;                     // inputs' and outputs' groups start on 16 bytes
+    int vec;                           // every group starts on 16 bytes
     const float *freq;                 // [R / 2]
     const int32_t *axes;               // [R / 2] or null
     const int32_t *positions;          // [n_axes, B, n] or null
@@ -25,6 +25,7 @@ struct Turn {
     TurnWeight qw, kw;
     int R, n_axes, norm;
     double eps, scale;
+    float eps32, scale32;
     int B, n, Hq, H;
     // append
     uint8_t *ck, *cv;
