@@ -523,6 +523,32 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
                                void *out, float *lse, int32_t *seq_status, void *workspace,
                                size_t workspace_bytes, aces_stream_t stream);
 
+/*
+ * The same attention for a batch whose sequences share prefixes (a system
+ * prompt, a document): the prefixes' rows lie in a cache of their own, and are
+ * read once for all sequences that share them.
+ *   shared        [shared_planes, groups, H, S0, R]: a cache as above, of the
+ *                 same layers, whose sequence g is the prefix of sequences g * B /
+ *                 groups .. of the batch (B a multiple of groups)
+ *   shared_len    [groups] int32: a prefix's positions
+ *   cache, prefix_len, count, mask, depth: the sequences' own rows, as above; a
+ *                 token's position is shared_len + prefix_len + its number or
+ *                 depth, for the window and the sinks too
+ *   seq_status    also ACES_ROW_RANGE where shared_len is negative or above S0
+ * The other arguments, outputs, limits and errors are aces_kv4_attention's, and a
+ * token's result is that of one cache with the prefix's rows before its own, but
+ * for the order of the sums.
+ * workspace: aces_kv4_shared_workspace_bytes(B, groups, n, Hq, H, D) bytes.
+ */
+size_t aces_kv4_shared_workspace_bytes(int B, int groups, int n, int Hq, int H, int D); /* 0 for invalid sizes */
+aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_t *q_strides, const void *shared,
+                                      int shared_planes, int groups, int S0, const int32_t *shared_len,
+                                      const void *cache, int planes, int layer, int B, int n, int Hq, int H, int S,
+                                      int D, const int32_t *prefix_len, const int32_t *count, const uint32_t *mask,
+                                      int64_t mask_stride, const int32_t *depth, int64_t depth_stride, float scale,
+                                      int window, int sinks, void *out, float *lse, int32_t *seq_status,
+                                      void *workspace, size_t workspace_bytes, aces_stream_t stream);
+
 #ifdef ACES_CHECKED
 /*
  * Checked build only (compiled with -DACES_CHECKED; a test aid, not part of

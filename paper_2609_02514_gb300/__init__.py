@@ -14,6 +14,7 @@ without the built library, or with host tensors, raises.
     cache_lookup(branch_tok, F, pi, tok)  Algorithm 1 state recovery
     kv4_cache, kv4_append, kv4_read       a KV cache in 4 bits
     kv4_attention(q, cache, ...)          tokens, trees and prompts against it
+    kv4_shared_attention(q, shared, ...)  the same for a batch behind shared prefixes
     rotate_qk(q, k, inv_freq, ...)        norms and positions of queries and keys
     kv4_append_rotated(cache, ...)        the same, the keys going into that cache
 """
@@ -27,7 +28,7 @@ import torch
 
 __all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
            "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
-           "rotate_qk", "kv4_append_rotated",
+           "rotate_qk", "kv4_append_rotated", "kv4_shared_attention", "kv4_shared_workspace_bytes",
            "ROW_NONFINITE", "ROW_BAD_Q", "ROW_TIMEOUT", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -134,6 +135,9 @@ def _open(path):
     lib.aces_kv4_append.argtypes = [P, I, I, I, I, I, I, P, P, I, P, P, P, P, I, P, P]
     lib.aces_kv4_read.argtypes = [P, I, I, I, I, I, I, P, I, P, P, I, P]
     lib.aces_kv4_attention.argtypes = [P, I, P, P, I, I, I, I, I, I, I, I, P, P, P, L, P, L, F, I, I, P, P, P, P, S, P]
+    lib.aces_kv4_shared_workspace_bytes.argtypes = [I, I, I, I, I, I]
+    lib.aces_kv4_shared_workspace_bytes.restype = S
+    lib.aces_kv4_shared_attention.argtypes = [P, I, P, P, I, I, I, P, P, I, I, I, I, I, I, I, I, P, P, P, L, P, L, F, I, I, P, P, P, P, S, P]
     lib.aces_rotate_qk.argtypes = [P, P, I, P, P, I, I, I, I, I, P, P, P, P, P, P]
     lib.aces_kv4_append_rotated.argtypes = [P, I, I, I, I, I, I, P, P, P, I, P, P, P, I, P, P, I, P, P, P, P, P]
     lib.aces_status_string.argtypes = [I]
@@ -141,12 +145,13 @@ def _open(path):
     for f in (lib.aces_verify, lib.aces_verify_exact, lib.aces_sparsify, lib.aces_cache_build,
               lib.aces_cache_lookup, lib.aces_resample_sparse, lib.aces_tree_budget, lib.aces_branch_alloc,
               lib.aces_compact_kv, lib.aces_tree_mask, lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention,
-              lib.aces_rotate_qk, lib.aces_kv4_append_rotated):
+              lib.aces_rotate_qk, lib.aces_kv4_append_rotated, lib.aces_kv4_shared_attention):
         f.restype = I
     # what the native half of the binding calls
     lib.kv4_entries = tuple(ctypes.cast(f, P).value for f in (lib.aces_kv4_append, lib.aces_kv4_read, lib.aces_kv4_attention,
                                                                   lib.aces_kv4_workspace_bytes,
-                                                                  lib.aces_rotate_qk, lib.aces_kv4_append_rotated))
+                                                                  lib.aces_rotate_qk, lib.aces_kv4_append_rotated,
+                                                                  lib.aces_kv4_shared_attention, lib.aces_kv4_shared_workspace_bytes))
     if hasattr(lib, "aces_checked_violation"):
         lib.aces_checked_violation.argtypes = [P]
         lib.aces_checked_violation.restype = I
@@ -543,6 +548,31 @@ def kv4_attention(q, cache, layer: int, prefix_len, mask=None, depth=None, count
         o.get("lse"), o.get("status"), workspace, _stream(dev))
     if code != 0:
         _check("aces_kv4_attention", code)
+    return o
+
+
+def kv4_shared_workspace_bytes(B: int, groups: int, n: int, Hq: int, H: int, D: int) -> int:
+    return int(load().aces_kv4_shared_workspace_bytes(int(B), int(groups), int(n), int(Hq), int(H), int(D)))
+
+
+def kv4_shared_attention(q, shared, shared_len, cache, layer: int, prefix_len, mask=None, depth=None, count=None, scale: float | None = None,
+                         window: int = 0, sinks: int = 0, out: dict | None = None, workspace: torch.Tensor | None = None):
+    """kv4_attention() for a batch whose sequences share prefixes, whose rows are read once for all.
+
+    shared [2 * layers, groups, H, S0, D / 2 + 16]: a kv4_cache() whose sequence g holds the prefix of
+    sequences g * B / groups .. of the batch, shared_len [groups] int32 its positions.  cache and
+    prefix_len hold what each sequence has cached itself; a token's position is shared_len + prefix_len +
+    its number (or depth).  The other arguments and the results are kv4_attention()'s; status also has
+    ROW_RANGE where shared_len does not lie in shared.  The workspace (kv4_shared_workspace_bytes())
+    holds float32 sums as large as q beside what kv4_attention() needs.
+    """
+    lib, native, dev = _lib or load(), _native_module or _native(), _kv4_device(cache)
+    o = {} if out is None else dict(out)
+    code, o["out"], o["lse"], o["status"] = native.shared_attention(
+        lib.kv4_entries[6], lib.kv4_entries[7], q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, o.get("out"),
+        o.get("lse"), o.get("status"), workspace, _stream(dev), shared, shared_len)
+    if code != 0:
+        _check("aces_kv4_shared_attention", code)
     return o
 
 

@@ -171,10 +171,13 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     });
 }
 
+using SharedAttention = decltype(&aces_kv4_shared_attention);
+using SharedBytes = decltype(&aces_kv4_shared_workspace_bytes);
+
 // attention(entry, workspace_bytes, q, cache, layer, prefix_len, mask, depth, count, scale, window, sinks, out, lse, status,
-//           workspace, stream) -> (status code, out, lse, status)
-PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
-    return guarded(n_args, 17, [&]() -> PyObject * {
+//           workspace, stream) -> (status code, out, lse, status); with two more, shared and shared_len, behind prefixes
+PyObject *attend(PyObject *const *a, Py_ssize_t n_args, bool behind) {
+    return guarded(n_args, behind ? 19 : 17, [&]() -> PyObject * {
         const Cache c = cache_of(a[3]);
         int64_t qs[3];
         const Tensor &q = rows(a[2], "q", c, qs);
@@ -205,13 +208,25 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         lse.take(a[13], "lse", row, at::kFloat, c.t);
         status.take(a[14], "status", one, at::kInt, c.t);
         const int layer = integer(a[4], "layer"), window = integer(a[10], "window"), sinks = integer(a[11], "sinks");
-        const auto entry = reinterpret_cast<Attention>(address(a[0]));
         const auto stream = (aces_stream_t)address(a[16]);
+        Cache p = c;
+        const void *shared_len = nullptr;
+        if (behind) {
+            const Tensor &t = cuda(a[17], "shared");
+            if (t.device() != c.t.device()) throw Refusal{"shared must lie on " + c.t.device().str()};
+            if (t.scalar_type() != at::kByte || t.dim() != 5 || !t.is_contiguous() || t.size(2) != c.H || t.size(4) != c.t.size(4) || t.size(1) < 1 ||
+                c.B % t.size(1) != 0 || t.size(0) > INT32_MAX || t.size(3) > INT32_MAX)
+                throw Refusal{"shared must be a contiguous uint8 [planes, groups, " + std::to_string(c.H) + ", S0, " + std::to_string(c.t.size(4)) +
+                              "], and the batch a multiple of groups"};
+            p.planes = (int)t.size(0), p.B = (int)t.size(1), p.S = (int)t.size(3);
+            shared_len = dense(a[18], "shared_len", {p.B}, at::kInt, c.t);
+        }
         // The workspace is the call's own: given back on return, it is only used again
         // behind the call's work on this stream.
         Tensor scratch;
         if (a[15] == Py_None) {
-            const size_t need = reinterpret_cast<Bytes>(address(a[1]))(c.B, n, Hq, c.H, c.D);
+            const size_t need = behind ? reinterpret_cast<SharedBytes>(address(a[1]))(c.B, p.B, n, Hq, c.H, c.D)
+                                       : reinterpret_cast<Bytes>(address(a[1]))(c.B, n, Hq, c.H, c.D);
             scratch = at::empty({(int64_t)std::max<size_t>(need, 16)}, c.t.options());
         } else {
             scratch = cuda(a[15], "workspace");
@@ -223,13 +238,22 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         out.make(full, q.scalar_type(), c.t);
         lse.make(row, at::kFloat, c.t);
         status.make(one, at::kInt, c.t);
-        const aces_status s = entry(
-            q.data_ptr(), code(q.scalar_type()), qs, c.t.data_ptr(), c.planes, layer, c.B, n, Hq, c.H, c.S, c.D, (const int32_t *)prefix,
-            (const int32_t *)count, (const uint32_t *)mask, ms, (const int32_t *)depth, ds, (float)scale, window, sinks, out.p, (float *)lse.p,
-            (int32_t *)status.p, ws, bytes, stream);
+        const aces_status s =
+            behind ? reinterpret_cast<SharedAttention>(address(a[0]))(
+                         q.data_ptr(), code(q.scalar_type()), qs, cuda(a[17], "shared").data_ptr(), p.planes, p.B, p.S, (const int32_t *)shared_len,
+                         c.t.data_ptr(), c.planes, layer, c.B, n, Hq, c.H, c.S, c.D, (const int32_t *)prefix, (const int32_t *)count,
+                         (const uint32_t *)mask, ms, (const int32_t *)depth, ds, (float)scale, window, sinks, out.p, (float *)lse.p,
+                         (int32_t *)status.p, ws, bytes, stream)
+                   : reinterpret_cast<Attention>(address(a[0]))(
+                         q.data_ptr(), code(q.scalar_type()), qs, c.t.data_ptr(), c.planes, layer, c.B, n, Hq, c.H, c.S, c.D, (const int32_t *)prefix,
+                         (const int32_t *)count, (const uint32_t *)mask, ms, (const int32_t *)depth, ds, (float)scale, window, sinks, out.p,
+                         (float *)lse.p, (int32_t *)status.p, ws, bytes, stream);
         return Py_BuildValue("(iNNN)", (int)s, out.object(), lse.object(), status.object());
     });
 }
+
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) { return attend(a, n_args, false); }
+PyObject *shared_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) { return attend(a, n_args, true); }
 
 using Rotate = decltype(&aces_rotate_qk);
 using AppendRotated = decltype(&aces_kv4_append_rotated);
@@ -380,7 +404,8 @@ PyObject *append_rotated(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     });
 }
 
-PyMethodDef methods[] = {{"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotate)), METH_FASTCALL, nullptr},
+PyMethodDef methods[] = {{"shared_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(shared_attention)), METH_FASTCALL, nullptr},
+                         {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotate)), METH_FASTCALL, nullptr},
                          {"append_rotated", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_rotated)), METH_FASTCALL, nullptr},
                          {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append)), METH_FASTCALL, nullptr},
                          {"read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(read)), METH_FASTCALL, nullptr},

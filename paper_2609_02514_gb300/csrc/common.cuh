@@ -51,6 +51,8 @@ cudaError_t check_take_kv4_rows(unsigned long long out[3]);
 cudaError_t check_take_kv4_few(unsigned long long out[3]);
 cudaError_t check_take_kv4_many(unsigned long long out[3]);
 cudaError_t check_take_turn(unsigned long long out[3]);
+cudaError_t check_take_kv4_few_first(unsigned long long out[3]);
+cudaError_t check_take_kv4_few_behind(unsigned long long out[3]);
 #else
 #define ACES_IN(i, n) true
 #endif

@@ -79,6 +79,13 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const int32_t *prefix, const int32_t *
     return q;
 }
 
+// What a pass of the attention is: a call of its own, or one of the two of a batch whose
+// sequences share prefixes.  The first takes a prefix for a sequence and all tokens of
+// those that share it (its group) for its new tokens, which see nothing but the prefix;
+// it leaves its sums, not yet divided, with their maximum and the sum of their weights.
+// The second takes each sequence's own rows, and adds those sums as one more piece.
+enum { KV4_ALONE = 0, KV4_FIRST = 1, KV4_BEHIND = 2 };
+
 // Position of new token t: its depth in the tree (a negative or absurd one is
 // taken as the nearest sensible one), or its number.
 __device__ __forceinline__ int kv4_pos(int P, const int32_t *depth, int t) {
@@ -102,6 +109,16 @@ struct Kv4Att {
     int B, n, Hq, H, G, S, D, words;
     int window, sinks;     // window 0: none
     float scale;           // of q . k, in log2 units, times KV4_STEP
+    // of two passes: sequences of a group; the first pass's sums [B, n, Hq, D], maxima
+    // and sums of weights [B, n, Hq], and status [groups]
+    int per;
+    float *part, *part_m, *part_l;
+    int32_t *part_status;
+    const int32_t *shared_len;  // [groups]
+    int shared_S;
+    // the first pass: a sequence's tokens (n is a group's), its own positions and counts
+    int own_n, own_S;
+    const int32_t *own_prefix, *own_count;
 };
 
 struct Kv4Rows {

@@ -51,6 +51,36 @@ bool many_rows(int f32, int B, int H, int n, int G) {
     return !f32 && rows > ((long long)B * H <= 32 ? 32 : 16);
 }
 
+// Checks of an attention call beside its cache, and what they make of the kernels' arguments.
+aces_status check_attention(const void *q, aces_dtype dt, const int64_t *q_strides, int B, int n, int Hq, int H, int D,
+                            const int32_t *prefix_len, const uint32_t *mask, int64_t mask_stride, const int32_t *depth,
+                            int64_t depth_stride, float scale, int window, int sinks, void *out, int32_t *seq_status, void *workspace,
+                            Kv4Att *a) {
+    if (dt != ACES_F32 && dt != ACES_BF16) return ACES_ERR_UNSUPPORTED;
+    if (!q || !q_strides || !prefix_len || !out || !seq_status || !workspace) return ACES_ERR_INVALID_ARG;
+    const size_t es = dt == ACES_F32 ? 4 : 2;
+    if ((uintptr_t)q % es || !aligned16(out) || !aligned16(workspace)) return ACES_ERR_INVALID_ARG;
+    if (n < 1 || Hq < H || Hq % H != 0) return ACES_ERR_INVALID_ARG;
+    if ((mask == nullptr) != (depth == nullptr)) return ACES_ERR_INVALID_ARG;
+    const int words = (n + 31) / 32;
+    if (mask && ((mask_stride != 0 && mask_stride < (int64_t)n * words) || (depth_stride != 0 && depth_stride < n)))
+        return ACES_ERR_INVALID_ARG;
+    if (!(scale > 0.0f && scale <= 0x1p110f)) return ACES_ERR_INVALID_ARG;  // a.scale below is finite
+    if (window < 0 || sinks < 0) return ACES_ERR_INVALID_ARG;
+    *a = {};
+    a->q = q;
+    a->qb = q_strides[0], a->qi = q_strides[1], a->qh = q_strides[2];
+    a->f32 = dt == ACES_F32;
+    a->out = out, a->status = seq_status;
+    a->prefix = prefix_len;
+    a->mask = mask, a->mask_b = mask_stride, a->depth = depth, a->depth_b = depth_stride;
+    a->B = B, a->n = n, a->Hq = Hq, a->H = H, a->G = Hq / H, a->D = D, a->words = words;
+    a->window = window;
+    a->sinks = window > 0 ? sinks : 0;
+    a->scale = (float)((double)scale * 1.4426950408889634 * (double)KV4_STEP);
+    return ACES_OK;
+}
+
 // Checks of what a rotation is, and its part of the kernel's arguments.
 aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, const void *q, const void *k, aces_dtype dt, Turn *a) {
     if (D != 64 && D != 128) return D < 1 ? ACES_ERR_INVALID_ARG : ACES_ERR_UNSUPPORTED;
@@ -166,36 +196,74 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
                                const int32_t *count, const uint32_t *mask, int64_t mask_stride, const int32_t *depth,
                                int64_t depth_stride, float scale, int window, int sinks, void *out, float *lse,
                                int32_t *seq_status, void *workspace, size_t workspace_bytes, aces_stream_t stream) {
-    Kv4Att a;
     uint8_t *pk, *pv;
     aces_status st = check_cache(cache, planes, layer, B, H, S, D, &pk, &pv);
     if (st != ACES_OK) return st;
-    if (dt != ACES_F32 && dt != ACES_BF16) return ACES_ERR_UNSUPPORTED;
-    if (!q || !q_strides || !prefix_len || !out || !seq_status || !workspace) return ACES_ERR_INVALID_ARG;
-    const size_t es = dt == ACES_F32 ? 4 : 2;
-    if ((uintptr_t)q % es || !aligned16(out) || !aligned16(workspace)) return ACES_ERR_INVALID_ARG;
-    if (n < 1 || Hq < H || Hq % H != 0) return ACES_ERR_INVALID_ARG;
+    Kv4Att a;
+    st = check_attention(q, dt, q_strides, B, n, Hq, H, D, prefix_len, mask, mask_stride, depth, depth_stride, scale, window, sinks, out,
+                         seq_status, workspace, &a);
+    if (st != ACES_OK) return st;
     const size_t need = aces_kv4_workspace_bytes(B, n, Hq, H, D);
     if (need == 0 || workspace_bytes < need) return ACES_ERR_INVALID_ARG;
-    if ((mask == nullptr) != (depth == nullptr)) return ACES_ERR_INVALID_ARG;
-    const int words = (n + 31) / 32;
-    if (mask && ((mask_stride != 0 && mask_stride < (int64_t)n * words) || (depth_stride != 0 && depth_stride < n)))
-        return ACES_ERR_INVALID_ARG;
-    if (!(scale > 0.0f && scale <= 0x1p110f)) return ACES_ERR_INVALID_ARG;  // a.scale below is finite
-    if (window < 0 || sinks < 0) return ACES_ERR_INVALID_ARG;
-    a.k = pk, a.v = pv;
-    a.q = q;
-    a.qb = q_strides[0], a.qi = q_strides[1], a.qh = q_strides[2];
-    a.f32 = dt == ACES_F32;
-    a.out = out, a.lse = lse, a.status = seq_status;
-    a.prefix = prefix_len, a.count = count;
-    a.mask = mask, a.mask_b = mask_stride, a.depth = depth, a.depth_b = depth_stride;
-    a.B = B, a.n = n, a.Hq = Hq, a.H = H, a.G = Hq / H, a.S = S, a.D = D, a.words = words;
-    a.window = window;
-    a.sinks = window > 0 ? sinks : 0;
-    a.scale = (float)((double)scale * 1.4426950408889634 * (double)KV4_STEP);
-    const auto launch = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many : launch_kv4_few;
+    a.k = pk, a.v = pv, a.S = S;
+    a.lse = lse, a.count = count;
+    const auto launch = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_ALONE> : launch_kv4_few<KV4_ALONE>;
     return launch(a, workspace, sm_count(), reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
+}
+
+// Workspace of two passes: the first's sums, maxima, sums of weights and status, then what
+// either pass needs for itself.
+static size_t shared_part_bytes(int B, int groups, int n, int Hq, int D) {
+    return (size_t)B * n * Hq * (D + 2) * 4 + ((size_t)groups * 4 + 15) / 16 * 16;
+}
+size_t aces_kv4_shared_workspace_bytes(int B, int groups, int n, int Hq, int H, int D) {
+    if (groups < 1 || B < groups || B % groups != 0) return 0;
+    const size_t own = aces_kv4_workspace_bytes(B, n, Hq, H, D);
+    if (own == 0) return 0;
+    const size_t first = aces_kv4_workspace_bytes(groups, B / groups * n, Hq, H, D);
+    return (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16 + (own > first ? own : first);
+}
+
+aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_t *q_strides, const void *shared, int shared_planes,
+                                      int groups, int S0, const int32_t *shared_len, const void *cache, int planes, int layer, int B,
+                                      int n, int Hq, int H, int S, int D, const int32_t *prefix_len, const int32_t *count,
+                                      const uint32_t *mask, int64_t mask_stride, const int32_t *depth, int64_t depth_stride, float scale,
+                                      int window, int sinks, void *out, float *lse, int32_t *seq_status, void *workspace,
+                                      size_t workspace_bytes, aces_stream_t stream) {
+    uint8_t *pk, *pv, *sk, *sv;
+    aces_status st = check_cache(cache, planes, layer, B, H, S, D, &pk, &pv);
+    if (st != ACES_OK) return st;
+    if (groups < 1 || B < groups || B % groups != 0) return ACES_ERR_INVALID_ARG;
+    st = check_cache(shared, shared_planes, layer, groups, H, S0, D, &sk, &sv);
+    if (st != ACES_OK) return st;
+    if (!shared_len) return ACES_ERR_INVALID_ARG;
+    Kv4Att a;
+    st = check_attention(q, dt, q_strides, B, n, Hq, H, D, prefix_len, mask, mask_stride, depth, depth_stride, scale, window, sinks, out,
+                         seq_status, workspace, &a);
+    if (st != ACES_OK) return st;
+    const size_t need = aces_kv4_shared_workspace_bytes(B, groups, n, Hq, H, D);
+    if (need == 0 || workspace_bytes < need) return ACES_ERR_INVALID_ARG;
+    const int per = B / groups;
+    const size_t rows = (size_t)B * n * Hq;
+    a.lse = lse, a.count = count, a.per = per;
+    a.part = reinterpret_cast<float *>(workspace);
+    a.part_m = a.part + rows * D;
+    a.part_l = a.part_m + rows;
+    a.part_status = reinterpret_cast<int32_t *>(a.part_l + rows);
+    a.shared_len = shared_len, a.shared_S = S0;
+    void *rest = reinterpret_cast<uint8_t *>(workspace) + (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16;
+    Kv4Att f = a;
+    f.k = sk, f.v = sv;
+    f.B = groups, f.n = per * n, f.S = S0;
+    f.prefix = shared_len, f.count = nullptr, f.status = a.part_status;
+    f.own_n = n, f.own_S = S, f.own_prefix = prefix_len, f.own_count = count;
+    a.k = pk, a.v = pv, a.S = S;
+    const int nsm = sm_count();
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const auto first = many_rows(f.f32, f.B, H, f.n, f.G) ? launch_kv4_many<KV4_FIRST> : launch_kv4_few<KV4_FIRST>;
+    const auto behind = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_BEHIND> : launch_kv4_few<KV4_BEHIND>;
+    if (first(f, rest, nsm, s) != cudaSuccess) return ACES_ERR_CUDA;
+    return behind(a, rest, nsm, s) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
 }
 
 aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const int64_t *q_strides, const int64_t *k_strides, int B, int n,

@@ -1,6 +1,6 @@
 // Attention over a 4-bit KV cache for many query rows (trees, prompts) of
-// bfloat16 (the format: kv4.cuh, the shares: kv4_plan.cuh), on the 5th-generation
-// tensor cores.
+// bfloat16 (the format: kv4.cuh, the shares and the passes: kv4_plan.cuh), on the
+// 5th-generation tensor cores.
 //
 // A persistent CTA an SM works on items of up to 256 query rows, 128 keys a
 // tile, with its warps in five parts:
@@ -173,11 +173,12 @@ __device__ __forceinline__ uint32_t span_bits(int lo, int hi, int w0) {
     return (y >= 32 ? 0xFFFFFFFFu : (1u << y) - 1u) & ~((1u << x) - 1u);
 }
 // Which of the positions [w0, w0 + 32) token i at position pos sees.
-__device__ __forceinline__ uint32_t seen_word(const Kv4Att &a, int b, int P, int cnt, int w0, int i, int pos) {
+template <int MODE>
+__device__ __forceinline__ uint32_t seen_word(const Kv4Att &a, int b, int P, int cnt, int sinks, int w0, int i, int pos) {
     const int first = a.window ? pos - a.window + 1 : 0;
-    if (!a.mask) return span_bits(0, P + i + 1, w0) & (span_bits(first, INT_MAX, w0) | span_bits(0, a.sinks, w0));
-    uint32_t r = w0 < P ? span_bits(0, P, w0) & (span_bits(first, INT_MAX, w0) | span_bits(0, a.sinks, w0)) : 0u;
-    if (w0 + 32 <= P || w0 >= P + cnt) return r;
+    if (MODE != KV4_FIRST && !a.mask) return span_bits(0, P + i + 1, w0) & (span_bits(first, INT_MAX, w0) | span_bits(0, sinks, w0));
+    uint32_t r = w0 < P ? span_bits(0, P, w0) & (span_bits(first, INT_MAX, w0) | span_bits(0, sinks, w0)) : 0u;
+    if (MODE == KV4_FIRST || w0 + 32 <= P || w0 >= P + cnt) return r;
     const uint32_t *row = a.mask + b * a.mask_b + (size_t)i * a.words;
     const int t0 = w0 - P;  // the token at w0, above -32
     const int wi = t0 >> 5, sh = t0 & 31;
@@ -187,7 +188,7 @@ __device__ __forceinline__ uint32_t seen_word(const Kv4Att &a, int b, int P, int
         const int32_t *dep = a.depth + b * a.depth_b;
         for (uint32_t left = bits; left; left &= left - 1) {
             const int x = __ffs(left) - 1, kp = kv4_pos(P, dep, t0 + x);
-            if (kp < first && kp >= a.sinks) bits &= ~(1u << x);
+            if (kp < first && kp >= sinks) bits &= ~(1u << x);
         }
     }
     return r | bits;
@@ -286,11 +287,11 @@ static __device__ __noinline__ void fold_sums(float *tot, uint32_t tO, float m, 
     tc_wait_st();
 }
 
-template <int D>
+template <int D, int MODE>
 __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, int RT) {
     using C = Many<D>;
     using Cost = ManyCost<D>;
-    using Seg = Kv4Seg<MKT, 1, Cost>;
+    using Seg = Kv4Seg<MKT, 1, Cost, MODE>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) unsigned long long bars[33];
     __shared__ uint32_t tmem_base;
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     }
     pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    const Kv4Start at = kv4_start<MKT, 1, Cost, MT>(a, R, RT);
+    const Kv4Start at = kv4_start<MKT, 1, Cost, MT, MODE>(a, R, RT);
     if (tid == 0) kv4_put_info<Cost>(ws, at);
     Seg seg;
     if (!seg.start(a, R, RT, at)) return;
@@ -359,11 +360,12 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             const bool single = NR - rt * R <= 128;
             const int slot_row = single ? row : x * 128 + row;
             const int r0 = rt * R + slot_row, i = r0 / a.G, gq = r0 - i * a.G;
-            const bool row_live = r0 < NR && key.live && i < key.cnt;
-            const int pos = row_live ? kv4_pos(P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0;
+            const Kv4Token tk = r0 < NR ? kv4_token<MODE>(a, key, b, i) : Kv4Token{false, 0};
+            const bool row_live = tk.live;
+            const int pos = tk.pos, sinks = kv4_sinks<MODE>(a, key);
             const bool warp_live = __any_sync(0xffffffffu, row_live);
             const int posmax = __reduce_max_sync(0xffffffffu, pos), imin = __reduce_min_sync(0xffffffffu, row_live ? i : INT_MAX);
-            const int all_see = a.mask || !warp_live ? P : P + imin + 1;
+            const int all_see = MODE == KV4_FIRST || a.mask || !warp_live ? P : P + imin + 1;
             const int T = min(seg.x1, key.tiles) - seg.x0;  // 0 for an item without keys
             const int mine = 2 * (single ? (T + 1 - x) >> 1 : T);  // of 64 keys
             // Queries (a row without one reads the first token's and keeps zeros), where the
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             // any (padding) it waits for nothing, and words for two of those could both be
             // there before the issuing warp looks: it would take the second for none.
             if (mine > 0) {
-                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + b * a.qb + (row_live ? i : 0) * a.qi +
+                const unsigned short *f = reinterpret_cast<const unsigned short *>(a.q) + kv4_query<MODE>(a, b, row_live ? i : 0) +
                                           (long long)(h * a.G + (row_live ? gq : 0)) * a.qh;
                 const uint32_t keep = row_live ? 0xFFFFFFFFu : 0u;
                 if (((uintptr_t)f & 15) == 0) {
@@ -418,7 +420,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     }
                     if (warp_live) {
                         const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + half * MKH;
-                        const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > a.sinks);
+                        const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > sinks);
                         const uint32_t at = tS + half * MKH;
                         float v[2][32];
                         tc_ld32(at, v[0]);
@@ -427,7 +429,8 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                         tc_wait_ld(v[1]);
                         if (masked) {
                             uint32_t see0 = 0u, see1 = 0u;
-                            if (row_live) see0 = seen_word(a, b, P, key.cnt, j0, i, pos), see1 = seen_word(a, b, P, key.cnt, j0 + 32, i, pos);
+                            if (row_live)
+                                see0 = seen_word<MODE>(a, b, P, key.cnt, sinks, j0, i, pos), see1 = seen_word<MODE>(a, b, P, key.cnt, sinks, j0 + 32, i, pos);
 #pragma unroll
                             for (int c = 0; c < 32; ++c) {
                                 if (!(see0 >> c & 1u)) v[0][c] = -INFINITY;
@@ -516,7 +519,13 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 l = sm_l[0][row] * ex2(sm_m[0][row] - ref) + sm_l[1][row] * ex2(sm_m[1][row] - ref);
                 m = M;
             }
-            const float k = whole ? (live && l != 0.0f ? f * KV4_STEP / l : 0.0f) : f;
+            float k = whole && MODE != KV4_FIRST ? (live && l != 0.0f ? f * KV4_STEP / l : 0.0f) : f;
+            float first_k = 0.0f, row_lse = 0.0f;  // the first pass's part (of the rows' first group)
+            if (MODE == KV4_BEHIND && whole && r < NR) {
+                const Kv4Mix mix = kv4_mix(a, orow, m, l);
+                k = live ? f * mix.own : 0.0f, first_k = live && !(single && x == 1) ? mix.first : 0.0f;
+                row_lse = live ? mix.lse : -INFINITY;
+            }
             // the second group's sums go to the first through its queries' place
             float4 *box = reinterpret_cast<float4 *>(sq + C::TILE);  // 32 channels of 128 rows
 #pragma unroll 1
@@ -541,6 +550,15 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[c] *= k;
                 }
+                if (MODE == KV4_BEHIND && first_k != 0.0f) {
+                    const float4 *part = reinterpret_cast<const float4 *>(a.part) + (size_t)orow * (D / 4) + 8 * w;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float4 p = part[c];
+                        v[4 * c] = fmaf(p.x, first_k, v[4 * c]), v[4 * c + 1] = fmaf(p.y, first_k, v[4 * c + 1]);
+                        v[4 * c + 2] = fmaf(p.z, first_k, v[4 * c + 2]), v[4 * c + 3] = fmaf(p.w, first_k, v[4 * c + 3]);
+                    }
+                }
                 if (single) {
                     if (x == 1) {
 #pragma unroll
@@ -563,7 +581,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 // (each warp in its own rows' place: another may be at the next segment's queries)
                 auto chunk = [&](int rw, int c) { return reinterpret_cast<uint4 *>(myq + swz(rw, c)); };
                 bool full;
-                if (whole) {
+                if (whole && MODE != KV4_FIRST) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         *chunk(row, 4 * w + c) = make_uint4(bf2_pack(v[8 * c], v[8 * c + 1]), bf2_pack(v[8 * c + 2], v[8 * c + 3]),
@@ -586,7 +604,9 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                     const int to = __shfl_sync(0xffffffffu, orow, rr);
                     if (r_first + rr >= NR) continue;
                     const uint4 o = *chunk(rw0 + rr, c);
-                    if (whole)
+                    if (whole && MODE == KV4_FIRST)
+                        reinterpret_cast<uint4 *>(a.part)[(size_t)to * (D / 4) + (w / (D / 64)) * CH + c] = o;
+                    else if (whole)
                         reinterpret_cast<uint4 *>(a.out)[(size_t)to * CH + c] = o;
                     else
                         reinterpret_cast<uint4 *>(slot)[(size_t)(sw0 + rr) * (D / 4) + (w / (D / 64)) * CH + c] = o;
@@ -597,8 +617,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                 if (!whole) {
                     slot[(size_t)R * D + srow] = m;
                     slot[(size_t)R * D + R + srow] = l;
+                } else if (MODE == KV4_FIRST) {
+                    a.part_m[orow] = m, a.part_l[orow] = l;
                 } else if (a.lse) {
-                    a.lse[orow] = live && l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                    a.lse[orow] = MODE == KV4_BEHIND ? row_lse : live && l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
                 }
             }
             first = false;
@@ -642,7 +664,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             uint32_t step = 0;
             do {
                 const uint8_t *kb = a.k + seg.row0(a) * C::RB, *vb = a.v + seg.row0(a) * C::RB;  // the key head's rows
-                const int top = min(seg.x1, seg.key.tiles), end = seg.key.P + seg.key.cnt;
+                const int top = min(seg.x1, seg.key.tiles), end = kv4_end<MODE>(seg.key);
                 int ahead = seg.x0 + 1;
 #pragma unroll 1
                 for (int y = seg.x0; y < top && !bad; ++y) {
@@ -754,25 +776,29 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
 // Rows of an item.
 static int many_rows_of(int n, int G) { return (long long)n * G <= 128 ? 128 : 256; }
 
-// (after the pieces: a CTA's totals, [D] by 256 rows and their maximum)
-size_t kv4_many_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(nsm, many_rows_of(n, G), D) + (size_t)nsm * 256 * (D + 1) * 4; }
-
-template <int D>
+template <int D, int MODE>
 static cudaError_t run_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
     const int R = many_rows_of(a.n, a.G), RT = (int)(((long long)a.n * a.G + R - 1) / R);
     Kv4Ws ws = kv4_ws_carve(workspace, nsm);
-    ws.total = ws.piece + (size_t)2 * nsm * R * (D + 2);
+    ws.total = ws.piece + (size_t)2 * nsm * R * (D + 2);  // after the pieces: a CTA's totals, [D] by 256 rows and their maximum
     static std::atomic<unsigned long long> allowed{0};
-    cudaError_t e = allow_smem(k_kv4_many<D>, Many<D>::SMEM, allowed);
+    cudaError_t e = allow_smem(k_kv4_many<D, MODE>, Many<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    k_kv4_many<D><<<nsm, MT, Many<D>::SMEM, s>>>(a, ws, R, RT);
+    k_kv4_many<D, MODE><<<nsm, MT, Many<D>::SMEM, s>>>(a, ws, R, RT);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_kv4_join(a, ws, nsm, R, s);
+    return e != cudaSuccess ? e : launch_kv4_join<MODE>(a, ws, nsm, R, s);
 }
 
+template <int MODE>
 cudaError_t launch_kv4_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
-    return a.D == 64 ? run_many<64>(a, workspace, nsm, s) : run_many<128>(a, workspace, nsm, s);
+    return a.D == 64 ? run_many<64, MODE>(a, workspace, nsm, s) : run_many<128, MODE>(a, workspace, nsm, s);
 }
+
+template cudaError_t launch_kv4_many<KV4_ALONE>(const Kv4Att &, void *, int, cudaStream_t);
+template cudaError_t launch_kv4_many<KV4_FIRST>(const Kv4Att &, void *, int, cudaStream_t);
+template cudaError_t launch_kv4_many<KV4_BEHIND>(const Kv4Att &, void *, int, cudaStream_t);
+
+size_t kv4_many_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(nsm, many_rows_of(n, G), D) + (size_t)nsm * 256 * (D + 1) * 4; }
 
 #ifdef ACES_CHECKED
 cudaError_t check_take_kv4_many(unsigned long long out[3]) { return check_take(out); }

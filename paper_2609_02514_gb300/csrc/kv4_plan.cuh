@@ -59,11 +59,72 @@ struct Kv4Keys {
     int lo, hi, s_hi;
     int st, mt0, tiles, units;
     int rows;              // of the tile
+    int sinks;             // first positions that stay visible (KV4_BEHIND: of the sequence's own)
     bool live;
 };
 
-template <int KT, int TPU>
-__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq &sq, int rt) {
+// A sequence's cached positions and new ones, from its lengths (shared: of its prefix).
+template <int MODE>
+__device__ __forceinline__ Kv4Seq kv4_seq_of(const Kv4Att &a, int P, int cnt, int shared) {
+    Kv4Seq q{P, MODE == KV4_FIRST ? a.n : cnt, true};
+    if (MODE == KV4_FIRST)
+        q.ok = P >= 0 && P <= a.S;
+    else
+        q.ok = P >= 0 && cnt >= 0 && cnt <= a.n && (long long)P + cnt <= a.S;
+    if (MODE == KV4_BEHIND) q.ok = q.ok && shared >= 0 && shared <= a.shared_S;
+    return q;
+}
+template <int MODE>
+__device__ __forceinline__ Kv4Seq kv4_seq_of(const Kv4Att &a, int b) {
+    if (MODE == KV4_ALONE) return kv4_seq(a.prefix, a.count, b, a.n, a.S);
+    return kv4_seq_of<MODE>(a, a.prefix[b], MODE == KV4_BEHIND && a.count ? a.count[b] : a.n, MODE == KV4_BEHIND ? a.shared_len[b / a.per] : 0);
+}
+// one behind the last position whose rows are read
+template <int MODE>
+__device__ __forceinline__ int kv4_end(const Kv4Keys &k) { return MODE == KV4_FIRST ? k.P : k.P + k.cnt; }
+template <int MODE>
+__device__ __forceinline__ int kv4_sinks(const Kv4Att &a, const Kv4Keys &k) { return MODE == KV4_BEHIND ? k.sinks : a.sinks; }
+template <int MODE>
+__device__ __forceinline__ int32_t kv4_status(const Kv4Att &a, int b) {
+    return (kv4_seq_of<MODE>(a, b).ok ? 0 : ACES_ROW_RANGE) | (MODE == KV4_BEHIND ? a.part_status[b / a.per] : 0);
+}
+
+// A new token: whether there is one, its position, and the queries' place in q.
+struct Kv4Token {
+    bool live;
+    int pos;
+};
+template <int MODE>
+__device__ __forceinline__ Kv4Token kv4_token(const Kv4Att &a, const Kv4Keys &k, int b, int i) {
+    if (MODE != KV4_FIRST) {
+        const bool ok = k.live && i < k.cnt;
+        return {ok, ok ? kv4_pos(k.P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0};
+    }
+    if (!k.live) return {false, 0};
+    const int s = i / a.own_n, own = b * a.per + s, t = i - s * a.own_n;  // the sequence and its token
+    const Kv4Seq q = kv4_seq(a.own_prefix, a.own_count, own, a.own_n, a.own_S);
+    if (!q.ok || t >= q.cnt) return {false, 0};
+    return {true, kv4_pos(k.P + q.P, a.depth ? a.depth + own * a.depth_b : nullptr, t)};
+}
+template <int MODE>
+__device__ __forceinline__ long long kv4_query(const Kv4Att &a, int b, int i) {
+    if (MODE != KV4_FIRST) return b * a.qb + i * a.qi;
+    const int s = i / a.own_n;
+    return (b * a.per + s) * a.qb + (i - s * a.own_n) * a.qi;
+}
+
+// How a row's own sums and the first pass's come together, and the row's lse.
+struct Kv4Mix {
+    float own, first, lse;
+};
+__device__ __forceinline__ Kv4Mix kv4_mix(const Kv4Att &a, size_t row, float M, float L) {
+    const float m = a.part_m[row], l = a.part_l[row], top = fmaxf(M, m), ref = top == -INFINITY ? 0.0f : top;
+    const float fo = ex2(M - ref), ff = ex2(m - ref), all = fmaf(L, fo, l * ff), k = all == 0.0f ? 0.0f : KV4_STEP / all;
+    return {fo * k, ff * k, all == 0.0f ? -INFINITY : (top + log2f(all)) * 0.6931471805599453f};
+}
+
+template <int KT, int TPU, int MODE>
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq &sq, int rt, int b) {
     Kv4Keys k;
     k.P = sq.P, k.cnt = sq.cnt;
     const int r0 = rt * R, r1 = min(r0 + R, a.n * a.G);  // at most 2^30 rows
@@ -72,10 +133,17 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq
     k.i1 = min((r1 - 1) / a.G, sq.cnt - 1);
     k.live = sq.ok && k.i0 < sq.cnt;
     k.lo = k.hi = k.s_hi = k.st = k.mt0 = k.tiles = 0;
+    k.sinks = a.sinks;
     if (k.live) {
-        k.hi = k.P + (a.mask ? k.cnt : k.i1 + 1);
-        k.lo = a.window ? max(0, k.P + (a.mask ? 0 : k.i0) - a.window + 1) : 0;
-        k.s_hi = min(a.sinks, k.lo);
+        if (MODE == KV4_BEHIND && a.sinks > 0) k.sinks = max(0, a.sinks - a.shared_len[b / a.per]);
+        if (MODE == KV4_FIRST) {
+            k.hi = k.P;
+            k.lo = a.window ? max(0, k.P - a.window + 1) : 0;
+        } else {
+            k.hi = k.P + (a.mask ? k.cnt : k.i1 + 1);
+            k.lo = a.window ? max(0, k.P + (a.mask ? 0 : k.i0) - a.window + 1) : 0;
+        }
+        k.s_hi = min(kv4_sinks<MODE>(a, k), k.lo);
         k.st = (k.s_hi + KT - 1) / KT;
         k.mt0 = max(k.lo / KT, k.st);
         k.tiles = k.st + max(0, (k.hi + KT - 1) / KT - k.mt0);
@@ -83,9 +151,9 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq
     k.units = max(1, (k.tiles + TPU - 1) / TPU);
     return k;
 }
-template <int KT, int TPU>
+template <int KT, int TPU, int MODE>
 __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int rt) {
-    return kv4_keys<KT, TPU>(a, R, kv4_seq(a.prefix, a.count, b, a.n, a.S), rt);
+    return kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, b), rt, b);
 }
 // first key of the x-th tile
 template <int KT>
@@ -93,11 +161,13 @@ __device__ __forceinline__ int kv4_tile(const Kv4Keys &k, int x) {
     return (x < k.st ? x : k.mt0 + x - k.st) * KT;
 }
 
-// Whether new or old position j is seen by token i at position pos.
-__device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end, int j, int i, int pos) {
+// Whether new or old position j is seen by token i at position pos (of the passes of two:
+// KV4_BEHIND counts positions from the sequence's own first).
+template <int MODE>
+__device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end, int sinks, int j, int i, int pos) {
     if (j >= end) return false;
     int kp = j;
-    if (j >= P) {
+    if (MODE != KV4_FIRST && j >= P) {
         const int t = j - P;
         if (a.mask) {
             if (!((__ldg(a.mask + b * a.mask_b + (size_t)i * a.words + (t >> 5)) >> (t & 31)) & 1u)) return false;
@@ -106,7 +176,7 @@ __device__ __forceinline__ bool kv4_sees(const Kv4Att &a, int b, int P, int end,
             return false;
         }
     }
-    return !a.window || kp > pos - a.window || kp < a.sinks;
+    return !a.window || kp > pos - a.window || kp < sinks;
 }
 
 // A CTA's range and the item it starts in, by all NTH threads.  off and left are
@@ -116,7 +186,7 @@ struct Kv4Start {
     int quantum, b, rt, h, off, cnt;
     Kv4Keys key;
 };
-template <int KT, int TPU, class Cost, int NTH>
+template <int KT, int TPU, class Cost, int NTH, int MODE>
 __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     __shared__ unsigned long long red[NTH / 32];
     __shared__ Kv4Start found;
@@ -125,7 +195,7 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     unsigned long long sum = 0, total;
     Kv4Keys k;
     for (int e = e0; e < e1; ++e) {
-        k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+        k = kv4_keys<KT, TPU, MODE>(a, R, e / RT, e % RT);
         sum += (unsigned long long)Cost::all(k) * a.H;
     }
     unsigned long long at = block_exscan_n<NTH>(sum, red, &total);
@@ -133,12 +203,12 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     const unsigned long long Q = max((total + gridDim.x - 1) / gridDim.x, (unsigned long long)Cost::MOST), w0 = Q * blockIdx.x;
     if (w0 >= at && w0 < at + sum) {
         for (int e = e0; e < e1; ++e) {
-            if (per > 1) k = kv4_keys<KT, TPU>(a, R, e / RT, e % RT);
+            if (per > 1) k = kv4_keys<KT, TPU, MODE>(a, R, e / RT, e % RT);
             const unsigned u = Cost::all(k);
             if (w0 < at + (unsigned long long)u * a.H) {
                 const unsigned x = (unsigned)(w0 - at);
                 found.b = e / RT, found.rt = e % RT, found.h = (int)(x / u), found.off = (int)(x % u);
-                found.cnt = kv4_seq(a.prefix, a.count, found.b, a.n, a.S).ok ? k.cnt : 0;
+                found.cnt = kv4_seq_of<MODE>(a, found.b).ok ? k.cnt : 0;
                 found.key = k;
                 break;
             }
@@ -153,17 +223,17 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
 }
 
 // Without shares: a cluster of CL CTAs has the whole item.
-template <int KT, int TPU, class Cost>
+template <int KT, int TPU, class Cost, int MODE>
 __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, int CL) {
     Kv4Start s;
     const int x = blockIdx.x / CL, e = x / a.H;
     s.h = x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
     s.off = 0;
-    s.key = kv4_keys<KT, TPU>(a, R, s.b, s.rt);
+    s.key = kv4_keys<KT, TPU, MODE>(a, R, s.b, s.rt);
     s.left = s.quantum = Cost::all(s.key);
     s.cnt = s.key.cnt;
     if (threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
-        a.status[s.b] = kv4_seq(a.prefix, a.count, s.b, a.n, a.S).ok ? 0 : ACES_ROW_RANGE;
+        a.status[s.b] = kv4_status<MODE>(a, s.b);
     return s;
 }
 // the most units an item can have, by the cache's and the window's lengths
@@ -185,20 +255,24 @@ __device__ __forceinline__ void kv4_put_info(const Kv4Ws &ws, const Kv4Start &at
 }
 
 // A CTA's segments, one after another: units [x0, x1) of an item.
-template <int KT, int TPU, class Cost>
+template <int KT, int TPU, class Cost, int MODE>
 struct Kv4Seg {
     unsigned long long left;  // after this segment, in the measure of Cost
     int b, rt, h, x0, x1;
     int next_P, next_cnt;     // of the next sequence, loaded long before they are wanted
+    int next_shared;
+    int shared;               // positions of the sequence's prefix
     Kv4Keys key;
     __device__ __forceinline__ void ask(const Kv4Att &a) {
         const int nb = min(b + 1, a.B - 1);
         next_P = a.prefix[nb];
-        next_cnt = a.count ? a.count[nb] : a.n;
+        next_cnt = MODE != KV4_FIRST && a.count ? a.count[nb] : a.n;
+        next_shared = MODE == KV4_BEHIND ? a.shared_len[nb / a.per] : 0;
     }
     __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
         if (at.left == 0) return false;
         b = at.b, rt = at.rt, h = at.h, left = at.left, key = at.key;
+        shared = MODE == KV4_BEHIND ? a.shared_len[b / a.per] : 0;
         ask(a);
         return take(at.off);
     }
@@ -206,14 +280,13 @@ struct Kv4Seg {
         if (left == 0) return false;
         if (++h == a.H) {
             h = 0;
-            Kv4Seq sq{key.P, key.cnt, true};
+            int P = key.P, cnt = key.cnt;
             if (++rt == RT) {
                 rt = 0, ++b;
-                sq.P = next_P, sq.cnt = next_cnt;
+                P = next_P, cnt = next_cnt, shared = next_shared;
                 ask(a);
             }
-            sq.ok = sq.P >= 0 && sq.cnt >= 0 && sq.cnt <= a.n && (long long)sq.P + sq.cnt <= a.S;
-            key = kv4_keys<KT, TPU>(a, R, sq, rt);
+            key = kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, P, cnt, shared), rt, b);
         }
         return take(0);
     }
@@ -244,10 +317,13 @@ inline cudaError_t allow_smem(F *fn, int bytes, std::atomic<unsigned long long> 
     return e;
 }
 
+template <int MODE>
 cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cudaStream_t s);
 size_t kv4_few_ws(int n, int G, int D, int nsm);
+template <int MODE>
 cudaError_t launch_kv4_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
 size_t kv4_many_ws(int n, int G, int D, int nsm);
+template <int MODE>
 cudaError_t launch_kv4_many(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s);
 
 // ---------------------------------------------------------------------------
