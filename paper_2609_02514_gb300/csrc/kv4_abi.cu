@@ -212,7 +212,7 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
 }
 
 // Workspace of two passes: the first's sums, maxima, sums of weights and status, then what
-// either pass needs for itself.
+// each pass needs for itself.
 static size_t shared_part_bytes(int B, int groups, int n, int Hq, int D) {
     return (size_t)B * n * Hq * (D + 2) * 4 + ((size_t)groups * 4 + 15) / 16 * 16;
 }
@@ -221,7 +221,7 @@ size_t aces_kv4_shared_workspace_bytes(int B, int groups, int n, int Hq, int H, 
     const size_t own = aces_kv4_workspace_bytes(B, n, Hq, H, D);
     if (own == 0) return 0;
     const size_t first = aces_kv4_workspace_bytes(groups, B / groups * n, Hq, H, D);
-    return (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16 + (own > first ? own : first);
+    return (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16 + (first + 15) / 16 * 16 + own;
 }
 
 aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_t *q_strides, const void *shared, int shared_planes,
@@ -251,7 +251,8 @@ aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_
     a.part_l = a.part_m + rows;
     a.part_status = reinterpret_cast<int32_t *>(a.part_l + rows);
     a.shared_len = shared_len, a.shared_S = S0;
-    void *rest = reinterpret_cast<uint8_t *>(workspace) + (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16;
+    uint8_t *first_ws = reinterpret_cast<uint8_t *>(workspace) + (shared_part_bytes(B, groups, n, Hq, D) + 15) / 16 * 16;
+    uint8_t *own_ws = first_ws + (aces_kv4_workspace_bytes(groups, per * n, Hq, H, D) + 15) / 16 * 16;  // the passes run side by side
     Kv4Att f = a;
     f.k = sk, f.v = sv;
     f.B = groups, f.n = per * n, f.S = S0;
@@ -262,8 +263,8 @@ aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const auto first = many_rows(f.f32, f.B, H, f.n, f.G) ? launch_kv4_many<KV4_FIRST> : launch_kv4_few<KV4_FIRST>;
     const auto behind = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_BEHIND> : launch_kv4_few<KV4_BEHIND>;
-    if (first(f, rest, nsm, s) != cudaSuccess) return ACES_ERR_CUDA;
-    return behind(a, rest, nsm, s) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
+    if (first(f, first_ws, nsm, s) != cudaSuccess) return ACES_ERR_CUDA;
+    return behind(a, own_ws, nsm, s) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
 }
 
 aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const int64_t *q_strides, const int64_t *k_strides, int B, int n,

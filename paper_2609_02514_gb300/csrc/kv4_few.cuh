@@ -140,7 +140,9 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         for (int s = 0; s < ST; ++s) mbar_init(bar0 + 8 * s, 1);
     if (tid == 0) any_timeout = 0;
     const bool direct = CL > 0;  // clusters of CL CTAs an item, else shares
-    if (!direct) pdl_trigger();  // the join may be placed as CTAs leave; it waits for all of them
+    // the join may be placed as CTAs leave, and the second pass beside the first: each waits
+    // for all of them where it needs their results
+    if (!direct || MODE == KV4_FIRST) pdl_trigger();
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
     using Seg = Kv4Seg<FKT, FW, FewCost, MODE>;
@@ -148,7 +150,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     if (tid == 0 && !direct) kv4_put_info<FewCost>(ws, at);
     __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
-    if (!cur.start(a, R, RT, at)) return;
+    if (!cur.start(a, R, RT, at)) {
+        if (MODE == KV4_BEHIND) pdl_wait();
+        return;
+    }
     const int rank = CL > 1 ? blockIdx.x % CL : 0;
     if (CL > 1) cur.x0 = cur.key.units * rank / CL, cur.x1 = cur.key.units * (rank + 1) / CL;
 
@@ -453,6 +458,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         }
         for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
         if (more) q_info(cur, info ^ 1);
+        if (MODE == KV4_BEHIND) {
+            pdl_wait();  // for the first pass's sums
+            if (direct && first && tid == 0 && rank == 0 && h == 0 && rt == 0) a.status[b] = kv4_status<MODE>(a, b);
+        }
         // merge the warps
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -599,6 +608,7 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
     __shared__ float4 part[JW][D4];
     __shared__ float part_m[JW], part_l[JW];
     const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, warp = tid >> 5, lane = tid & 31;
+    if (MODE == KV4_FIRST) pdl_trigger();
     pdl_wait();
     if (c == 0) {
         if (y != 0) return;
@@ -771,10 +781,14 @@ static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid), cfg.blockDim = dim3(FT), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = s;
-    cudaLaunchAttribute shape;
-    shape.id = cudaLaunchAttributeClusterDimension;
-    shape.val.clusterDim.x = direct ? CL : 1, shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
-    cfg.attrs = &shape, cfg.numAttrs = CL > 1 ? 1 : 0;
+    cudaLaunchAttribute attrs[2];
+    cfg.attrs = attrs, cfg.numAttrs = 0;
+    if (CL > 1) {
+        cudaLaunchAttribute &shape = attrs[cfg.numAttrs++];
+        shape.id = cudaLaunchAttributeClusterDimension;
+        shape.val.clusterDim.x = CL, shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
+    }
+    if (MODE == KV4_BEHIND) kv4_beside(attrs[cfg.numAttrs++]);
     e = cudaLaunchKernelEx(&cfg, k_kv4_few<D, F32, NT, MODE>, a, ws, RT, CL);
     return e != cudaSuccess || direct ? e : launch_kv4_join<MODE>(a, ws, grid, C::R, s);
 }

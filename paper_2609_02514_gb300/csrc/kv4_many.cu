@@ -331,7 +331,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
     const Kv4Start at = kv4_start<MKT, 1, Cost, MT, MODE>(a, R, RT);
     if (tid == 0) kv4_put_info<Cost>(ws, at);
     Seg seg;
-    if (!seg.start(a, R, RT, at)) return;
+    if (!seg.start(a, R, RT, at)) {
+        if (MODE == KV4_BEHIND) pdl_wait();
+        return;
+    }
     if (warp == MMM) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -521,6 +524,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             }
             float k = whole && MODE != KV4_FIRST ? (live && l != 0.0f ? f * KV4_STEP / l : 0.0f) : f;
             float first_k = 0.0f, row_lse = 0.0f;  // the first pass's part (of the rows' first group)
+            if (MODE == KV4_BEHIND) pdl_wait();  // for the first pass's sums
             if (MODE == KV4_BEHIND && whole && r < NR) {
                 const Kv4Mix mix = kv4_mix(a, orow, m, l);
                 k = live ? f * mix.own : 0.0f, first_k = live && !(single && x == 1) ? mix.first : 0.0f;
@@ -762,6 +766,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
         if (leader) tc_commit(b_end);  // nothing runs on when the columns are given back
         if (!mbar_wait(b_end, 0)) bad = true;
     }
+    if (MODE == KV4_BEHIND) pdl_wait();
     if (bad) any_timeout = 1;
     __syncwarp();
     tc_before();
@@ -784,8 +789,12 @@ static cudaError_t run_many(const Kv4Att &a, void *workspace, int nsm, cudaStrea
     static std::atomic<unsigned long long> allowed{0};
     cudaError_t e = allow_smem(k_kv4_many<D, MODE>, Many<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    k_kv4_many<D, MODE><<<nsm, MT, Many<D>::SMEM, s>>>(a, ws, R, RT);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(nsm), cfg.blockDim = dim3(MT), cfg.dynamicSmemBytes = Many<D>::SMEM, cfg.stream = s;
+    cudaLaunchAttribute beside;
+    kv4_beside(beside);
+    cfg.attrs = &beside, cfg.numAttrs = MODE == KV4_BEHIND ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, k_kv4_many<D, MODE>, a, ws, R, RT);
     return e != cudaSuccess ? e : launch_kv4_join<MODE>(a, ws, nsm, R, s);
 }
 

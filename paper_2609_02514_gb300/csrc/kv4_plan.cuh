@@ -232,7 +232,8 @@ __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, in
     s.key = kv4_keys<KT, TPU, MODE>(a, R, s.b, s.rt);
     s.left = s.quantum = Cost::all(s.key);
     s.cnt = s.key.cnt;
-    if (threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
+    // (KV4_BEHIND: the first pass's status is not there yet)
+    if (MODE != KV4_BEHIND && threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
         a.status[s.b] = kv4_status<MODE>(a, s.b);
     return s;
 }
@@ -315,6 +316,12 @@ inline cudaError_t allow_smem(F *fn, int bytes, std::atomic<unsigned long long> 
     e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == cudaSuccess && dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
     return e;
+}
+
+// The second pass starts beside the first, whose sums it waits for before it uses them.
+inline void kv4_beside(cudaLaunchAttribute &a) {
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
 }
 
 template <int MODE>
