@@ -116,6 +116,7 @@ struct Kv4Att {
     int32_t *part_status;
     const int32_t *shared_len;  // [groups]
     int shared_S;
+    int longest_first;          // CTAs take the sequences by their lengths
     // the first pass: a sequence's tokens (n is a group's), its own positions and counts
     int own_n, own_S;
     const int32_t *own_prefix, *own_count;

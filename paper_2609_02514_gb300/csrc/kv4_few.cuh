@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 
     using Seg = Kv4Seg<FKT, FW, FewCost, MODE>;
-    const Kv4Start at = direct ? kv4_whole<FKT, FW, FewCost, MODE>(a, R, RT, CL) : kv4_start<FKT, FW, FewCost, FT, MODE>(a, R, RT);
+    const Kv4Start at = direct ? kv4_whole<FKT, FW, FewCost, FT, MODE>(a, R, RT, CL, reinterpret_cast<int *>(merge)) : kv4_start<FKT, FW, FewCost, FT, MODE>(a, R, RT);
     if (tid == 0 && !direct) kv4_put_info<FewCost>(ws, at);
     __syncwarp();  // each warp waits on its own barriers only
     Seg cur;
@@ -768,12 +768,14 @@ inline int few_cluster(long long items, int most, bool f32, int nsm) {
 }
 
 template <int D, bool F32, int NT, int MODE>
-static cudaError_t run_few(const Kv4Att &a, void *workspace, int nsm, cudaStream_t s) {
+static cudaError_t run_few(Kv4Att a, void *workspace, int nsm, cudaStream_t s) {
     using C = Few<D, F32, NT>;
     const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
     const long long items = (long long)a.B * RT * a.H;
     const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
     const bool direct = CL > 0;
+    // In more than one wave the long sequences go first: a late one would be waited for alone.
+    a.longest_first = CL == 1 && items > nsm * C::MINB && a.B > 1 && a.B <= KV4_RANKED;
     const int grid = direct ? (int)items * CL : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);
     static std::atomic<unsigned long long> allowed{0};

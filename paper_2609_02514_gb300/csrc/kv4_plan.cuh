@@ -222,12 +222,29 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
     return s;
 }
 
+// The sequence with `rank` longer ones before it (equal ones in their order), by all
+// NTH threads; len: shared memory for KV4_RANKED + 1 numbers.
+constexpr int KV4_RANKED = 512;
+template <int NTH>
+__device__ __forceinline__ int kv4_ranked(const Kv4Att &a, int rank, int *len) {
+    for (int b = threadIdx.x; b < a.B; b += NTH) len[b] = a.prefix[b] + (a.count ? a.count[b] : a.n);
+    __syncthreads();
+    for (int b = threadIdx.x; b < a.B; b += NTH) {
+        int before = 0;
+        for (int x = 0; x < a.B; ++x) before += len[x] > len[b] || (len[x] == len[b] && x < b);
+        if (before == rank) len[KV4_RANKED] = b;
+    }
+    __syncthreads();
+    return len[KV4_RANKED];
+}
+
 // Without shares: a cluster of CL CTAs has the whole item.
-template <int KT, int TPU, class Cost, int MODE>
-__device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, int CL) {
+template <int KT, int TPU, class Cost, int NTH, int MODE>
+__device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, int CL, int *scratch) {
     Kv4Start s;
     const int x = blockIdx.x / CL, e = x / a.H;
     s.h = x - e * a.H, s.b = e / RT, s.rt = e - s.b * RT;
+    if (MODE == KV4_BEHIND && a.longest_first) s.b = kv4_ranked<NTH>(a, s.b, scratch);
     s.off = 0;
     s.key = kv4_keys<KT, TPU, MODE>(a, R, s.b, s.rt);
     s.left = s.quantum = Cost::all(s.key);
