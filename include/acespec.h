@@ -437,7 +437,7 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *                prefix)
  *   q_weight, k_weight   float32 or bfloat16, [D] (stride 0) or a row for each
  *                head (stride D or more), or NULL: ones; only with norm
- *   eps          1e-30 .. 1e30
+ *   eps          1e-30 .. 1
  *   scale        2^-20 .. 2^20 (1 as a rule; of scaled position schemes)
  * Numbers are float32 inside (angles 64 bits); each result is rounded once.
  */

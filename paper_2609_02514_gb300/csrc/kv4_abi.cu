@@ -92,7 +92,7 @@ aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, c
     if (t->positions && (t->n_axes < 1 || t->n_axes > ACES_MAX_AXES || (t->n_axes > 1 && !t->axes))) return ACES_ERR_INVALID_ARG;
     if (t->depth && t->depth_stride != 0 && t->depth_stride < n) return ACES_ERR_INVALID_ARG;
     if (!(t->scale >= 0x1p-20 && t->scale <= 0x1p20)) return ACES_ERR_INVALID_ARG;
-    if (t->norm ? !(t->eps >= 1e-30 && t->eps <= 1e30) : (t->q_weight || t->k_weight)) return ACES_ERR_INVALID_ARG;
+    if (t->norm ? !(t->eps >= 1e-30 && t->eps <= 1.0) : (t->q_weight || t->k_weight)) return ACES_ERR_INVALID_ARG;
     const size_t es = dt == ACES_F32 ? 4 : 2;
     if ((uintptr_t)q % es || (uintptr_t)k % es) return ACES_ERR_INVALID_ARG;
     const void *w[2] = {t->q_weight, t->k_weight};
@@ -112,7 +112,8 @@ aces_status check_turn(const aces_turn *t, int D, int B, int n, int Hq, int H, c
     a->start = t->start, a->base = t->base, a->depth = t->depth, a->depth_b = t->depth_stride;
     a->R = t->rot_dim, a->n_axes = t->positions ? t->n_axes : 1, a->norm = t->norm;
     a->eps = t->eps, a->scale = t->scale;
-    a->eps32 = (float)t->eps, a->scale32 = (float)t->scale;
+    a->eps32 = (float)t->eps, a->eps_low = (float)(t->eps - a->eps32);
+    a->scale32 = (float)t->scale, a->scale_low = (float)(t->scale - a->scale32);
     a->B = B, a->n = n, a->Hq = Hq, a->H = H;
     return ACES_OK;
 }

@@ -20,10 +20,12 @@
 // The cache's codes are those of z in 64 bits, so that they do not depend on how sums and
 // products were ordered here.  Float32's z is within E of that; where a quotient lies
 // closer than that to a border, or the step could be another, the whole warp does the
-// row again in 64 bits (three rows of a thousand).
+// row again to 46 bits (three rows of a thousand; then one number of 10^12 may be decided
+// otherwise).
 #define ACES_FILE 10  // site numbers of the checked build
 #include "kv4_quant.cuh"
 #include "turn.cuh"
+#include "twofold.cuh"
 
 namespace aces {
 
@@ -36,7 +38,7 @@ constexpr long long SLICE_WARPS = 24;  // an SM's warps, below which units are c
 // (in place, a row is read by the lanes that write it, before they do: a plain load)
 __device__ __forceinline__ uint4 load16(const void *p) {
     uint4 v;
-    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 // 16 bytes of a row: its numbers, whatever the alignment
@@ -185,90 +187,122 @@ __device__ __forceinline__ bool quantise_near(float (&z)[G], float E, uint32_t (
     return none || (sure && far < 0.5f - fmaf(E, fabsf(inv), 1.0e-6f));
 }
 
-// A row in 64 bits, and into the cache, by a whole warp: a lane has D / 32 neighbouring
-// channels, four lanes a group.
+// 1 / (2 pi) in two parts
+constexpr double INV_TURN = 0.15915494309189535, INV_TURN_LO = -9.839338337591493e-18;
+
+// A row again, to some 46 bits, and into the cache, by a whole warp: a lane has D / 32
+// neighbouring channels, four lanes a group.
 template <int D, bool F32, bool INTER>
 static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h, uint8_t *row) {
     constexpr int G = D / KV4_GROUPS, CH = D / 32;
     constexpr uint32_t ALL = 0xffffffffu;
     const int lane = threadIdx.x & 31, d0 = lane * CH, half = a.R / 2;
     const long long at = b * a.k.b + i * a.k.i + h * a.k.h + d0;
-    double y[CH], ss = 0.0;
-#pragma unroll
-    for (int e = 0; e < CH; ++e) {
-        y[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
-                   : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
-        ss = fma(y[e], y[e], ss);
-    }
-    if (a.norm) {
-        for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(ALL, ss, x);
-        const double r = 1.0 / sqrt(ss / D + a.eps);
-#pragma unroll
-        for (int e = 0; e < CH; ++e) y[e] = y[e] * weight_at(a.kw, h * a.kw.h + d0 + e) * r;  // (x w is exact: equal ones stay equal)
-    }
     // A lane works out half of its pairs' cosines and sines: interleaved pairs are its own,
-    // the others are shared with the lane that has their other channels.
+    // the others are shared with the lane that has their other channels.  (The angle is
+    // rounded as a product in 64 bits is.)
     const bool turns = d0 < a.R, second = !INTER && d0 >= half;
     const int other = INTER || !turns ? lane : second ? lane - half / CH : lane + half / CH;
-    double sn[CH / 2], cn[CH / 2];
+    Two sn[CH / 2], cn[CH / 2];
 #pragma unroll
     for (int x = 0; x < CH / 2; ++x) {
-        sn[x] = 0.0, cn[x] = 1.0;
+        sn[x] = {0.0f, 0.0f}, cn[x] = {1.0f, 0.0f};
         if (!turns) continue;
         const int j = INTER ? d0 / 2 + x : second ? d0 - half + CH / 2 + x : d0 + x;
-        sincos((double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j), &sn[x], &cn[x]);
+        const double angle = (double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j);
+        const double hi = angle * INV_TURN, lo = fma(angle, INV_TURN, -hi) + angle * INV_TURN_LO;  // turns, in two parts
+        const double t = hi - rint(hi) + lo;
+        const float th = (float)t;
+        two_sincos({th, (float)(t - th)}, sn[x], cn[x]);
     }
-    double z[CH];
+    float xs[CH], big = 0.0f;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        xs[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
+                    : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
+        big = fmaxf(big, fabsf(xs[e]));
+    }
+    Two y[CH];
+#pragma unroll
+    for (int e = 0; e < CH; ++e) y[e] = {xs[e], 0.0f};
+    if (a.norm) {
+        // numbers whose squares pass float32: 2^-70 of them (eps is nothing beside those)
+        const float down = __any_sync(ALL, big > 0x1p55f) ? 0x1p-70f : 1.0f;
+        Two ss = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+            xs[e] *= down;
+            ss = ss + two_product(xs[e], xs[e]);
+        }
+        for (int x = 16; x > 0; x >>= 1) ss = ss + Two{__shfl_xor_sync(ALL, ss.h, x), __shfl_xor_sync(ALL, ss.l, x)};
+        const Two m = Two{ss.h / D, ss.l / D} + (down == 1.0f ? Two{a.eps32, a.eps_low} : Two{0.0f, 0.0f});
+        const Two r = two_rsqrt(m);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) y[e] = two_product(xs[e], weight_at(a.kw, h * a.kw.h + d0 + e)) * r;  // (x w is exact: equal ones stay equal)
+    }
+    Two z[CH];
+    auto turned = [&](Two u, Two v, Two c, Two s) {  // u c - v s
+        Two p = u * c + -(v * s);
+        // (what is not finite has no second part)
+        return fabsf(p.h) <= FLT_MAX && fabsf(p.l) <= FLT_MAX ? p : Two{fmaf(u.h, c.h, -(v.h * s.h)), 0.0f};
+    };
     if (INTER) {
 #pragma unroll
         for (int x = 0; x < CH / 2; ++x) {
-            const double u = y[2 * x], v = y[2 * x + 1];
-            z[2 * x] = u * cn[x] - v * sn[x];
-            z[2 * x + 1] = v * cn[x] + u * sn[x];
+            z[2 * x] = turned(y[2 * x], y[2 * x + 1], cn[x], sn[x]);
+            z[2 * x + 1] = turned(y[2 * x + 1], -y[2 * x], cn[x], sn[x]);
         }
     } else {
 #pragma unroll
         for (int e = 0; e < CH; ++e) {
             const int x = e % (CH / 2);
             const bool mine = (e >= CH / 2) == second;
-            const double yo = __shfl_sync(ALL, y[e], other), so = __shfl_sync(ALL, sn[x], other), co = __shfl_sync(ALL, cn[x], other);
-            const double s = mine ? sn[x] : so, c = mine ? cn[x] : co;
-            z[e] = second ? y[e] * c + yo * s : y[e] * c - yo * s;
+            const Two yo = {__shfl_sync(ALL, y[e].h, other), __shfl_sync(ALL, y[e].l, other)};
+            const Two so = {__shfl_sync(ALL, sn[x].h, other), __shfl_sync(ALL, sn[x].l, other)};
+            const Two co = {__shfl_sync(ALL, cn[x].h, other), __shfl_sync(ALL, cn[x].l, other)};
+            z[e] = turned(y[e], second ? -yo : yo, mine ? cn[x] : co, mine ? sn[x] : so);
         }
     }
-    constexpr double CAP = (double)KV4_CAP;
-    double top = 0.0;
+    Two top = {0.0f, 0.0f};
+    auto larger = [](Two p, Two q) {  // in magnitude
+        const float ph = fabsf(p.h), qh = fabsf(q.h);
+        return ph > qh || (ph == qh && copysignf(1.0f, p.h) * p.l > copysignf(1.0f, q.h) * q.l);
+    };
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
-        z[e] = turns ? z[e] * a.scale : y[e];
-        z[e] = z[e] == z[e] ? fmin(fmax(z[e], -CAP), CAP) : 0.0;
-        if (fabs(z[e]) > fabs(top)) top = z[e];  // the first of the largest
+        z[e] = !turns ? y[e] : a.scale == 1.0 ? z[e] : turned(z[e], {0.0f, 0.0f}, {a.scale32, a.scale_low}, {0.0f, 0.0f});
+        if (!(z[e].h == z[e].h)) z[e] = {0.0f, 0.0f};
+        if (larger(z[e], {KV4_CAP, 0.0f})) z[e] = {copysignf(KV4_CAP, z[e].h), 0.0f};
+        if (larger(z[e], top)) top = z[e];  // the first of the largest
     }
 #pragma unroll
     for (int x = 1; x < 4; x <<= 1) {
-        const double o = __shfl_xor_sync(ALL, top, x);
-        if (lane & x ? fabs(o) >= fabs(top) : fabs(o) > fabs(top)) top = o;
+        const Two o = {__shfl_xor_sync(ALL, top.h, x), __shfl_xor_sync(ALL, top.l, x)};
+        if (lane & x ? !larger(top, o) : larger(o, top)) top = o;
     }
-    // -top / 2^19 in five significant bits, ties to even
-    double t = 0.0;
-    if (fabs(top) >= (double)KV4_TINY) {
-        const unsigned long long bits = (unsigned long long)__double_as_longlong(-top * 1.9073486328125e-06);
-        unsigned long long m = bits & 0x7FFFFFFFFFFFFFFFull;
-        m = (m + 0x7FFFFFFFFFFFull + ((m >> 48) & 1ull)) & ~0xFFFFFFFFFFFFull;
-        t = __longlong_as_double((long long)((bits & 0x8000000000000000ull) | m));
+    // The step: kv4_t() of the first part, but that where this lies on a half the second
+    // one decides.
+    float t = larger({KV4_TINY, 0.0f}, top) ? 0.0f : kv4_t(top.h);
+    if (t != 0.0f && top.l != 0.0f && (__float_as_uint(top.h) & 0x7FFFFu) == 0x40000u) {
+        const bool up = (top.l > 0.0f) == (top.h > 0.0f);
+        const uint32_t u = __float_as_uint(top.h * -1.9073486328125e-06f) & ~0x7FFFFu;  // -2^-19
+        t = __uint_as_float(u + (up ? 0x80000u : 0u));
     }
-    const double s = t * (double)KV4_STEP;
+    const float s = t * KV4_STEP, inv = s == 0.0f ? 0.0f : __frcp_rn(s), hs = 0.5f * fabsf(s);
     uint32_t w = 0u;
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
         const int c = (d0 + e) & 7;  // of its word
-        const double r = s == 0.0 ? 0.0 : fmin(fmax(rint(z[e] / s), -8.0), 7.0);
-        w |= (uint32_t)((int)r + 8) << (4 * (c >> 1) + 16 * (c & 1));
+        float r = rintf(z[e].h * inv);
+        const float d = fmaf(-r, s, z[e].h);  // exact, on the grid of the halves
+        const bool along = (z[e].l > 0.0f) == (d > 0.0f);
+        if (fabsf(d) > hs || (fabsf(d) == hs && hs != 0.0f && (z[e].l == 0.0f ? ((int)r & 1) : along))) r += (d > 0.0f) == (s > 0.0f) ? 1.0f : -1.0f;
+        w |= (uint32_t)((int)fminf(fmaxf(r, -8.0f), 7.0f) + 8) << (4 * (c >> 1) + 16 * (c & 1));
     }
 #pragma unroll
     for (int x = 1; x < 8 / CH; x <<= 1) w |= __shfl_xor_sync(ALL, w, x);
     if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = w;
-    if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint((float)t) >> 16);
+    if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint(t) >> 16);
 }
 
 // ---------------------------------------------------------------------------
@@ -474,8 +508,7 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     for (int x = 0; x < 2; ++x) {
         const int j = lane + 32 * x;
         if (j >= R / 2) continue;
-        const double f = __ldg(a.freq + j), hi = f * 0.15915494309189535;
-        const double lo = fma(f, 0.15915494309189535, -hi) + f * -9.839338337591493e-18;
+        const double f = __ldg(a.freq + j), hi = f * INV_TURN, lo = fma(f, INV_TURN, -hi) + f * INV_TURN_LO;
         const unsigned long long u = __double2ull_rz((hi - floor(hi)) * 0x1p64) + (unsigned long long)__double2ll_rn(lo * 0x1p64);
         fh[x] = (uint32_t)(u >> 32), fl[x] = (uint32_t)u;
         axis[x] = turn_axis(a, j);
@@ -489,6 +522,16 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
 
     // units: some tokens of a sequence, and a share of their rows
     const uint32_t per = (uint32_t)(a.n + T - 1) >> lt, units = (uint32_t)a.B * per * slices;
+    // positions of the lane's pairs, asked for a unit ahead
+    int p_next[2];
+    auto ask = [&](uint32_t x) {
+        if (x >= units) return;
+        const uint32_t unit = slices > 1 ? x / slices : x, b = unit / per;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            if (lane + 32 * y < R / 2) p_next[y] = turn_position(a, (int)b, (int)(unit - b * per) * T, axis[y]);
+    };
+    ask(blockIdx.x * TW + warp);
 #pragma unroll 1
     for (uint32_t x = blockIdx.x * TW + warp; x < units; x += gridDim.x * TW) {
         const uint32_t unit = slices > 1 ? x / slices : x;
@@ -528,12 +571,13 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
             for (int y = 0; y < 2; ++y) {
                 const int j = lane + 32 * y;
                 if (j >= R / 2) continue;
-                const uint32_t p = (uint32_t)turn_position(a, b, i0 + tok, axis[y]);
+                const uint32_t p = (uint32_t)(tok == 0 ? p_next[y] : turn_position(a, b, i0 + tok, axis[y]));
                 const uint32_t turns = p * fh[y] + __umulhi(p, fl[y]) - (p >> 31 ? fl[y] : 0u);
                 float sn, cn;
                 sincospif((float)(int)turns * 0x1p-31f, &sn, &cn);
                 cs[tok * D + j] = cn * a.scale32, cs[tok * D + D / 2 + j] = sn * a.scale32;
             }
+        ask(x + gridDim.x * TW);
         if (APPEND && lane < TOKENS) st[lane] = 0;
         __syncwarp();
 

@@ -25,7 +25,7 @@ struct Turn {
     TurnWeight qw, kw;
     int R, n_axes, norm;
     double eps, scale;
-    float eps32, scale32;
+    float eps32, eps_low, scale32, scale_low;  // in two parts
     int B, n, Hq, H;
     // append
     uint8_t *ck, *cv;

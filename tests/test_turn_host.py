@@ -43,7 +43,7 @@ TURN_REFUSALS = [
     (dict(positions=FAKE, n_axes=0), 1), (dict(positions=FAKE, n_axes=5, axes=FAKE), 1), (dict(positions=FAKE, n_axes=2), 1),
     (dict(depth=FAKE, depth_stride=2), 1), (dict(depth=FAKE, depth_stride=-3), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
     (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(scale=2.0 ** 21), 1), (dict(norm=1), 1), (dict(norm=1, eps=-1.0), 1),
-    (dict(norm=1, eps=1e-31), 1), (dict(norm=1, eps=float("nan")), 1), (dict(norm=1, eps=1e31), 1), (dict(q_weight=FAKE), 1),
+    (dict(norm=1, eps=1e-31), 1), (dict(norm=1, eps=float("nan")), 1), (dict(norm=1, eps=1.5), 1), (dict(norm=1, eps=float("inf")), 1), (dict(q_weight=FAKE), 1),
     (dict(k_weight=FAKE), 1), (dict(norm=1, eps=1e-6, q_weight=FAKE, q_weight_dt=3), 2),
     (dict(norm=1, eps=1e-6, k_weight=FAKE, k_weight_stride=32), 1), (dict(norm=1, eps=1e-6, k_weight=FAKE + 2, k_weight_dt=0), 1)]
 
