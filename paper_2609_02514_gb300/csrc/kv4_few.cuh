@@ -602,14 +602,16 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
 // (a warp a row, two at a time: 14.1), 7.6 for 300 of four rows, with cold caches.
 constexpr int JN = 256, JW = JN / 32;
 template <int D, bool F32, int MODE>
-__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y) {
+__global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int R, int Y, int items) {
     constexpr int D4 = D / 4, PW = 32 / D4;  // float4 of a row; pieces a warp reads at a time
     __shared__ int late;
     __shared__ float4 part[JW][D4];
     __shared__ float part_m[JW], part_l[JW];
-    const int tid = threadIdx.x, c = blockIdx.x / Y, y = blockIdx.x - c * Y, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, group = blockIdx.x / Y, y = blockIdx.x - group * Y, warp = tid >> 5, lane = tid & 31;
+    const bool deep = MODE == KV4_FIRST && items > 0;
     if (MODE == KV4_FIRST) pdl_trigger();
     pdl_wait();
+    int c = deep ? (group == items ? 0 : -1) : group;
     if (c == 0) {
         if (y != 0) return;
         if (tid == 0) late = 0;
@@ -621,9 +623,23 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
             a.status[b] = kv4_status<MODE>(a, b) | (late ? ACES_ROW_TIMEOUT : 0);
         return;
     }
-    const Kv4Info in = ws.info[c];
     // inside the item, and the first to start there
-    if (in.cnt < 0 || in.off < in.inside || in.off - in.quantum >= in.inside) return;
+    auto joins = [](const Kv4Info &in) { return in.cnt >= 0 && in.off >= in.inside && in.off - in.quantum < in.inside; };
+    if (deep) {  // a block has an item and looks for that CTA
+        __shared__ int at;
+        if (tid == 0) at = -1;
+        __syncthreads();
+        const int RT = (a.n * a.G + R - 1) / R;
+        for (int x = tid; x < C; x += JN) {
+            const Kv4Info in = ws.info[x];
+            if (joins(in) && (in.b * RT + in.rt) * a.H + in.h == group) at = x;
+        }
+        __syncthreads();
+        c = at;
+        if (c < 0) return;
+    }
+    const Kv4Info in = ws.info[c];
+    if (!joins(in)) return;
     const int pieces = 1 + (in.all - in.off + in.quantum - 1) / in.quantum;
     const int stride = R * (D + 2), NR = min(R, a.n * a.G - in.rt * R);
     const float *first = ws.piece + (size_t)(2 * (c - 1) + (in.off >= in.quantum ? 0 : 1)) * stride;
@@ -664,7 +680,13 @@ __global__ void __launch_bounds__(JN) k_kv4_join(Kv4Att a, Kv4Ws ws, int C, int 
         const int r = in.rt * R + row, i = r / a.G;
         put_row<D, F32, MODE>(a, ((size_t)in.b * a.n + i) * a.Hq + in.h * a.G + (r - i * a.G), d4, o, M, L, i < in.cnt);
     };
-    if (pieces <= 3 || NR > 16) {
+    if (deep) {  // a warp a row, eight pieces under way
+        for (int row = y * JW + warp; row < NR; row += Y * JW) {
+            float M, L;
+            const float4 o = add(row, 0, 1, M, L);
+            if (lane < D4) put(row, lane, o, M, L);
+        }
+    } else if (pieces <= 3 || NR > 16) {
         constexpr int LN = 8, RW = 32 / LN, V = D4 / LN;  // lanes of a row, rows of a warp
         const int d4 = lane % LN;
         for (int row0 = (y * JW + warp) * RW; row0 < NR; row0 += Y * JW * RW) {
@@ -737,7 +759,14 @@ cudaError_t launch_kv4_join(const Kv4Att &a, const Kv4Ws &ws, int C, int R, cuda
     const int Y = rows <= 16 ? rows : (rows + 31) / 32;  // blocks of an item
     const auto fn = a.D == 64 ? (a.f32 ? k_kv4_join<64, true, MODE> : k_kv4_join<64, false, MODE>)
                               : (a.f32 ? k_kv4_join<128, true, MODE> : k_kv4_join<128, false, MODE>);
-    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y);
+    // A prefix's few items, each in many pieces: blocks by items, a row a warp.  (Eight
+    // items of 256 rows in 19 pieces: 64 blocks by CTAs 19.1 us, these 11.1, with cold caches.)
+    const long long items = (long long)a.B * ((a.n * a.G + R - 1) / R) * a.H;
+    if (MODE == KV4_FIRST && rows > 16 && items * 4 <= C) {
+        const int by_item = (rows + JW - 1) / JW;
+        return launch_after(fn, ((int)items + 1) * by_item, JN, 1, s, a, ws, C, R, by_item, (int)items);
+    }
+    return launch_after(fn, C * Y, JN, 1, s, a, ws, C, R, Y, 0);
 }
 
 // CTAs of a cluster that has an item to itself, or 0: shares and a join.  An item's
