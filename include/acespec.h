@@ -70,7 +70,7 @@ typedef enum { ACES_F32 = 0, ACES_BF16 = 1 } aces_dtype;
 #define ACES_ROW_NONFINITE 1 /* NaN / +inf logits, or all logits -inf      */
 #define ACES_ROW_BAD_Q 2     /* invalid draft probability or draft token   */
 #define ACES_ROW_TIMEOUT 4   /* a wait for a kernel's own copies or products
-                                gave up after seconds (aces_kv4_attention):
+                                gave up after seconds (the attention calls):
                                 the results are not valid                */
 #define ACES_ROW_RANGE 8     /* positions outside the cache (aces_kv4_*)   */
 
@@ -423,7 +423,7 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *   t = p * inv_freq[j] in 64 bits, p the token's position on the pair's axis
  * for the pairs j < rot_dim / 2 of channels (u, v): (j, j + rot_dim / 2), or
  * with interleaved (2 j, 2 j + 1).  Channels from rot_dim on stay y.
- *   inv_freq     [rot_dim / 2] float32
+ *   inv_freq     [rot_dim / 2] float32, finite
  *   rot_dim      a multiple of D / 4, at most D
  *   axes         [rot_dim / 2] int32 or NULL: the pairs' axes (beyond 0 ..
  *                n_axes - 1 the nearest; needed with more than one)

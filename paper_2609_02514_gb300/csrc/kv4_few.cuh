@@ -803,7 +803,8 @@ static cudaError_t run_few(Kv4Att a, void *workspace, int nsm, cudaStream_t s) {
     const long long items = (long long)a.B * RT * a.H;
     const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
     const bool direct = CL > 0;
-    // In more than one wave the long sequences go first: a late one would be waited for alone.
+    // In more than one wave the long sequences go first: a late one would be waited for alone
+    // (64 sequences of 100 to 2000 positions behind an empty prefix: 59 -> 55 us).
     a.longest_first = CL == 1 && items > nsm * C::MINB && a.B > 1 && a.B <= KV4_RANKED;
     const int grid = direct ? (int)items * CL : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);

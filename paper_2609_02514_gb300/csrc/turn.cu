@@ -22,6 +22,16 @@
 // closer than that to a border, or the step could be another, the whole warp does the
 // row again to 46 bits (three rows of a thousand; then one number of 10^12 may be decided
 // otherwise).
+//
+// What bounds it.  Rotation of 8192 tokens of two sequences, 32 and 8 heads of 128 in
+// bfloat16 (336 MB): 66 us, 5.1 TB/s; without norms 62, a copy of as many dense bytes 52.
+// The warps wait for their loads: neither more warps of fewer registers (five or six CTAs an
+// SM: 72, 73 us) nor more steps under way (72) nor fewer instructions were faster, and the
+// other forms that were measured were slower: eight rows a step with tables in shared
+// memory 76, a CTA for some tokens with a barrier behind its tables 81.
+// Into the cache, 80 tokens of 64 sequences: 44 us (111 MB), 35 when no row is done again: a
+// warp that meets one is late by some 9 us, and has two or three tokens in all.  In
+// float64 those rows made it 48, one after another by their four lanes 94.
 #define ACES_FILE 10  // site numbers of the checked build
 #include "kv4_quant.cuh"
 #include "turn.cuh"
@@ -31,7 +41,10 @@ namespace aces {
 
 constexpr int TW = 4, TN = TW * 32;
 constexpr int TOKENS = 8;  // of a warp, at most
-constexpr long long SLICE_WARPS = 24;  // an SM's warps, below which units are cut
+// A unit's rows go to several warps while there are fewer units than this for an SM (image
+// tokens, 4611 of 12 and 4 heads of 64 in float32: 24 of them 12.4 us, 36 15.5; with 0 one
+// token of 32 and 8 heads 10.5 us instead of 8).
+constexpr long long SLICE_WARPS = 24;
 
 // ---------------------------------------------------------------------------
 // loads and stores
@@ -486,7 +499,7 @@ __device__ __forceinline__ void turn_heads(const Turn &a, const TurnHeads &from,
     }
 }
 
-constexpr int TURN_CTAS = 4;  // an SM
+constexpr int TURN_CTAS = 4;  // an SM, of up to 128 registers a thread
 
 // VEC: every 16 bytes lie on their grid; FULL: all channels turn.
 template <int D, bool F32, bool APPEND, bool INTER, bool VEC, bool FULL>
@@ -521,12 +534,12 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     __syncthreads();
 
     // units: some tokens of a sequence, and a share of their rows
-    const uint32_t per = (uint32_t)(a.n + T - 1) >> lt, units = (uint32_t)a.B * per * slices;
+    const uint32_t per = (uint32_t)(a.n + T - 1) >> lt, whole = (uint32_t)a.B * per, units = whole * slices;
     // positions of the lane's pairs, asked for a unit ahead
     int p_next[2];
     auto ask = [&](uint32_t x) {
         if (x >= units) return;
-        const uint32_t unit = slices > 1 ? x / slices : x, b = unit / per;
+        const uint32_t unit = x % whole, b = unit / per;
 #pragma unroll
         for (int y = 0; y < 2; ++y)
             if (lane + 32 * y < R / 2) p_next[y] = turn_position(a, (int)b, (int)(unit - b * per) * T, axis[y]);
@@ -534,8 +547,9 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     ask(blockIdx.x * TW + warp);
 #pragma unroll 1
     for (uint32_t x = blockIdx.x * TW + warp; x < units; x += gridDim.x * TW) {
-        const uint32_t unit = slices > 1 ? x / slices : x;
-        const int slice = (int)(x - unit * slices), b = (int)(unit / per), i0 = (int)(unit - b * per) * T, tokens = min(T, a.n - i0);
+        // (all first slices, which cost the most, before the others)
+        const uint32_t share = slices > 1 ? x / whole : 0, unit = x - share * whole;
+        const int slice = (int)share, b = (int)(unit / per), i0 = (int)(unit - b * per) * T, tokens = min(T, a.n - i0);
         // The warp's share: of rows for the cache, eight at a time, keys then values, all in the
         // first slice, which has the tokens' status; of the others steps of every token.
         const int ok = (tokens * a.H + 7) >> 3, ks = APPEND ? 0 : (a.H + RW - 1) / RW, steps = ks + (a.Hq + RW - 1) / RW;
@@ -711,7 +725,6 @@ template <int D, bool F32, bool APPEND, bool INTER>
 static cudaError_t run_turn(const Turn &a, int nsm, cudaStream_t s) {
     const int lt = turn_tokens(a, APPEND, nsm);
     const long long units = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
-    // A unit's rows go to several warps while those are few.
     constexpr int RW = 512 / D;
     const int most = APPEND ? 1 + (a.Hq + RW - 1) / RW : (a.H + RW - 1) / RW + (a.Hq + RW - 1) / RW;
     int slices = 1;
