@@ -70,6 +70,7 @@ constexpr uint32_t KV4_BITS = (8u - 0x4B400000u) * 0x11111111u;
 struct Kv4Seq {
     int P, cnt;
     bool ok;
+    int shared;  // positions of its prefix (KV4_BEHIND, KV4_SPLIT)
 };
 __device__ __forceinline__ Kv4Seq kv4_seq(const int32_t *prefix, const int32_t *count, int b, int n, int S) {
     Kv4Seq q;
@@ -83,8 +84,9 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const int32_t *prefix, const int32_t *
 // sequences share prefixes.  The first takes a prefix for a sequence and all tokens of
 // those that share it (its group) for its new tokens, which see nothing but the prefix;
 // it leaves its sums, not yet divided, with their maximum and the sum of their weights.
-// The second takes each sequence's own rows, and adds those sums as one more piece.
-enum { KV4_ALONE = 0, KV4_FIRST = 1, KV4_BEHIND = 2 };
+// The second takes each sequence's own rows, and adds those sums as one more piece.  Or
+// one pass has every sequence's rows in two places, its prefix's tiles before its own.
+enum { KV4_ALONE = 0, KV4_FIRST = 1, KV4_BEHIND = 2, KV4_SPLIT = 3 };
 
 // Position of new token t: its depth in the tree (a negative or absurd one is
 // taken as the nearest sensible one), or its number.
@@ -116,6 +118,7 @@ struct Kv4Att {
     int32_t *part_status;
     const int32_t *shared_len;  // [groups]
     int shared_S;
+    const uint8_t *k0, *v0;     // KV4_SPLIT: the prefixes' planes [groups, H, shared_S, row]
     int longest_first;          // CTAs take the sequences by their lengths
     // the first pass: a sequence's tokens (n is a group's), its own positions and counts
     int own_n, own_S;

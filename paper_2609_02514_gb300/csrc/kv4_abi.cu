@@ -135,6 +135,27 @@ bool apart(const int64_t *stride, int B, int n, int H, int D) {
 }
 TurnHeads heads(const void *p, const int64_t *s) { return {const_cast<void *>(p), s[0], s[1], s[2]}; }
 
+// Whether a prefix's rows are worth a pass of their own: it saves every sequence's work
+// on them but one's, and costs the parts' way through memory, more launches and a second
+// set of items.  In microseconds, of the prefix's capacity or the window:
+//   few rows: 256 keys of an item take a CTA 1.75, two CTAs an SM (float32 three times);
+//   many: 128 keys of 256 rows 2.1 of an SM, of up to 128 rows two thirds of it.
+constexpr double FEW_EXTRA = 20.0, MANY_EXTRA = 50.0;
+bool two_passes(const Kv4Att &a, int groups, int nsm) {
+    long long keys = a.shared_S;
+    if (a.window && keys > (long long)a.window + a.sinks) keys = (long long)a.window + a.sinks;
+    auto work = [&](int sequences, long long rows) {
+        if (many_rows(a.f32, sequences, a.H, (int)(rows / a.G), a.G)) {
+            const long long rest = rows % 256;
+            return 2.1 / 6 * (rows / 256 * 6 + (rest == 0 ? 0 : rest <= 128 ? 4 : 6)) * sequences * a.H * (keys / 128.0) / nsm;
+        }
+        return (a.f32 ? 5.2 : 1.75) * ((rows + 15) / 16) * sequences * a.H * (keys / 256.0) / (2.0 * nsm);
+    };
+    const long long rows = (long long)a.n * a.G;
+    const bool many = many_rows(a.f32, a.B, a.H, a.n, a.G);
+    return work(a.B, rows) - work(groups, rows * a.per) > (many ? MANY_EXTRA : FEW_EXTRA);
+}
+
 }  // namespace
 
 extern "C" {
@@ -262,6 +283,11 @@ aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_
     a.k = pk, a.v = pv, a.S = S;
     const int nsm = sm_count();
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (!two_passes(a, groups, nsm)) {
+        a.k0 = sk, a.v0 = sv;
+        const auto split = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_SPLIT> : launch_kv4_few<KV4_SPLIT>;
+        return split(a, own_ws, nsm, s) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
+    }
     const auto first = many_rows(f.f32, f.B, H, f.n, f.G) ? launch_kv4_many<KV4_FIRST> : launch_kv4_few<KV4_FIRST>;
     const auto behind = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_BEHIND> : launch_kv4_few<KV4_BEHIND>;
     if (first(f, first_ws, nsm, s) != cudaSuccess) return ACES_ERR_CUDA;

@@ -81,7 +81,7 @@ __device__ __forceinline__ void put_row(const Kv4Att &a, size_t orow, int d4, fl
         if (d4 == 0) a.part_m[orow] = M, a.part_l[orow] = L;
         return;
     }
-    const bool none = !live || (MODE == KV4_ALONE && L == 0.0f);
+    const bool none = !live || (MODE != KV4_BEHIND && L == 0.0f);
     float k = none ? 0.0f : KV4_STEP / L, lse = none ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     if (none) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (MODE == KV4_BEHIND && !none) {
@@ -161,18 +161,23 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     bool bad = false;  // a wait gave up
     // this warp's y-th tile of the segment, into the ring's next place
     const uint8_t *kb = nullptr, *vb = nullptr;  // the key head's rows
-    auto place_rows = [&](const Seg &g) { kb = a.k + g.row0(a) * RB, vb = a.v + g.row0(a) * RB; };
+    const uint8_t *kb0 = nullptr, *vb0 = nullptr;  // and its prefix's
+    auto place_rows = [&](const Seg &g) {
+        kb = a.k + g.row0(a) * RB, vb = a.v + g.row0(a) * RB;
+        if (MODE == KV4_SPLIT) kb0 = a.k0 + g.row0_prefix(a) * RB, vb0 = a.v0 + g.row0_prefix(a) * RB;
+    };
     place_rows(cur);
     auto issue = [&](const Seg &g, int y, int place) {
         if (lane != 0 || bad) return;
-        const int j0 = kv4_tile<FKT>(g.key, (g.x0 + y) * FW + warp), rows = min(FKT, kv4_end<MODE>(g.key) - j0);
-        if (!ACES_IN(j0, a.S) || !ACES_IN(j0 + rows - 1, a.S)) return;
+        const Kv4Place at = kv4_place<FKT, MODE>(g.key, (g.x0 + y) * FW + warp);
+        const int j0 = at.j0, rows = min(FKT, (at.prefix ? g.key.s0 : kv4_end<MODE>(g.key)) - j0), S = at.prefix ? a.shared_S : a.S;
+        if (!ACES_IN(j0, S) || !ACES_IN(j0 + rows - 1, S)) return;
         const int s = place % ST;
         const uint32_t bytes = rows * RB, dst = ring + s * C::STAGE;
         const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)RB;
         mbar_expect(bar0 + 8 * s, 2 * bytes);
-        bulk_load(dst, kb + off, bytes, bar0 + 8 * s);
-        bulk_load(dst + FKT * RB, vb + off, bytes, bar0 + 8 * s);
+        bulk_load(dst, (at.prefix ? kb0 : kb) + off, bytes, bar0 + 8 * s);
+        bulk_load(dst + FKT * RB, (at.prefix ? vb0 : vb) + off, bytes, bar0 + 8 * s);
     };
     auto my_tiles = [&](const Seg &g) {
         const int top = min(g.x1 * FW, g.key.tiles) - g.x0 * FW - warp;
@@ -289,7 +294,10 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 mbar_drain<ST>(bar0, seq);
             }
             const uint8_t *kt = ringp + s * C::STAGE, *vt = kt + FKT * RB;
-            const int j0 = kv4_tile<FKT>(key, (cur.x0 + y) * FW + warp);
+            const Kv4Place place = kv4_place<FKT, MODE>(key, (cur.x0 + y) * FW + warp);
+            const int j0 = place.j0;
+            // (rows' positions are counted from the sequence's own first one)
+            const int shift = place.prefix ? key.s0 : 0, first_sinks = place.prefix ? a.sinks : sinks, sure = place.prefix ? key.s0 : all_see;
             float S[NT][2][4];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
@@ -335,7 +343,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 }
             }
             // scores to weights
-            const bool masked = j0 + FKT > all_see || (a.window && j0 <= posmax - a.window && j0 + FKT > sinks);
+            const bool masked = j0 + FKT > sure || (a.window && j0 <= posmax + shift - a.window && j0 + FKT > first_sinks);
             uint32_t pk[NT][2][SPL][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -347,7 +355,8 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                             for (int x = 0; x < 2; ++x)
-                                if (ri.x < 0 || !kv4_sees<MODE>(a, b, P, end, sinks, j0 + mt * 16 + x * 8 + g, ri.x, ri.y))
+                                if (ri.x < 0 || !(place.prefix ? kv4_sees<KV4_FIRST>(a, b, key.s0, key.s0, a.sinks, j0 + mt * 16 + x * 8 + g, ri.x, ri.y + shift)
+                                                               : kv4_sees<MODE>(a, b, P, end, sinks, j0 + mt * 16 + x * 8 + g, ri.x, ri.y)))
                                     S[nt][mt][2 * x + c] = -INFINITY;
                     }
                 }
@@ -801,7 +810,7 @@ static cudaError_t run_few(Kv4Att a, void *workspace, int nsm, cudaStream_t s) {
     using C = Few<D, F32, NT>;
     const int RT = (int)(((long long)a.n * a.G + C::R - 1) / C::R);
     const long long items = (long long)a.B * RT * a.H;
-    const int most = kv4_most_units(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
+    const int most = kv4_most_units<MODE>(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
     const bool direct = CL > 0;
     // In more than one wave the long sequences go first: a late one would be waited for alone
     // (64 sequences of 100 to 2000 positions behind an empty prefix: 59 -> 55 us).

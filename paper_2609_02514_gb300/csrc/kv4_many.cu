@@ -422,8 +422,11 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                         tc_after();
                     }
                     if (warp_live) {
-                        const int j0 = kv4_tile<MKT>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1)) + half * MKH;
-                        const bool masked = j0 + MKH > all_see || (a.window && j0 <= posmax - a.window && j0 + MKH > sinks);
+                        const Kv4Place place = kv4_place<MKT, MODE>(key, seg.x0 + (single ? (y & ~1) + x : y >> 1));
+                        const int j0 = place.j0 + half * MKH;
+                        // (rows' positions are counted from the sequence's own first one)
+                        const int shift = place.prefix ? key.s0 : 0, first_sinks = place.prefix ? a.sinks : sinks, sure = place.prefix ? key.s0 : all_see;
+                        const bool masked = j0 + MKH > sure || (a.window && j0 <= posmax + shift - a.window && j0 + MKH > first_sinks);
                         const uint32_t at = tS + half * MKH;
                         float v[2][32];
                         tc_ld32(at, v[0]);
@@ -432,7 +435,10 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
                         tc_wait_ld(v[1]);
                         if (masked) {
                             uint32_t see0 = 0u, see1 = 0u;
-                            if (row_live)
+                            if (row_live && place.prefix)
+                                see0 = seen_word<KV4_FIRST>(a, b, key.s0, 0, a.sinks, j0, i, pos + shift),
+                                see1 = seen_word<KV4_FIRST>(a, b, key.s0, 0, a.sinks, j0 + 32, i, pos + shift);
+                            else if (row_live)
                                 see0 = seen_word<MODE>(a, b, P, key.cnt, sinks, j0, i, pos), see1 = seen_word<MODE>(a, b, P, key.cnt, sinks, j0 + 32, i, pos);
 #pragma unroll
                             for (int c = 0; c < 32; ++c) {
@@ -668,30 +674,34 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             uint32_t step = 0;
             do {
                 const uint8_t *kb = a.k + seg.row0(a) * C::RB, *vb = a.v + seg.row0(a) * C::RB;  // the key head's rows
+                const uint8_t *kb0 = nullptr, *vb0 = nullptr;                                    // and its prefix's
+                if (MODE == KV4_SPLIT) kb0 = a.k0 + seg.row0_prefix(a) * C::RB, vb0 = a.v0 + seg.row0_prefix(a) * C::RB;
                 const int top = min(seg.x1, seg.key.tiles), end = kv4_end<MODE>(seg.key);
                 int ahead = seg.x0 + 1;
 #pragma unroll 1
                 for (int y = seg.x0; y < top && !bad; ++y) {
                     for (; ahead < min(top, y + AHEAD); ++ahead) {
-                        const int j0 = kv4_tile<MKT>(seg.key, ahead);
-                        const uint32_t bytes = min(MKT, end - j0) * C::RB;
+                        const Kv4Place place = kv4_place<MKT, MODE>(seg.key, ahead);
+                        const int j0 = place.j0;
+                        const uint32_t bytes = min(MKT, (place.prefix ? seg.key.s0 : end) - j0) * C::RB;
                         const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)C::RB;
-                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(kb + off), "r"(bytes) : "memory");
-                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(vb + off), "r"(bytes) : "memory");
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((place.prefix ? kb0 : kb) + off), "r"(bytes) : "memory");
+                        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((place.prefix ? vb0 : vb) + off), "r"(bytes) : "memory");
                     }
-                    const int j0 = kv4_tile<MKT>(seg.key, y);
+                    const Kv4Place place = kv4_place<MKT, MODE>(seg.key, y);
+                    const int j0 = place.j0, stop = place.prefix ? seg.key.s0 : end, S = place.prefix ? a.shared_S : a.S;
                     // past the sequence's end the ring keeps what it has: any bytes are
                     // numbers, and their weights are 0
-                    const uint32_t bytes = min(MKT, end - j0) * C::RB;
+                    const uint32_t bytes = min(MKT, stop - j0) * C::RB;
                     const unsigned long long off = (unsigned long long)(uint32_t)j0 * (uint32_t)C::RB;
-                    const bool in = ACES_IN(j0, a.S) && ACES_IN(end - 1, a.S);
+                    const bool in = ACES_IN(j0, S) && ACES_IN(stop - 1, S);
 #pragma unroll 1
                     for (int v = 0; v < 2; ++v, ++step) {
                         const uint32_t rs = step % C::NR;
                         wait(b_rfree + 8 * rs, step / C::NR + 1);
                         if (bad) break;
                         mbar_expect(b_rfull + 8 * rs, in ? bytes : 0);
-                        if (in) bulk_load(raw0 + rs * C::RAW, (v ? vb : kb) + off, bytes, b_rfull + 8 * rs);
+                        if (in) bulk_load(raw0 + rs * C::RAW, (place.prefix ? (v ? vb0 : kb0) : (v ? vb : kb)) + off, bytes, b_rfull + 8 * rs);
                     }
                 }
             } while (!bad && seg.next(a, R, RT));
@@ -806,6 +816,7 @@ cudaError_t launch_kv4_many(const Kv4Att &a, void *workspace, int nsm, cudaStrea
 template cudaError_t launch_kv4_many<KV4_ALONE>(const Kv4Att &, void *, int, cudaStream_t);
 template cudaError_t launch_kv4_many<KV4_FIRST>(const Kv4Att &, void *, int, cudaStream_t);
 template cudaError_t launch_kv4_many<KV4_BEHIND>(const Kv4Att &, void *, int, cudaStream_t);
+template cudaError_t launch_kv4_many<KV4_SPLIT>(const Kv4Att &, void *, int, cudaStream_t);
 
 size_t kv4_many_ws(int n, int G, int D, int nsm) { return kv4_ws_bytes(nsm, many_rows_of(n, G), D) + (size_t)nsm * 256 * (D + 1) * 4; }
 

@@ -65,31 +65,33 @@ struct Kv4Keys {
     int lo, hi, s_hi;
     int st, mt0, tiles, units;
     int rows;              // of the tile
-    int sinks;             // first positions that stay visible (KV4_BEHIND: of the sequence's own)
+    int sinks;             // first positions that stay visible (KV4_BEHIND, KV4_SPLIT: of the sequence's own)
+    int s0, st0, m0, t0;   // KV4_SPLIT: the prefix's positions, and its tiles, which come first
     bool live;
 };
 
 // A sequence's cached positions and new ones, from its lengths (shared: of its prefix).
 template <int MODE>
 __device__ __forceinline__ Kv4Seq kv4_seq_of(const Kv4Att &a, int P, int cnt, int shared) {
-    Kv4Seq q{P, MODE == KV4_FIRST ? a.n : cnt, true};
+    Kv4Seq q{P, MODE == KV4_FIRST ? a.n : cnt, true, 0};
     if (MODE == KV4_FIRST)
         q.ok = P >= 0 && P <= a.S;
     else
         q.ok = P >= 0 && cnt >= 0 && cnt <= a.n && (long long)P + cnt <= a.S;
-    if (MODE == KV4_BEHIND) q.ok = q.ok && shared >= 0 && shared <= a.shared_S;
+    q.shared = shared;
+    if (MODE >= KV4_BEHIND) q.ok = q.ok && shared >= 0 && shared <= a.shared_S;
     return q;
 }
 template <int MODE>
 __device__ __forceinline__ Kv4Seq kv4_seq_of(const Kv4Att &a, int b) {
     if (MODE == KV4_ALONE) return kv4_seq(a.prefix, a.count, b, a.n, a.S);
-    return kv4_seq_of<MODE>(a, a.prefix[b], MODE == KV4_BEHIND && a.count ? a.count[b] : a.n, MODE == KV4_BEHIND ? a.shared_len[b / a.per] : 0);
+    return kv4_seq_of<MODE>(a, a.prefix[b], MODE >= KV4_BEHIND && a.count ? a.count[b] : a.n, MODE >= KV4_BEHIND ? a.shared_len[b / a.per] : 0);
 }
 // one behind the last position whose rows are read
 template <int MODE>
 __device__ __forceinline__ int kv4_end(const Kv4Keys &k) { return MODE == KV4_FIRST ? k.P : k.P + k.cnt; }
 template <int MODE>
-__device__ __forceinline__ int kv4_sinks(const Kv4Att &a, const Kv4Keys &k) { return MODE == KV4_BEHIND ? k.sinks : a.sinks; }
+__device__ __forceinline__ int kv4_sinks(const Kv4Att &a, const Kv4Keys &k) { return MODE >= KV4_BEHIND ? k.sinks : a.sinks; }
 template <int MODE>
 __device__ __forceinline__ int32_t kv4_status(const Kv4Att &a, int b) {
     return (kv4_seq_of<MODE>(a, b).ok ? 0 : ACES_ROW_RANGE) | (MODE == KV4_BEHIND ? a.part_status[b / a.per] : 0);
@@ -130,7 +132,7 @@ __device__ __forceinline__ Kv4Mix kv4_mix(const Kv4Att &a, size_t row, float M, 
 }
 
 template <int KT, int TPU, int MODE>
-__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq &sq, int rt, int b) {
+__device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq &sq, int rt) {
     Kv4Keys k;
     k.P = sq.P, k.cnt = sq.cnt;
     const int r0 = rt * R, r1 = min(r0 + R, a.n * a.G);  // at most 2^30 rows
@@ -141,7 +143,7 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq
     k.lo = k.hi = k.s_hi = k.st = k.mt0 = k.tiles = 0;
     k.sinks = a.sinks;
     if (k.live) {
-        if (MODE == KV4_BEHIND && a.sinks > 0) k.sinks = max(0, a.sinks - a.shared_len[b / a.per]);
+        if (MODE >= KV4_BEHIND) k.sinks = max(0, a.sinks - sq.shared);
         if (MODE == KV4_FIRST) {
             k.hi = k.P;
             k.lo = a.window ? max(0, k.P - a.window + 1) : 0;
@@ -154,17 +156,38 @@ __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, const Kv4Seq
         k.mt0 = max(k.lo / KT, k.st);
         k.tiles = k.st + max(0, (k.hi + KT - 1) / KT - k.mt0);
     }
+    k.s0 = k.st0 = k.m0 = k.t0 = 0;
+    if (MODE == KV4_SPLIT && k.live) {
+        k.s0 = sq.shared;
+        const int lo = a.window ? min(max(0, k.s0 + k.P + (a.mask ? 0 : k.i0) - a.window + 1), k.s0) : 0;
+        k.st0 = (min(a.sinks, lo) + KT - 1) / KT;
+        k.m0 = max(lo / KT, k.st0);
+        k.t0 = k.st0 + (lo < k.s0 ? max(0, (k.s0 + KT - 1) / KT - k.m0) : 0);
+        k.tiles += k.t0;
+    }
     k.units = max(1, (k.tiles + TPU - 1) / TPU);
     return k;
 }
 template <int KT, int TPU, int MODE>
 __device__ __forceinline__ Kv4Keys kv4_keys(const Kv4Att &a, int R, int b, int rt) {
-    return kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, b), rt, b);
+    return kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, b), rt);
 }
 // first key of the x-th tile
 template <int KT>
 __device__ __forceinline__ int kv4_tile(const Kv4Keys &k, int x) {
     return (x < k.st ? x : k.mt0 + x - k.st) * KT;
+}
+
+// The x-th tile: its first key, and whether that is of the prefix (KV4_SPLIT).
+struct Kv4Place {
+    int j0;
+    bool prefix;
+};
+template <int KT, int MODE>
+__device__ __forceinline__ Kv4Place kv4_place(const Kv4Keys &k, int x) {
+    if (MODE != KV4_SPLIT) return {kv4_tile<KT>(k, x), false};
+    if (x < k.t0) return {(x < k.st0 ? x : k.m0 + x - k.st0) * KT, true};
+    return {kv4_tile<KT>(k, x - k.t0), false};
 }
 
 // Whether new or old position j is seen by token i at position pos (of the passes of two:
@@ -261,8 +284,9 @@ __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, in
     return s;
 }
 // the most units an item can have, by the cache's and the window's lengths
+template <int MODE>
 inline int kv4_most_units(const Kv4Att &a, int keys) {
-    long long most = a.S;
+    long long most = MODE == KV4_SPLIT ? (long long)a.S + a.shared_S + 2 * keys : a.S;  // (two ends inside tiles)
     if (a.window) most = most < (long long)a.window + a.sinks + a.n + 2 * keys ? most : (long long)a.window + a.sinks + a.n + 2 * keys;
     return (int)((most + keys - 1) / keys);
 }
@@ -291,12 +315,12 @@ struct Kv4Seg {
         const int nb = min(b + 1, a.B - 1);
         next_P = a.prefix[nb];
         next_cnt = MODE != KV4_FIRST && a.count ? a.count[nb] : a.n;
-        next_shared = MODE == KV4_BEHIND ? a.shared_len[nb / a.per] : 0;
+        next_shared = MODE >= KV4_BEHIND ? a.shared_len[nb / a.per] : 0;
     }
     __device__ __forceinline__ bool start(const Kv4Att &a, int R, int RT, const Kv4Start &at) {
         if (at.left == 0) return false;
         b = at.b, rt = at.rt, h = at.h, left = at.left, key = at.key;
-        shared = MODE == KV4_BEHIND ? a.shared_len[b / a.per] : 0;
+        shared = MODE >= KV4_BEHIND ? a.shared_len[b / a.per] : 0;
         ask(a);
         return take(at.off);
     }
@@ -310,7 +334,7 @@ struct Kv4Seg {
                 P = next_P, cnt = next_cnt, shared = next_shared;
                 ask(a);
             }
-            key = kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, P, cnt, shared), rt, b);
+            key = kv4_keys<KT, TPU, MODE>(a, R, kv4_seq_of<MODE>(a, P, cnt, shared), rt);
         }
         return take(0);
     }
@@ -325,6 +349,8 @@ struct Kv4Seg {
     }
     // first row of the item's key head in a plane
     __device__ __forceinline__ size_t row0(const Kv4Att &a) const { return (size_t)((size_t)b * a.H + h) * a.S; }
+    // and of its prefix's
+    __device__ __forceinline__ size_t row0_prefix(const Kv4Att &a) const { return (size_t)((size_t)(b / a.per) * a.H + h) * a.shared_S; }
     __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == key.units; }
 };
 

@@ -1,5 +1,6 @@
 """kv4_shared_attention against float64 numpy over each sequence's rows in one piece: its
-prefix's, then its own.  The bounds are test_gpu_kv4.py's; the two passes' sums come
+prefix's, then its own.  Short prefixes are read by every sequence; a pass of their own goes
+by the shared cache's capacity, so the same sizes run both ways.  The bounds are test_gpu_kv4.py's; the two passes' sums come
 together as its pieces do (an exponential, a product and an add each in float32, 2^-21
 together), which its 2^-17 for exponentials and sums has room for."""
 import numpy as np
@@ -66,9 +67,19 @@ SHAPES = [
 ]
 
 
+def _roomy(A, shared):
+    """The same prefixes in a cache of 3 million positions (of all of them together)."""
+    planes, groups, H, S0, R = shared.shape
+    wide = torch.empty(planes, groups, H, 3_000_000 // (groups * H), R, dtype=torch.uint8, device="cuda")
+    wide[:, :, :, :S0] = shared
+    wide[:, :, :, S0:S0 + 200] = 255
+    return wide
+
+
+@pytest.mark.parametrize("passes", [1, 2])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", SHAPES, ids=lambda c: "-".join(map(str, c)).replace(" ", "")[:60])
-def test_attention_is_the_definition(A, case, dtype):
+def test_attention_is_the_definition(A, case, dtype, passes):
     B, n, Hq, H, D, lens, P, form, window, sinks = case
     rng = np.random.default_rng(B + 7 * n + Hq + lens[0])
     mask = depth = words = dev_depth = None
@@ -85,6 +96,8 @@ def test_attention_is_the_definition(A, case, dtype):
     for b in range(B):
         cache[:, b, :, P[b] + cnt[b]:] = 255
     q = _torch(rng.standard_normal((B, n, Hq, D)) * 0.8, dtype)
+    if passes == 2:
+        shared = _roomy(A, shared)
     r = A.kv4_shared_attention(q, shared, _i32(lens), cache, 1, _i32(P), mask=words, depth=dev_depth, count=_i32(cnt), window=window,
                                sinks=sinks)
     torch.cuda.synchronize()
@@ -92,9 +105,28 @@ def test_attention_is_the_definition(A, case, dtype):
     _check(r, _f64(q), (K0, V0), lens, (K, V), P, cnt, dtype, D ** -0.5, mask, depth, window, sinks)
 
 
+# windows so wide, of so many sequences, that the prefix has its own pass
+@pytest.mark.parametrize("B,groups,n,Hq,H,D,length,window,sinks,dtype", [
+    (128, 1, 1, 8, 8, 64, 1500, 1000, 4, "bf16"), (96, 2, 1, 16, 8, 128, 1300, 1200, 1300, "bf16"), (128, 1, 1, 4, 4, 64, 1100, 700, 7, "f32"),
+    (24, 1, 20, 16, 8, 64, 6500, 6000, 5, "bf16")])
+def test_windows_of_large_batches(A, B, groups, n, Hq, H, D, length, window, sinks, dtype):
+    rng = np.random.default_rng(B)
+    lens = [length - 100 * g for g in range(groups)]
+    shared, K0, V0 = _filled(A, rng, groups, H, length + 900, D)
+    cache, K, V = _filled(A, rng, B, H, 60 + n, D)
+    P, cnt = [int(x) for x in rng.integers(0, 60, B)], [n] * B
+    q = _torch(rng.standard_normal((B, n, Hq, D)), dtype)
+    r = A.kv4_shared_attention(q, shared, _i32(lens), cache, 0, _i32(P), window=window, sinks=sinks)
+    for b in (0, 1, B // 2 - 1, B // 2, B - 1):
+        g = b // (B // groups)
+        _check({key: r[key][b:b + 1] for key in ("out", "lse")}, _f64(q)[b:b + 1], (K0[g:g + 1], V0[g:g + 1]), lens[g:g + 1], (K[b:b + 1], V[b:b + 1]),
+               P[b:b + 1], cnt[b:b + 1], dtype, D ** -0.5, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("passes", [1, 2])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,Hq,H", [(6, 4, 2), (50, 6, 2)])
-def test_any_mask_any_strides(A, dtype, n, Hq, H):
+def test_any_mask_any_strides(A, dtype, n, Hq, H, passes):
     """A mask and depths of every sequence, rows that see nothing, another scale, and
     queries inside a wider array off the 16-byte grid."""
     B, D, lens = 4, 64, [0, 40]
@@ -110,22 +142,27 @@ def test_any_mask_any_strides(A, dtype, n, Hq, H):
     wide = torch.zeros(B, n, Hq * D + 3, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
     q = wide[:, :, 1:1 + Hq * D].unflatten(-1, (Hq, D))
     q.copy_(_torch(rng.standard_normal((B, n, Hq, D)), dtype))
-    for window, sinks in ((0, 0), (6, 2), (60, 0)):
+    if passes == 2:
+        shared = _roomy(A, shared)
+    for window, sinks in ((0, 0), (6, 2), (60, 0), (2_000_000, 0)):
         r = A.kv4_shared_attention(q, shared, _i32(lens), cache, 0, _i32(P), mask=_words(mask), depth=_i32(depth), count=_i32(cnt), scale=0.21,
                                    window=window, sinks=sinks)
         _check(r, _f64(q), (K0, V0), lens, (K, V), P, cnt, dtype, 0.21, mask, depth, window, sinks)
         assert not r["out"][0, 2].any() and torch.isneginf(r["lse"][0, 2]).all() and not r["out"][3].any()
 
 
+@pytest.mark.parametrize("passes", [1, 2])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 40])
-def test_sequences_outside_the_caches(A, dtype, n):
+def test_sequences_outside_the_caches(A, dtype, n, passes):
     B, Hq, H, D, S, S0 = 8, 4, 2, 128, 60, 30
     rng = np.random.default_rng(3)
     shared, K0, V0 = _filled(A, rng, 4, H, S0, D)
     cache, K, V = _filled(A, rng, B, H, S, D)
     q = _torch(rng.standard_normal((B, n, Hq, D)), dtype)
-    lens, P, cnt = [30, -1, 31, 4], [-1, 20, 3, 4, 5, 6, 61 - n, 0], [n, n, n, n, n, n, n, n + 1]
+    if passes == 2:
+        shared = _roomy(A, shared)
+    lens, P, cnt = [30, -1, shared.shape[3] + 1, 4], [-1, 20, 3, 4, 5, 6, 61 - n, 0], [n, n, n, n, n, n, n, n + 1]
     r = A.kv4_shared_attention(q, shared, _i32(lens), cache, 0, _i32(P), count=_i32(cnt))
     np.testing.assert_array_equal(r["status"].cpu().numpy(), [8, 0, 8, 8, 8, 8, 8, 8])
     for b in (0, 2, 3, 4, 5, 6, 7):
@@ -133,13 +170,16 @@ def test_sequences_outside_the_caches(A, dtype, n):
     _check({key: r[key][1:2] for key in ("out", "lse")}, _f64(q)[1:2], (K0, V0), [30], (K[1:2], V[1:2]), [20], [n], dtype, D ** -0.5)
 
 
+@pytest.mark.parametrize("passes", [1, 2])
 @pytest.mark.parametrize("n", [1, 40])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_a_bad_query_spoils_its_own_row(A, n, dtype):
+def test_a_bad_query_spoils_its_own_row(A, n, dtype, passes):
     B, Hq, H, D, S = 24, 4, 2, 64, 100
     rng = np.random.default_rng(4)
     shared, _, _ = _filled(A, rng, 1, H, 90, D)
     cache, _, _ = _filled(A, rng, B, H, S, D)
+    if passes == 2:
+        shared = _roomy(A, shared)
     q = _torch(rng.standard_normal((B, n, Hq, D)), dtype)
     P, cnt = _i32(list(range(B))), _i32([n] * (B - 1) + [n - 1])
     call = lambda x: A.kv4_shared_attention(x, shared, _i32([80]), cache, 0, P, count=cnt)  # noqa: E731
@@ -156,8 +196,9 @@ def test_a_bad_query_spoils_its_own_row(A, n, dtype):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("passes", [1, 2])
 @pytest.mark.parametrize("n,B", [(1, 3), (1, 50), (40, 3)])
-def test_it_is_the_attention_over_one_cache(A, n, B):
+def test_it_is_the_attention_over_one_cache(A, n, B, passes):
     """Against kv4_attention over caches that hold the prefix's rows before their own, moved as bytes."""
     Hq, H, D, S0, lens = 8, 2, 128, 500, [437]
     rng = np.random.default_rng(B)
@@ -168,6 +209,8 @@ def test_it_is_the_attention_over_one_cache(A, n, B):
     whole[:, :, :, :437] = shared[:, :, :, :437]
     whole[:, :, :, 437:437 + 200 + n] = cache
     q = _torch(rng.standard_normal((B, n, Hq, D)), "bf16")
+    if passes == 2:
+        shared = _roomy(A, shared)
     for window, sinks in ((0, 0), (300, 4)):
         r = A.kv4_shared_attention(q, shared, _i32(lens), cache, 0, _i32(P), window=window, sinks=sinks)
         one = A.kv4_attention(q, whole, 0, _i32(437 + P), window=window, sinks=sinks)
@@ -176,13 +219,16 @@ def test_it_is_the_attention_over_one_cache(A, n, B):
         assert (r["lse"] - one["lse"]).abs().max() <= 2.0 ** -17 * 40
 
 
-def test_graphs_streams_and_workspaces(A):
+@pytest.mark.parametrize("passes", [1, 2])
+def test_graphs_streams_and_workspaces(A, passes):
     B, n, Hq, H, D = 12, 1, 8, 2, 128
     rng = np.random.default_rng(9)
     shared, _, _ = _filled(A, rng, 2, H, 3000, D)
     cache, _, _ = _filled(A, rng, B, H, 300, D)
     q = _torch(rng.standard_normal((B, n, Hq, D)), "bf16")
     lens, P = _i32([3000, 2500]), _i32(list(range(0, 12 * 20, 20)))
+    if passes == 2:
+        shared = _roomy(A, shared)
     want = A.kv4_shared_attention(q, shared, lens, cache, 0, P)
     need = A.kv4_shared_workspace_bytes(B, 2, n, Hq, H, D)
     ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
