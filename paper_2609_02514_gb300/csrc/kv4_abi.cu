@@ -140,7 +140,14 @@ TurnHeads heads(const void *p, const int64_t *s) { return {const_cast<void *>(p)
 // set of items.  In microseconds, of the prefix's capacity or the window:
 //   few rows: 256 keys of an item take a CTA 1.75, two CTAs an SM (float32 three times);
 //   many: 128 keys of 256 rows 2.1 of an SM, of up to 128 rows two thirds of it.
-constexpr double FEW_EXTRA = 20.0, MANY_EXTRA = 50.0;
+// Measured (us, one pass / two; 32 heads over 8 of 128, 50 to 500 own positions; saved by
+// the estimate in brackets): one token of 4 sequences behind 2000 positions 15 / 26 (1), of
+// 16 29 / 31 (5), of 8 behind 8000 34 / 32 (9), of 32 behind 2000 40 / 36 (10), of 4 behind
+// 32000 49 / 37 (17), of 16 behind 8000 54 / 36 (18); 20 tokens of 8 behind 8000 79 / 89
+// (18), of 4 behind 32000 121 / 129 (28), of 16 behind 8000 131 / 119 (39); 80 tokens of 8
+// behind 8000 191 / 189 (23), of 32 behind 2000 239 / 262 (23), of 16 behind 8000 347 / 326 (46).  Float32, 12 heads
+// over 4 of 64: one token of 32 behind 2000 26 / 27 (14), of 8 behind 16000 33 / 31 (26).
+constexpr double FEW_EXTRA = 7.0, F32_EXTRA = 20.0, MANY_EXTRA = 33.0;
 bool two_passes(const Kv4Att &a, int groups, int nsm) {
     long long keys = a.shared_S;
     if (a.window && keys > (long long)a.window + a.sinks) keys = (long long)a.window + a.sinks;
@@ -153,7 +160,7 @@ bool two_passes(const Kv4Att &a, int groups, int nsm) {
     };
     const long long rows = (long long)a.n * a.G;
     const bool many = many_rows(a.f32, a.B, a.H, a.n, a.G);
-    return work(a.B, rows) - work(groups, rows * a.per) > (many ? MANY_EXTRA : FEW_EXTRA);
+    return work(a.B, rows) - work(groups, rows * a.per) > (many ? MANY_EXTRA : a.f32 ? F32_EXTRA : FEW_EXTRA);
 }
 
 }  // namespace

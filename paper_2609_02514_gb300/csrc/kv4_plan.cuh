@@ -13,12 +13,14 @@
 // one CTA's range is written out by it; the pieces of one that several share go
 // to the workspace as sums not yet divided, with their reference maximum, and
 // k_kv4_join adds them in the CTAs' order.
-// Passes: a batch behind shared prefixes (KV4_FIRST, KV4_BEHIND in kv4.cuh) runs the same
-// kernels twice.  All rows of a group's sequences meet their prefix as one many-row item a
-// tile, so its keys are read and dequantised once for 256 rows, not once a sequence: 64
-// requests of one token behind 16384 positions (32 heads over 8 of 128, 100 to 2000 own
-// positions) take 75 us; with the prefix in each one's own cache there are 1.43 GB to read, 210
-// us at the copy rate, and kv4_attention takes XX.
+// Passes: a batch behind shared prefixes runs the kernels twice (KV4_FIRST, KV4_BEHIND in
+// kv4.cuh), where that pays (the rule in kv4_abi.cu): all rows of a group's sequences
+// meet their prefix as one item's, so its keys are read and dequantised once for 256
+// rows, not once a sequence.  64 requests of one token behind 16384 positions (32 heads
+// over 8 of 128, 100 to 2000 own positions) take 76 us; with the prefix's rows in each one's
+// own cache there are 1.43 GB to read, and kv4_attention takes 274.  The second pass runs
+// beside the first and waits for it only where it adds its sums.  Elsewhere one pass
+// (KV4_SPLIT) has a sequence's tiles in two places.
 // Where no item can have more than KV4_DIRECT units for each CTA of a cluster, or one
 // CTA (the cache is short, or the window), it takes the item and adds its parts up in
 // shared memory: nothing to join (few rows only: few_cluster() and its figures).
