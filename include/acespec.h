@@ -526,7 +526,8 @@ aces_status aces_kv4_attention(const void *q, aces_dtype dt, const int64_t *q_st
 /*
  * The same attention for a batch whose sequences share prefixes (a system
  * prompt, a document): the prefixes' rows lie in a cache of their own, and are
- * read once for all sequences that share them.
+ * read once for all sequences that share them, in a pass of its own, where S0 (or
+ * the window), B and n make that pay; else by each sequence.
  *   shared        [shared_planes, groups, H, S0, R]: a cache as above, of the
  *                 same layers, whose sequence g is the prefix of sequences g * B /
  *                 groups .. of the batch (B a multiple of groups)

@@ -557,7 +557,8 @@ def kv4_shared_workspace_bytes(B: int, groups: int, n: int, Hq: int, H: int, D: 
 
 def kv4_shared_attention(q, shared, shared_len, cache, layer: int, prefix_len, mask=None, depth=None, count=None, scale: float | None = None,
                          window: int = 0, sinks: int = 0, out: dict | None = None, workspace: torch.Tensor | None = None):
-    """kv4_attention() for a batch whose sequences share prefixes, whose rows are read once for all.
+    """kv4_attention() for a batch whose sequences share prefixes, whose rows lie once, and where
+    that pays are read once for all.
 
     shared [2 * layers, groups, H, S0, D / 2 + 16]: a kv4_cache() whose sequence g holds the prefix of
     sequences g * B / groups .. of the batch, shared_len [groups] int32 its positions.  cache and

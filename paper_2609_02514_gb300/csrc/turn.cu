@@ -42,7 +42,7 @@ namespace aces {
 constexpr int TW = 4, TN = TW * 32;
 constexpr int TOKENS = 8;  // of a warp, at most
 // A unit's rows go to several warps while there are fewer units than this for an SM (image
-// tokens, 4611 of 12 and 4 heads of 64 in float32: 24 of them 12.4 us, 36 15.5; with 0 one
+// tokens, 4611 of 12 and 4 heads of 64 in float32: with 24 12.4 us, with 36 15.5; with 0 one
 // token of 32 and 8 heads 10.5 us instead of 8).
 constexpr long long SLICE_WARPS = 24;
 
