@@ -24,12 +24,11 @@
 // otherwise).
 //
 // What bounds it.  Rotation of 8192 tokens of two sequences, 32 and 8 heads of 128 in
-// bfloat16 (336 MB): 66 us, 5.1 TB/s; without norms 62, a copy of as many dense bytes 52.
-// The warps wait for their loads: neither more warps of fewer registers (five or six CTAs an
-// SM: 72, 73 us) nor more steps under way (72) nor fewer instructions were faster, and the
-// other forms that were measured were slower: eight rows a step with tables in shared
-// memory 76, a CTA for some tokens with a barrier behind its tables 81.
-// Into the cache, 80 tokens of 64 sequences: 44 us (111 MB), 35 when no row is done again: a
+// bfloat16 (336 MB): 59 us, 5.7 TB/s; a copy of as many dense bytes takes 52.  Bytes under way
+// are what counts: through registers, which hold two steps, it was 66 whatever the number of
+// warps or instructions, and with a pipeline that ran dry behind every token; four steps of
+// 1 KB a warp through shared memory, across tokens, are enough (six: 59).
+// Into the cache, 80 tokens of 64 sequences: 45 us (111 MB), 35 when no row is done again: a
 // warp that meets one is late by some 9 us, and has two or three tokens in all.  In
 // float64 those rows made it 48, one after another by their four lanes 94.
 #define ACES_FILE 10  // site numbers of the checked build
@@ -397,34 +396,108 @@ __device__ __forceinline__ void turn4(float (&y)[2][HC], int c, int e, const flo
     }
 }
 
-// Heads of one token that stay numbers, steps [s0, s1) of 32 / LN heads each, the next
-// but one step's loads under way.  ws: weights that all heads share; cs: the token's cosines
-// and sines.
-template <int D, bool F32, bool INTER, bool VEC, bool FULL>
-__device__ __forceinline__ void turn_heads(const Turn &a, const TurnHeads &from, const TurnHeads &to, const TurnWeight &wt, const float *ws,
-                                           const float *cs, int b, int i, int heads, int s0, int s1) {
+// What a warp works on: tokens [i0, i0 + tokens) of a sequence, and a share of their rows:
+// of those for the cache all, in the first slice, which has the tokens' status; of the
+// others steps [s0, s1) of every token (keys, then queries; RW heads a step).
+struct Unit {
+    int b, i0, tokens, slice, s0, s1;
+};
+struct Units {
+    uint32_t per, whole, units, stride;  // of a sequence, of a slice, in all; from one of a warp's to its next
+    int T, slices, first, ks, steps;     // first: slices without steps
+    __device__ __forceinline__ Unit at(const Turn &a, uint32_t x) const {
+        Unit u;
+        // (all first slices, which cost the most, before the others)
+        const uint32_t share = slices > 1 ? x / whole : 0, unit = x - share * whole;
+        u.slice = (int)share, u.b = (int)(unit / per), u.i0 = (int)(unit - u.b * per) * T, u.tokens = min(T, a.n - u.i0);
+        u.s0 = 0, u.s1 = steps;
+        if (slices > 1) {
+            u.s0 = u.slice < first ? 0 : steps * (u.slice - first) / (slices - first);
+            u.s1 = u.slice < first ? 0 : steps * (u.slice - first + 1) / (slices - first);
+        }
+        return u;
+    }
+};
+
+// The steps of a rotation's warp in their order, DEPTH of them under way into the warp's ring
+// in shared memory: each lane copies its own numbers and reads them back, so nothing but
+// its own copies is waited for.
+template <int D, bool F32, bool INTER, bool FULL>
+struct Feed {
+    using My = Lane<D, F32, INTER, FULL, false>;
+    static constexpr int W = My::W, LN = My::LN, RW = 32 / LN, DEPTH = F32 ? 2 : 4, RING = DEPTH * 2 * W * 512;
+    Units all;
+    Unit u;
+    uint32_t x, ring;
+    int s, tok, put, get;
+    __device__ __forceinline__ void open(const Turn &a) {
+        for (; x < all.units; x += all.stride) {
+            u = all.at(a, x);
+            if (u.s0 < u.s1) break;
+        }
+        s = u.s0, tok = 0;
+    }
+    __device__ __forceinline__ void start(const Turn &a, const Units &w, uint32_t x0, uint32_t place) {
+        all = w, x = x0, ring = place + (threadIdx.x & 31) * 16, put = get = 0;
+        u = Unit{0, 0, 0, 0, 0, 0};
+        open(a);
+        for (int p = 0; p < DEPTH; ++p) ask(a);
+    }
+    __device__ __forceinline__ void ask(const Turn &a) {
+        if (x < all.units) {
+            const int lane = threadIdx.x & 31;
+            const My my{lane % LN, FULL ? D : a.R};
+            const bool q = s >= all.ks;
+            const TurnHeads &from = q ? a.q : a.k;
+            // (lanes without a head have the last one's numbers)
+            const int h = min((q ? s - all.ks : s) * RW + lane / LN, (q ? a.Hq : a.H) - 1);
+            const char *p = reinterpret_cast<const char *>(from.p) + (u.b * from.b + (u.i0 + tok) * from.i + h * from.h) * (F32 ? 4 : 2);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (put * 2 * W + c * W + w) * 512),
+                                 "l"(p + my.chan(c, w) * (F32 ? 4 : 2))
+                                 : "memory");
+            if (++s == u.s1) {
+                s = u.s0;
+                if (++tok == u.tokens) x += all.stride, open(a);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        put = put + 1 == DEPTH ? 0 : put + 1;
+    }
+    __device__ __forceinline__ void take(uint4 (&r)[2][W]) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(r[c][w].x), "=r"(r[c][w].y), "=r"(r[c][w].z), "=r"(r[c][w].w)
+                             : "r"(ring + (get * 2 * W + c * W + w) * 512)
+                             : "memory");
+        get = get + 1 == DEPTH ? 0 : get + 1;
+    }
+};
+
+// Heads of one token that stay numbers, steps [s0, s1).  ws: weights that all heads share;
+// cs: the token's cosines and sines.
+template <int D, bool F32, bool APPEND, bool INTER, bool VEC, bool FULL>
+__device__ __forceinline__ void turn_heads(const Turn &a, Feed<D, F32, INTER, FULL> &feed, const TurnHeads &from, const TurnHeads &to,
+                                           const TurnWeight &wt, const float *ws, const float *cs, int b, int i, int heads, int s0, int s1) {
     using My = Lane<D, F32, INTER, FULL, false>;
     constexpr int HC = My::HC, PC = My::PC, LN = My::LN, RW = 32 / LN, W = My::W;
     static_assert(HC == 8, "16 channels a lane");
     const int lane = threadIdx.x & 31;
     const My my{lane % LN, FULL ? D : a.R};
-    constexpr int DEPTH = F32 ? 1 : 2;  // steps under way
+    // (a rotation's steps come through the ring, whose code costs the write more registers than it has)
+    constexpr bool RING = VEC && !APPEND;
     constexpr int ES = F32 ? 4 : 2;
-    uint4 raw[DEPTH][2][W];
     const int row = lane / LN;
-    const char *src = reinterpret_cast<const char *>(from.p) + (b * from.b + i * from.i) * ES;
+    uint4 r[2][W];
+    if (!RING) load_row<VEC, F32>(my, from, b, i, min(s0 * RW + row, heads - 1), r);
     char *dst = reinterpret_cast<char *>(to.p) + (b * to.b + i * to.i) * ES;
-    // (lanes without a head have the last one's numbers, and write nothing)
-    auto fetch = [&](int s, uint4 (&r)[2][W]) {
-        if (s >= s1) return;
-        const char *p = src + min(s * RW + row, heads - 1) * from.h * ES;
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int w = 0; w < W; ++w) r[c][w] = load_word<VEC, F32>(p, my.chan(c, w));
-    };
-#pragma unroll
-    for (int p = 0; p < DEPTH; ++p) fetch(s0 + p, raw[p]);
     // A pair's turn and weights in one: z_u = x_u ta + x_v tb, z_v = x_v tc + x_u td.  Pair
     // e: y[0][e], y[1][e], or interleaved y[e / 4][2 (e % 4)] and its neighbour.  Numbers
     // that do not turn have ta and tc, their weights.
@@ -457,11 +530,16 @@ __device__ __forceinline__ void turn_heads(const Turn &a, const TurnHeads &from,
         }
     };
     if (!a.norm || wt.h == 0) tables(0);
-    auto step = [&](int s, uint4 (&r)[2][W]) {
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
         const int h = s * RW + row;
         float y[2][HC];
+        if (RING) feed.take(r);
         numbers<F32>(r, y);
-        fetch(s + DEPTH, r);
+        if (RING)
+            feed.ask(a);
+        else if (s + 1 < s1)
+            load_row<VEC, F32>(my, from, b, i, min(h + RW, heads - 1), r);
         float in = 1.0f;
         if (a.norm) {
             in = inv_norm<D, LN>(a, y);
@@ -484,18 +562,12 @@ __device__ __forceinline__ void turn_heads(const Turn &a, const TurnHeads &from,
             }
             u0 = p0, u1 = p1, v0 = q0, v1 = q1;
         }
-        if (h >= heads) return;
+        if (h >= heads) continue;
         char *p = dst + h * to.h * ES;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int w = 0; w < W; ++w) store_word<VEC, F32>(p, my.chan(c, w), y[c] + w * PC);
-    };
-#pragma unroll 1
-    for (int s = s0; s < s1; s += DEPTH) {
-#pragma unroll
-        for (int p = 0; p < DEPTH; ++p)
-            if (p == 0 || s + p < s1) step(s + p, raw[p]);
     }
 }
 
@@ -507,7 +579,8 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     constexpr int G = D / KV4_GROUPS, RB = kv4_row_bytes(D), RW = 512 / D;  // RW: heads of a step that stay numbers
     using My = Lane<D, F32, INTER, FULL, true>;
     constexpr int PC = My::PC;
-    extern __shared__ __align__(16) float tables[];  // [warp]: weights of queries and keys [D], then [token] cosines, sines [D / 2]
+    // weights of queries and keys [D], of each warp [token] cosines, sines [D / 2], and its ring
+    extern __shared__ __align__(16) float tables[];
     __shared__ int sts[TW][TOKENS];
     const int T = 1 << lt, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, R = FULL ? D : a.R;
     float *ws = tables, *cs = tables + 2 * D + warp * (T * D);
@@ -533,32 +606,30 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
         }
     __syncthreads();
 
-    // units: some tokens of a sequence, and a share of their rows
-    const uint32_t per = (uint32_t)(a.n + T - 1) >> lt, whole = (uint32_t)a.B * per, units = whole * slices;
+    Units all;
+    all.per = (uint32_t)(a.n + T - 1) >> lt, all.whole = (uint32_t)a.B * all.per, all.units = all.whole * slices, all.stride = gridDim.x * TW;
+    all.T = T, all.slices = slices, all.first = APPEND && slices > 1 ? 1 : 0;
+    all.ks = APPEND ? 0 : (a.H + RW - 1) / RW, all.steps = all.ks + (a.Hq + RW - 1) / RW;
+    const int ks = all.ks;
+    const uint32_t x0 = blockIdx.x * TW + warp;
+    using Heads = Feed<D, F32, INTER, FULL>;
+    Heads feed;
+    if (VEC && !APPEND) feed.start(a, all, x0, (uint32_t)__cvta_generic_to_shared(tables + 2 * D + TW * T * D) + warp * Heads::RING);
     // positions of the lane's pairs, asked for a unit ahead
     int p_next[2];
     auto ask = [&](uint32_t x) {
-        if (x >= units) return;
-        const uint32_t unit = x % whole, b = unit / per;
+        if (x >= all.units) return;
+        const uint32_t unit = x % all.whole, b = unit / all.per;
 #pragma unroll
         for (int y = 0; y < 2; ++y)
-            if (lane + 32 * y < R / 2) p_next[y] = turn_position(a, (int)b, (int)(unit - b * per) * T, axis[y]);
+            if (lane + 32 * y < R / 2) p_next[y] = turn_position(a, (int)b, (int)(unit - b * all.per) * T, axis[y]);
     };
-    ask(blockIdx.x * TW + warp);
+    ask(x0);
 #pragma unroll 1
-    for (uint32_t x = blockIdx.x * TW + warp; x < units; x += gridDim.x * TW) {
-        // (all first slices, which cost the most, before the others)
-        const uint32_t share = slices > 1 ? x / whole : 0, unit = x - share * whole;
-        const int slice = (int)share, b = (int)(unit / per), i0 = (int)(unit - b * per) * T, tokens = min(T, a.n - i0);
-        // The warp's share: of rows for the cache, eight at a time, keys then values, all in the
-        // first slice, which has the tokens' status; of the others steps of every token.
-        const int ok = (tokens * a.H + 7) >> 3, ks = APPEND ? 0 : (a.H + RW - 1) / RW, steps = ks + (a.Hq + RW - 1) / RW;
-        int s0 = 0, s1 = steps;
-        if (slices > 1) {
-            const int first = APPEND ? 1 : 0;  // slices without steps
-            s0 = slice < first ? 0 : steps * (slice - first) / (slices - first);
-            s1 = slice < first ? 0 : steps * (slice - first + 1) / (slices - first);
-        }
+    for (uint32_t x = x0; x < all.units; x += all.stride) {
+        const Unit u = all.at(a, x);
+        const int b = u.b, i0 = u.i0, tokens = u.tokens, slice = u.slice, s0 = u.s0, s1 = u.s1;
+        const int ok = (tokens * a.H + 7) >> 3;  // eight rows for the cache at a time, keys, then values
         const int octets = APPEND && slice == 0 ? 2 * ok : 0;
 
         // The row of this lane in an octet: token, head.  Lanes without one (false) have the
@@ -591,7 +662,7 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                 sincospif((float)(int)turns * 0x1p-31f, &sn, &cn);
                 cs[tok * D + j] = cn * a.scale32, cs[tok * D + D / 2 + j] = sn * a.scale32;
             }
-        ask(x + gridDim.x * TW);
+        ask(x + all.stride);
         if (APPEND && lane < TOKENS) st[lane] = 0;
         __syncwarp();
 
@@ -600,7 +671,7 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
         for (int y = APPEND ? 1 : 0; y < 2 * tokens; y += APPEND ? 2 : 1) {
             const int q = y & 1, tok = y >> 1, from = q ? max(s0 - ks, 0) : s0, to = q ? s1 - ks : min(s1, ks);
             if (from < to)
-                turn_heads<D, F32, INTER, VEC, FULL>(a, q ? a.q : a.k, q ? a.oq : a.ok, q ? a.qw : a.kw, ws + (q ? 0 : D), cs + tok * D, b, i0 + tok,
+                turn_heads<D, F32, APPEND, INTER, VEC, FULL>(a, feed, q ? a.q : a.k, q ? a.oq : a.ok, q ? a.qw : a.kw, ws + (q ? 0 : D), cs + tok * D, b, i0 + tok,
                                                      q ? a.Hq : a.H, from, to);
         }
         if (!APPEND) continue;
@@ -731,7 +802,7 @@ static cudaError_t run_turn(const Turn &a, int nsm, cudaStream_t s) {
     while (slices < most && units * slices < SLICE_WARPS * nsm) ++slices;
     const long long want = (units * slices + TW - 1) / TW;
     const unsigned grid = (unsigned)(want < (long long)TURN_CTAS * nsm ? want : (long long)TURN_CTAS * nsm);
-    const size_t tables = (size_t)((TW << lt) + 2) * (D * 4);
+    const size_t tables = (size_t)((TW << lt) + 2) * (D * 4) + (a.vec && !APPEND ? TW * Feed<D, F32, INTER, true>::RING : 0);
     const auto fn = !a.vec ? k_turn<D, F32, APPEND, INTER, false, false>
                   : a.R == D ? k_turn<D, F32, APPEND, INTER, true, true>
                              : k_turn<D, F32, APPEND, INTER, true, false>;
