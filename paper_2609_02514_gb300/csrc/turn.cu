@@ -708,13 +708,13 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                             mul2(y[c][e + 2], y[c][e + 3], v.z, v.w);
                         }
                 }
-                // Float32's z is within 14 u = 14 * 2^-24 of the 64-bit one, relative to the length h
-                // of its pair: the sum of squares 9 u (four in a row, three and two levels more), half
-                // of which shows in the root, the mean with eps 0.5 u, the root, r w and its product
-                // with x 1 u each: 8 u; a product of the two and their sum 2 u; cosine and sine 1 u and
-                // 2 pi 2^-26 < 1.6 u of their angle, absolute, for both together 2^0.5 as much of h:
-                // 3.7 u.  With the scale's two roundings below 16 u.
-                // (E: the largest square of a group, or of what turns of pairs among both)
+                // Float32's z is within 17 u = 17 * 2^-24 of the 64-bit one, relative to the length h
+            // of its pair: the sum of squares 9 u (four in a row, three and two levels more), half
+            // of which shows in the root, the mean with eps 0.5 u, the root 1.5 u, r w and its
+            // product with x 1 u each: 8.5 u; a product of the two and their sum 2 u; cosine and
+            // sine 1 u and 2 pi 2^-26 < 1.6 u of their angle, absolute, for both together 2^0.5
+            // as much of h: 3.7 u; the scale's two roundings 2 u.
+            // (E: the largest square of a group, or of what turns of pairs among both)
                 float E[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
@@ -745,7 +745,7 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                 float near[2];
 #pragma unroll
                 for (int c = 0; c < 2; ++c)  // (the least length: of squares below float32)
-                    near[c] = fmaxf(__fsqrt_rn(E[c]), 1e-22f) * (my.turns(c, 0) ? a.scale32 : 1.0f) * 0x1p-20f;
+                    near[c] = fmaxf(__fsqrt_rn(E[c]), 1e-22f) * (my.turns(c, 0) ? a.scale32 : 1.0f) * 0x1.1p-20f;
                 sure = quantise_near<G>(y[0], near[0], w[0], &t[0], &bad);
                 sure &= quantise_near<G>(y[1], near[1], w[1], &t[1], &bad1);
             }

@@ -152,6 +152,21 @@ def test_in_place_and_strided_outputs(A):
         A.rotate_qk(want["q"], want["k"], f, start=start, out=dict(q=torch.empty(1, 9, 6, 64, device="cuda", dtype=torch.bfloat16).expand(2, 9, 6, 64)))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_in_place_of_many_tokens(A, dtype):
+    """Rows are read ahead of those that are written, of several tokens a warp."""
+    rng = np.random.default_rng(13)
+    q, k = _heads(rng, 2, 9000, (5, 3), 64, dtype, "fused")
+    f, start = _freq(64), _i32([1, 70000])
+    want = A.rotate_qk(q, k, f, start=start, eps=1e-6)
+    A.rotate_qk(q, k, f, start=start, eps=1e-6, out=dict(q=q, k=k))
+    assert torch.equal(q, want["q"]) and torch.equal(k, want["k"])
+    for b, i in ((0, 0), (1, 8999), (1, 3), (0, 6000)):
+        one = A.rotate_qk(want["q"][b:b + 1, i:i + 1], want["k"][b:b + 1, i:i + 1], f, start=start[b:b + 1] + i)
+        many = A.rotate_qk(want["q"], want["k"], f, start=start)
+        assert torch.equal(one["q"][0, 0], many["q"][b, i]) and torch.equal(one["k"][0, 0], many["k"][b, i])
+
+
 def test_rows_do_not_hang_on_their_neighbours(A):
     """A token's numbers are the same bits alone and in a batch of any size."""
     rng = np.random.default_rng(4)
