@@ -334,10 +334,9 @@ __device__ __forceinline__ void numbers(const uint4 (&raw)[2][W], float (&y)[2][
         for (int e = 0; e < HC; ++e) y[c][e] = Elem<F32 ? ACES_F32 : ACES_BF16>::get(raw[c][e / (F32 ? 4 : 8)], e % (F32 ? 4 : 8));
 }
 
-// 1 / the norm of a row, whose lanes are LN neighbours.  Numbers whose squares pass
-// float32 become 2^-70 of themselves.
-template <int D, int LN, int HC>
-__device__ __forceinline__ float inv_norm(const Turn &a, float (&y)[2][HC]) {
+// The sum of a row's squares, whose lanes are LN neighbours: eight sums a lane, then a tree.
+template <int LN, int HC>
+__device__ __forceinline__ float squares(const float (&y)[2][HC]) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = y[0][e];
@@ -351,19 +350,23 @@ __device__ __forceinline__ float inv_norm(const Turn &a, float (&y)[2][HC]) {
     float ss = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
     for (int x = 1; x < LN; x <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
+    return ss;
+}
+
+// 1 / the norm of a row, whose lanes are LN neighbours.  Numbers whose squares pass
+// float32 become 2^-70 of themselves, and are summed in the same order.
+template <int D, int LN, int HC>
+__device__ __forceinline__ float inv_norm(const Turn &a, float (&y)[2][HC]) {
+    float ss = squares<LN>(y);
     const bool huge = !(ss < 1e37f);
     float eps = a.eps32;
     if (__any_sync(0xffffffffu, huge)) {
-        float s2 = 0.0f;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int e = 0; e < HC; ++e) {
+            for (int e = 0; e < HC; ++e)
                 if (huge) y[c][e] *= 0x1p-70f;
-                s2 = fmaf(y[c][e], y[c][e], s2);
-            }
-#pragma unroll
-        for (int x = 1; x < LN; x <<= 1) s2 += __shfl_xor_sync(0xffffffffu, s2, x);
+        const float s2 = squares<LN>(y);
         if (huge) ss = s2, eps = 0.0f;
     }
     // (a Newton step behind the approximation: within 1.5 * 2^-24)
