@@ -439,7 +439,8 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *                head (stride D or more), or NULL: ones; only with norm
  *   eps          1e-30 .. 1
  *   scale        2^-20 .. 2^20 (1 as a rule; of scaled position schemes)
- * Numbers are float32 inside (angles 64 bits); each result is rounded once.
+ * Numbers are float32 inside (angles 64 bits), so a product beyond its range is
+ * infinite; each result is rounded once.
  */
 #define ACES_MAX_AXES 4
 typedef struct {
@@ -472,7 +473,8 @@ aces_status aces_rotate_qk(const void *q, const void *k, aces_dtype dt, const in
  * The same for new tokens of a cache in 4 bits, whose keys, so turned, and
  * values are quantised as they are written (aces_kv4_append's arguments and
  * status; the keys are not rounded to dt before: their codes are those of the
- * numbers in 64 bits).  q_out has every token, padding too.
+ * numbers in 64 bits, and ACES_ROW_NONFINITE says that one of those, or a value,
+ * is not finite).  q_out has every token, padding too.
  */
 aces_status aces_kv4_append_rotated(void *cache, int planes, int layer, int B, int H, int S, int D, const void *q,
                                     const void *k, const void *v, aces_dtype dt, const int64_t *q_strides,

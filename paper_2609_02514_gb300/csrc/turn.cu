@@ -21,7 +21,7 @@
 // products were ordered here.  Float32's z is within E of that; where a quotient lies
 // closer than that to a border, or the step could be another, the whole warp does the
 // row again to 46 bits (three rows of a thousand; then one number of 10^12 may be decided
-// otherwise).
+// otherwise), or in float64 where products could pass float32.
 //
 // What bounds it.  Rotation of 8192 tokens of two sequences, 32 and 8 heads of 128 in
 // bfloat16 (336 MB): 59 us, 5.7 TB/s; a copy of as many dense bytes takes 52.  Bytes under way
@@ -160,9 +160,9 @@ struct Lane {
 
 // ---------------------------------------------------------------------------
 // Codes of a group of z whose numbers are within E of the 64-bit ones: false where those
-// could have other codes.
+// could have other codes, or float32 had none.
 template <int G>
-__device__ __forceinline__ bool quantise_near(float (&z)[G], float E, uint32_t (&w)[G / 8], float *t_out, bool *bad) {
+__device__ __forceinline__ bool quantise_near(const float (&z)[G], float E, uint32_t (&w)[G / 8], float *t_out) {
     float mx = z[0], mn = z[0];
 #pragma unroll
     for (int i = 1; i < G; i += 2) {
@@ -170,11 +170,9 @@ __device__ __forceinline__ bool quantise_near(float (&z)[G], float E, uint32_t (
         asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(mx) : "f"(y), "f"(u));
         asm("min.NaN.f32 %0, %0, %1, %2;" : "+f"(mn) : "f"(y), "f"(u));
     }
-    *bad = false;
-    if (!(mx <= FLT_MAX && mn >= -FLT_MAX)) {  // not finite: what it is does not hang on roundings
-        quantise<G, true>(z, w, t_out, bad);
-        return true;
-    }
+    // (products of finite numbers may pass float32, and the numbers beside one that is none
+    // have their codes too)
+    const bool finite = mx <= FLT_MAX && mn >= -FLT_MAX;
     const float big = fmaxf(mx, -mn);
     const float t = kv4_t(mx > -mn ? fminf(mx, KV4_CAP) : fmaxf(mn, -KV4_CAP)), s = t * KV4_STEP;
     const bool none = big + E < KV4_TINY;  // (a group of zeros among them)
@@ -196,20 +194,117 @@ __device__ __forceinline__ bool quantise_near(float (&z)[G], float E, uint32_t (
     }
     *t_out = t;
     // E in steps, and the quotient's own roundings (8.25 * 2^-24, and those of the test)
-    return none || (sure && far < 0.5f - fmaf(E, fabsf(inv), 1.0e-6f));
+    return finite && (none || (sure && far < 0.5f - fmaf(E, fabsf(inv), 1.0e-6f)));
 }
 
 // 1 / (2 pi) in two parts
 constexpr double INV_TURN = 0.15915494309189535, INV_TURN_LO = -9.839338337591493e-18;
 
-// A row again, to some 46 bits, and into the cache, by a whole warp: a lane has D / 32
-// neighbouring channels, four lanes a group.
+// A row again in float64, whatever its numbers and weights are, by a whole warp: a lane has
+// D / 32 neighbouring channels, four lanes a group.  True where a number is none.
 template <int D, bool F32, bool INTER>
-static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h, uint8_t *row) {
+static __device__ __noinline__ bool wide_row(const Turn &a, int b, int i, int h, uint8_t *row) {
     constexpr int G = D / KV4_GROUPS, CH = D / 32;
     constexpr uint32_t ALL = 0xffffffffu;
     const int lane = threadIdx.x & 31, d0 = lane * CH, half = a.R / 2;
     const long long at = b * a.k.b + i * a.k.i + h * a.k.h + d0;
+    double y[CH], ss = 0.0;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        y[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
+                   : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
+        ss = fma(y[e], y[e], ss);
+        if (a.norm) y[e] *= (double)weight_at(a.kw, h * a.kw.h + d0 + e);
+    }
+    if (a.norm) {
+        for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(ALL, ss, x);
+        const double norm = sqrt(ss / D + a.eps);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) y[e] /= norm;
+    }
+    const bool turns = d0 < a.R, second = !INTER && d0 >= half;
+    const int other = INTER || !turns ? lane : second ? lane - half / CH : lane + half / CH;
+    double z[CH];
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        const double yo = INTER ? y[e ^ 1] : __shfl_sync(ALL, y[e], other);
+        z[e] = y[e];
+        if (turns) {
+            const int j = INTER ? (d0 + e) / 2 : second ? d0 - half + e : d0 + e;
+            const double angle = (double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j);
+            const double hi = angle * INV_TURN, lo = fma(angle, INV_TURN, -hi) + angle * INV_TURN_LO;  // turns, in two parts
+            double sn, cn;
+            sincospi(2.0 * (hi - rint(hi) + lo), &sn, &cn);
+            const bool v = INTER ? e & 1 : second;
+            z[e] = a.scale * (v ? y[e] * cn + yo * sn : y[e] * cn - yo * sn);
+        }
+        bad |= !(fabs(z[e]) <= DBL_MAX);
+        z[e] = z[e] == z[e] ? fmin(fmax(z[e], -(double)KV4_CAP), (double)KV4_CAP) : 0.0;
+    }
+    double top = z[0];  // the group's first of the largest
+#pragma unroll
+    for (int e = 1; e < CH; ++e)
+        if (fabs(z[e]) > fabs(top)) top = z[e];
+#pragma unroll
+    for (int x = 1; x < 4; x <<= 1) {
+        const double o = __shfl_xor_sync(ALL, top, x);
+        if (lane & x ? !(fabs(top) > fabs(o)) : fabs(o) > fabs(top)) top = o;
+    }
+    double t = 0.0;  // kv4_t()
+    if (fabs(top) >= (double)KV4_TINY) {
+        const unsigned long long u = (unsigned long long)__double_as_longlong(top * -0x1p-19);
+        t = __longlong_as_double((long long)((u + ((1ull << 47) - 1) + (u >> 48 & 1)) & ~((1ull << 48) - 1)));
+    }
+    const double s = t * (double)KV4_STEP;
+    uint32_t w = 0u;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        const int c = (d0 + e) & 7, r = s == 0.0 ? 0 : (int)fmin(fmax(rint(z[e] / s), -8.0), 7.0);
+        w |= (uint32_t)(r + 8) << (4 * (c >> 1) + 16 * (c & 1));
+    }
+#pragma unroll
+    for (int x = 1; x < 8 / CH; x <<= 1) w |= __shfl_xor_sync(ALL, w, x);
+    if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = w;
+    if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint((float)t) >> 16);
+    return __any_sync(ALL, bad);
+}
+
+// A row again, to some 46 bits, and into the cache, by a whole warp: a lane has D / 32
+// neighbouring channels, four lanes a group.  Rows whose products could leave float32 are
+// wide_row()'s.  True where a number is none.
+template <int D, bool F32, bool INTER>
+static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h, uint8_t *row) {
+    constexpr int G = D / KV4_GROUPS, CH = D / 32;
+    constexpr uint32_t ALL = 0xffffffffu;
+    const int lane = threadIdx.x & 31, d0 = lane * CH, half = a.R / 2;
+    const long long at = b * a.k.b + i * a.k.i + h * a.k.h + d0;
+    // Within these limits no product passes float32, and none loses its lower half.
+    Two y[CH];
+    float xs[CH];
+    bool far = false;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        xs[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
+                    : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
+        y[e] = {xs[e], 0.0f};
+        far |= !(fabsf(xs[e]) <= 0x1p55f);
+        if (a.norm) {
+            const float wt = weight_at(a.kw, h * a.kw.h + d0 + e);
+            y[e] = two_product(xs[e], wt);  // (exact: equal ones stay equal)
+            far |= !(fabsf(wt) <= 0x1p60f) || (fabsf(y[e].h) < 0x1p-100f && xs[e] != 0.0f && wt != 0.0f);
+        }
+    }
+    if (__any_sync(ALL, far)) return wide_row<D, F32, INTER>(a, b, i, h, row);
+    if (a.norm) {
+        Two ss = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < CH; ++e) ss = ss + two_product(xs[e], xs[e]);
+        for (int x = 16; x > 0; x >>= 1) ss = ss + Two{__shfl_xor_sync(ALL, ss.h, x), __shfl_xor_sync(ALL, ss.l, x)};
+        const Two r = two_rsqrt(Two{ss.h / D, ss.l / D} + Two{a.eps32, a.eps_low});
+#pragma unroll
+        for (int e = 0; e < CH; ++e) y[e] = y[e] * r;
+    }
     // A lane works out half of its pairs' cosines and sines: interleaved pairs are its own,
     // the others are shared with the lane that has their other channels.  (The angle is
     // rounded as a product in 64 bits is.)
@@ -227,37 +322,8 @@ static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h
         const float th = (float)t;
         two_sincos({th, (float)(t - th)}, sn[x], cn[x]);
     }
-    float xs[CH], big = 0.0f;
-#pragma unroll
-    for (int e = 0; e < CH; ++e) {
-        xs[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
-                    : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
-        big = fmaxf(big, fabsf(xs[e]));
-    }
-    Two y[CH];
-#pragma unroll
-    for (int e = 0; e < CH; ++e) y[e] = {xs[e], 0.0f};
-    if (a.norm) {
-        // numbers whose squares pass float32: 2^-70 of them (eps is nothing beside those)
-        const float down = __any_sync(ALL, big > 0x1p55f) ? 0x1p-70f : 1.0f;
-        Two ss = {0.0f, 0.0f};
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-            xs[e] *= down;
-            ss = ss + two_product(xs[e], xs[e]);
-        }
-        for (int x = 16; x > 0; x >>= 1) ss = ss + Two{__shfl_xor_sync(ALL, ss.h, x), __shfl_xor_sync(ALL, ss.l, x)};
-        const Two m = Two{ss.h / D, ss.l / D} + (down == 1.0f ? Two{a.eps32, a.eps_low} : Two{0.0f, 0.0f});
-        const Two r = two_rsqrt(m);
-#pragma unroll
-        for (int e = 0; e < CH; ++e) y[e] = two_product(xs[e], weight_at(a.kw, h * a.kw.h + d0 + e)) * r;  // (x w is exact: equal ones stay equal)
-    }
     Two z[CH];
-    auto turned = [&](Two u, Two v, Two c, Two s) {  // u c - v s
-        Two p = u * c + -(v * s);
-        // (what is not finite has no second part)
-        return fabsf(p.h) <= FLT_MAX && fabsf(p.l) <= FLT_MAX ? p : Two{fmaf(u.h, c.h, -(v.h * s.h)), 0.0f};
-    };
+    auto turned = [&](Two u, Two v, Two c, Two s) { return u * c + -(v * s); };
     if (INTER) {
 #pragma unroll
         for (int x = 0; x < CH / 2; ++x) {
@@ -282,8 +348,7 @@ static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h
     };
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
-        z[e] = !turns ? y[e] : a.scale == 1.0 ? z[e] : turned(z[e], {0.0f, 0.0f}, {a.scale32, a.scale_low}, {0.0f, 0.0f});
-        if (!(z[e].h == z[e].h)) z[e] = {0.0f, 0.0f};
+        z[e] = !turns ? y[e] : a.scale == 1.0 ? z[e] : z[e] * Two{a.scale32, a.scale_low};
         if (larger(z[e], {KV4_CAP, 0.0f})) z[e] = {copysignf(KV4_CAP, z[e].h), 0.0f};
         if (larger(z[e], top)) top = z[e];  // the first of the largest
     }
@@ -315,6 +380,7 @@ static __device__ __noinline__ void exact_row(const Turn &a, int b, int i, int h
     for (int x = 1; x < 8 / CH; x <<= 1) w |= __shfl_xor_sync(ALL, w, x);
     if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = w;
     if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint(t) >> 16);
+    return false;
 }
 
 // ---------------------------------------------------------------------------
@@ -749,8 +815,8 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
 #pragma unroll
                 for (int c = 0; c < 2; ++c)  // (the least length: of squares below float32)
                     near[c] = fmaxf(__fsqrt_rn(E[c]), 1e-22f) * (my.turns(c, 0) ? a.scale32 : 1.0f) * 0x1.1p-20f;
-                sure = quantise_near<G>(y[0], near[0], w[0], &t[0], &bad);
-                sure &= quantise_near<G>(y[1], near[1], w[1], &t[1], &bad1);
+                sure = quantise_near<G>(y[0], near[0], w[0], &t[0]);
+                sure &= quantise_near<G>(y[1], near[1], w[1], &t[1]);
             }
             if (mine && !in) atomicOr(&st[tok], ACES_ROW_RANGE);
             if (in && (bad || bad1)) atomicOr(&st[tok], ACES_ROW_NONFINITE);
@@ -777,7 +843,7 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                 const int from = __ffs(again) - 1;
                 uint8_t *to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, (unsigned long long)row, from));
                 const int ri = __shfl_sync(0xffffffffu, i, from), rh = __shfl_sync(0xffffffffu, h, from);
-                if (to) exact_row<D, F32, INTER>(a, b, ri, rh, to);
+                if (to && exact_row<D, F32, INTER>(a, b, ri, rh, to) && lane == 0) atomicOr(&st[ri - i0], ACES_ROW_NONFINITE);
             }
         }
         if (slice == 0) {
