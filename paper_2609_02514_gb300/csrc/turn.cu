@@ -20,8 +20,8 @@
 // The cache's codes are those of z in 64 bits, so that they do not depend on how sums and
 // products were ordered here.  Float32's z is within E of that; where a quotient lies
 // closer than that to a border, or the step could be another, the whole warp does the
-// row again to 46 bits (three rows of a thousand; then one number of 10^12 may be decided
-// otherwise), or in float64 where products could pass float32.
+// row again to 46 bits (three rows of a thousand), or in float64 where those do not decide
+// or products could pass float32.
 //
 // What bounds it.  Rotation of 8192 tokens of two sequences, 32 and 8 heads of 128 in
 // bfloat16 (336 MB): 59 us, 5.7 TB/s; a copy of as many dense bytes takes 52.  Bytes under way
@@ -271,8 +271,8 @@ static __device__ __noinline__ bool wide_row(const Turn &a, int b, int i, int h,
 }
 
 // A row again, to some 46 bits, and into the cache, by a whole warp: a lane has D / 32
-// neighbouring channels, four lanes a group.  Rows whose products could leave float32 are
-// wide_row()'s.  True where a number is none.
+// neighbouring channels, four lanes a group.  Rows whose products could leave float32, and
+// those with a number within 2^-40 of a border, are left to wide_row(): false.
 template <int D, bool F32, bool INTER>
 static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h, uint8_t *row) {
     constexpr int G = D / KV4_GROUPS, CH = D / 32;
@@ -295,7 +295,7 @@ static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h
             far |= !(fabsf(wt) <= 0x1p60f) || (fabsf(y[e].h) < 0x1p-100f && xs[e] != 0.0f && wt != 0.0f);
         }
     }
-    if (__any_sync(ALL, far)) return wide_row<D, F32, INTER>(a, b, i, h, row);
+    if (__any_sync(ALL, far)) return false;
     if (a.norm) {
         Two ss = {0.0f, 0.0f};
 #pragma unroll
@@ -360,6 +360,11 @@ static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h
     // The step: kv4_t() of the first part, but that where this lies on a half the second
     // one decides.
     float t = larger({KV4_TINY, 0.0f}, top) ? 0.0f : kv4_t(top.h);
+    // Numbers that are not exact here, and this close to a border, may be rounded onto it or
+    // across it in float64 (5 times a scale of 1.2 is 6 there): wide_row() has them.
+    const bool exact = !turns || a.scale == 1.0;
+    auto close = [&](float off, Two x) { return fabsf(off) < 0x1p-40f * fabsf(x.h) && (a.norm || !exact || x.l != 0.0f); };
+    bool unclear = t != 0.0f && (__float_as_uint(top.h) & 0x7FFFFu) == 0x40000u && close(top.l, top);
     if (t != 0.0f && top.l != 0.0f && (__float_as_uint(top.h) & 0x7FFFFu) == 0x40000u) {
         const bool up = (top.l > 0.0f) == (top.h > 0.0f);
         const uint32_t u = __float_as_uint(top.h * -1.9073486328125e-06f) & ~0x7FFFFu;  // -2^-19
@@ -373,14 +378,16 @@ static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h
         float r = rintf(z[e].h * inv);
         const float d = fmaf(-r, s, z[e].h);  // exact, on the grid of the halves
         const bool along = (z[e].l > 0.0f) == (d > 0.0f);
+        unclear |= hs != 0.0f && close(fabsf(d) - hs + (along ? fabsf(z[e].l) : -fabsf(z[e].l)), z[e]);
         if (fabsf(d) > hs || (fabsf(d) == hs && hs != 0.0f && (z[e].l == 0.0f ? ((int)r & 1) : along))) r += (d > 0.0f) == (s > 0.0f) ? 1.0f : -1.0f;
         w |= (uint32_t)((int)fminf(fmaxf(r, -8.0f), 7.0f) + 8) << (4 * (c >> 1) + 16 * (c & 1));
     }
+    if (__any_sync(ALL, unclear)) return false;
 #pragma unroll
     for (int x = 1; x < 8 / CH; x <<= 1) w |= __shfl_xor_sync(ALL, w, x);
     if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = w;
     if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = (unsigned short)(__float_as_uint(t) >> 16);
-    return false;
+    return true;
 }
 
 // ---------------------------------------------------------------------------
@@ -843,7 +850,8 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                 const int from = __ffs(again) - 1;
                 uint8_t *to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, (unsigned long long)row, from));
                 const int ri = __shfl_sync(0xffffffffu, i, from), rh = __shfl_sync(0xffffffffu, h, from);
-                if (to && exact_row<D, F32, INTER>(a, b, ri, rh, to) && lane == 0) atomicOr(&st[ri - i0], ACES_ROW_NONFINITE);
+                if (to && !exact_row<D, F32, INTER>(a, b, ri, rh, to) && wide_row<D, F32, INTER>(a, b, ri, rh, to) && lane == 0)
+                    atomicOr(&st[ri - i0], ACES_ROW_NONFINITE);
             }
         }
         if (slice == 0) {

@@ -131,3 +131,15 @@ def test_rows_of_all_sizes(A, dtype, D, inter):  # noqa: F811
     f, pos = _freq(D), rng.integers(0, 5000, n)
     for turn in (dict(), dict(scale=0.83), dict(eps=1e-30), dict(eps=1e-6), dict(eps=1.0, scale=1.2)):
         assert np.isfinite(_check(A, k, f, pos, dtype, inter, **turn)).all()
+
+
+@ROWS
+def test_scaled_numbers_on_borders(A, dtype, D, inter):  # noqa: F811
+    """At position 0 a scale of a short decimal fraction makes products that 64 bits round onto a border between
+    codes, or between steps, from a place that is not quite there."""
+    rng = np.random.default_rng(D + inter)
+    n, H = 300, 4
+    k = rng.integers(-120, 121, (n, H, D)) * np.exp2(rng.integers(-8, 9, (n, H, 1)))
+    for scale in (1.2, 1.3, 0.7, 1.1, 0.9, 5.2):
+        _check(A, k, _freq(D), np.zeros(n, int), dtype, inter, scale=scale)
+        _check(A, k, _freq(D // 2), np.zeros(n, int), dtype, inter, scale=scale)
