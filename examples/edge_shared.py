@@ -3,8 +3,9 @@
 The system prompt's rows are written once, into a cache of one sequence.  Each request's own
 prompt, its draft tree and its next token go into the request's own cache; queries and keys
 are normed and turned by their positions on the way, which start behind the system prompt,
-and attend to both caches, whose shared part is read once for all requests.  A toy model of a
-few layers (random projections) stands where the draft model would.
+and attend to both caches; a shared part that is long enough for its number of requests is read
+once for all of them (the default sizes are not: each request reads it).  A toy model of a few
+layers (random projections) stands where the draft model would.
 
     python examples/edge_shared.py
 """

@@ -26,7 +26,7 @@ import threading
 
 import torch
 
-__all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
+__all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "checked_shared_passes", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
            "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
            "rotate_qk", "kv4_append_rotated", "kv4_shared_attention", "kv4_shared_workspace_bytes",
            "ROW_NONFINITE", "ROW_BAD_Q", "ROW_TIMEOUT", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
@@ -105,6 +105,15 @@ def checked_cache_selects():
     return int(n.value)
 
 
+def checked_shared_passes(force: int = 0):
+    """The passes that the checked build's last kv4_shared_attention took, 1 or 2; from now on it
+    takes `force`, or with 0 as many as its rule says."""
+    lib = load()
+    if not hasattr(lib, "aces_checked_shared_passes"):
+        raise RuntimeError("the product library does not say: call use_checked() first")
+    return int(lib.aces_checked_shared_passes(int(force)))
+
+
 def _open(path):
     if path in _libs:
         return _libs[path]
@@ -157,6 +166,8 @@ def _open(path):
         lib.aces_checked_violation.restype = I
         lib.aces_checked_cache_selects.argtypes = [P]
         lib.aces_checked_cache_selects.restype = I
+        lib.aces_checked_shared_passes.argtypes = [I]
+        lib.aces_checked_shared_passes.restype = I
     _libs[path] = lib
     return lib
 

@@ -163,6 +163,10 @@ bool two_passes(const Kv4Att &a, int groups, int nsm) {
     return work(a.B, rows) - work(groups, rows * a.per) > (many ? MANY_EXTRA : a.f32 ? F32_EXTRA : FEW_EXTRA);
 }
 
+#ifdef ACES_CHECKED
+int forced_passes = 0, last_passes = 0;  // of kv4_shared_attention; not for calls from several threads
+#endif
+
 }  // namespace
 
 extern "C" {
@@ -290,7 +294,12 @@ aces_status aces_kv4_shared_attention(const void *q, aces_dtype dt, const int64_
     a.k = pk, a.v = pv, a.S = S;
     const int nsm = sm_count();
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (!two_passes(a, groups, nsm)) {
+    bool two = two_passes(a, groups, nsm);
+#ifdef ACES_CHECKED
+    if (forced_passes) two = forced_passes == 2;
+    last_passes = two ? 2 : 1;
+#endif
+    if (!two) {
         a.k0 = sk, a.v0 = sv;
         const auto split = many_rows(a.f32, B, H, n, a.G) ? launch_kv4_many<KV4_SPLIT> : launch_kv4_few<KV4_SPLIT>;
         return split(a, own_ws, nsm, s) == cudaSuccess ? ACES_OK : ACES_ERR_CUDA;
@@ -342,5 +351,15 @@ aces_status aces_kv4_append_rotated(void *cache, int planes, int layer, int B, i
                ? ACES_OK
                : ACES_ERR_CUDA;
 }
+
+#ifdef ACES_CHECKED
+// How many passes the last aces_kv4_shared_attention took; the next ones take `force` (0: by
+// their rule).  For the package's tests: not part of the header.
+int aces_checked_shared_passes(int force);
+int aces_checked_shared_passes(int force) {
+    forced_passes = force;
+    return last_passes;
+}
+#endif
 
 }  // extern "C"
