@@ -26,7 +26,7 @@ import threading
 
 import torch
 
-__all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "checked_shared_passes", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
+__all__ = ["load", "use_checked", "checked_violation", "checked_cache_selects", "checked_shared_passes", "checked_late", "lib_path", "workspace_bytes", "verify", "sparsify", "cache_build", "cache_lookup",
            "kv4_cache", "kv4_append", "kv4_read", "kv4_attention", "kv4_workspace_bytes",
            "rotate_qk", "kv4_append_rotated", "kv4_shared_attention", "kv4_shared_workspace_bytes",
            "ROW_NONFINITE", "ROW_BAD_Q", "ROW_TIMEOUT", "ROW_RANGE", "COUNTERS_OFFSET", "AcespecError"]
@@ -114,6 +114,15 @@ def checked_shared_passes(force: int = 0):
     return int(lib.aces_checked_shared_passes(int(force)))
 
 
+def checked_late(head: int = -1):
+    """From now on the checked build's CTAs of a key head in kv4_shared_attention's second pass of few
+    rows say that a wait gave up, and those of head 0 come a millisecond later; -1: none do."""
+    lib = load()
+    if not hasattr(lib, "aces_checked_late"):
+        raise RuntimeError("the product library's waits cannot be told to give up: call use_checked() first")
+    _check("aces_checked_late", lib.aces_checked_late(int(head)))
+
+
 def _open(path):
     if path in _libs:
         return _libs[path]
@@ -168,6 +177,8 @@ def _open(path):
         lib.aces_checked_cache_selects.restype = I
         lib.aces_checked_shared_passes.argtypes = [I]
         lib.aces_checked_shared_passes.restype = I
+        lib.aces_checked_late.argtypes = [I]
+        lib.aces_checked_late.restype = I
     _libs[path] = lib
     return lib
 

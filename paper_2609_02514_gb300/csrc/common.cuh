@@ -54,6 +54,7 @@ cudaError_t check_take_turn(unsigned long long out[3]);
 cudaError_t check_take_kv4_few_first(unsigned long long out[3]);
 cudaError_t check_take_kv4_few_behind(unsigned long long out[3]);
 cudaError_t check_take_kv4_few_split(unsigned long long out[3]);
+cudaError_t check_set_late(int late);
 #else
 #define ACES_IN(i, n) true
 #endif

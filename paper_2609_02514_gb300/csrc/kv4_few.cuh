@@ -53,6 +53,19 @@ __device__ __forceinline__ float4 cluster_ld4(uint32_t addr) {
     return v;
 }
 
+#ifdef ACES_CHECKED
+// 1 + the key head whose CTAs say that a wait gave up, which those of head 0 are a millisecond
+// behind (tests of the second pass's status; 0: none)
+static __device__ int g_late;
+#define ACES_LATE(h) (g_late == (h) + 1)
+#define ACES_BEHIND_LATE(h) \
+    if (g_late && (h) == 0) \
+        for (int z = 0; z < 1000; ++z) __nanosleep(1000);
+#else
+#define ACES_LATE(h) false
+#define ACES_BEHIND_LATE(h)
+#endif
+
 // A wait that gave up: the ring's other copies (a place without one costs as long a wait)
 template <int ST>
 static __device__ __noinline__ void mbar_drain(uint32_t bar0, int seq) {
@@ -468,8 +481,11 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
         for (int y = 0; y < min(ST, mine); ++y) issue(cur, y, seq + y);
         if (more) q_info(cur, info ^ 1);
         if (MODE == KV4_BEHIND) {
+            ACES_BEHIND_LATE(h)
             pdl_wait();  // for the first pass's sums
-            if (direct && first && tid == 0 && rank == 0 && h == 0 && rt == 0) a.status[b] = kv4_status<MODE>(a, b);
+            // (with the status that kv4_whole() wrote and what other CTAs of the sequence found)
+            if (direct && first && tid == 0 && rank == 0 && h == 0 && rt == 0 && a.part_status[b / a.per])
+                atomicOr(a.status + b, a.part_status[b / a.per]);
         }
         // merge the warps
 #pragma unroll
@@ -481,7 +497,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
                 l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], 16);
                 if (g == 0) sm_m[warp][nt * 8 + 2 * t + c] = m[nt][c], sm_l[warp][nt * 8 + 2 * t + c] = l[nt][c];
             }
-        if (bad && lane == 0) any_timeout = 1;
+        if ((bad || (MODE == KV4_BEHIND && ACES_LATE(h))) && lane == 0) any_timeout = 1;
         __syncthreads();
         // (a cluster's parts stay in the rings, whose tiles are all used)
         float *slot = CL > 1 ? reinterpret_cast<float *>(smem) : ws.piece + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * R * (D + 2);

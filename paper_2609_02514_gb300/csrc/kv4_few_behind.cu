@@ -9,6 +9,7 @@ template cudaError_t launch_kv4_few<KV4_BEHIND>(const Kv4Att &, void *, int, cud
 
 #ifdef ACES_CHECKED
 cudaError_t check_take_kv4_few_behind(unsigned long long out[3]) { return check_take(out); }
+cudaError_t check_set_late(int late) { return cudaMemcpyToSymbol(g_late, &late, sizeof(late)); }
 #endif
 
 }  // namespace aces

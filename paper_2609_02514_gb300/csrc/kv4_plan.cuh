@@ -280,9 +280,9 @@ __device__ __forceinline__ Kv4Start kv4_whole(const Kv4Att &a, int R, int RT, in
     s.key = kv4_keys<KT, TPU, MODE>(a, R, s.b, s.rt);
     s.left = s.quantum = Cost::all(s.key);
     s.cnt = s.key.cnt;
-    // (KV4_BEHIND: the first pass's status is not there yet)
-    if (MODE != KV4_BEHIND && threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
-        a.status[s.b] = kv4_status<MODE>(a, s.b);
+    // (KV4_BEHIND: the first pass's status is not there yet, and is added when it is)
+    if (threadIdx.x == 0 && s.h == 0 && s.rt == 0 && x * CL == blockIdx.x)
+        a.status[s.b] = kv4_seq_of<MODE>(a, s.b).ok ? 0 : ACES_ROW_RANGE;
     return s;
 }
 // the most units an item can have, by the cache's and the window's lengths
