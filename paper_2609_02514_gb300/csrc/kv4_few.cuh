@@ -828,9 +828,16 @@ static cudaError_t run_few(Kv4Att a, void *workspace, int nsm, cudaStream_t s) {
     const long long items = (long long)a.B * RT * a.H;
     const int most = kv4_most_units<MODE>(a, FW * FKT), CL = few_cluster(items, most, F32, nsm);
     const bool direct = CL > 0;
-    // In more than one wave the long sequences go first: a late one would be waited for alone
-    // (64 sequences of 100 to 2000 positions behind an empty prefix: 59 -> 55 us).
-    a.longest_first = CL == 1 && items > nsm * C::MINB && a.B > 1 && a.B <= KV4_RANKED;
+    // In more than one wave the long sequences go first: a late one would be waited for alone.
+    // Every CTA compares all pairs of lengths for it, so not with many sequences, with short
+    // ones, or in float32, whose CTAs wait for products.  One token behind 16384 shared
+    // positions, 32 heads over 8 of 128, without the order / with it (us; up to 740, 1000 and 2000
+    // own positions): 64 sequences 69.5 / 67.5, 72.5 / 70.9, 86.5 / 81.9; 80 89.7 / 92.2,
+    // 97.1 / 96.1, 111.8 / 109.4; 96 97.5 / 98.1, 103.1 / 102.4, 119.2 / 114.3; 128 115.2 /
+    // 119.7, 123.7 / 127.0, 143.7 / 140.1; 512 of up to 2000 448 / 636.  Up to 250: 64
+    // 63.6 / 65.0, 96 88.4 / 91.7.  Float32, 12 heads over 4 of 64, up to 1000: 64 73.8 / 73.2,
+    // 80 88.7 / 90.4, 96 101.1 / 101.7.
+    a.longest_first = !F32 && CL == 1 && most >= 4 && items > nsm * C::MINB && a.B > 1 && a.B <= KV4_RANKED;
     const int grid = direct ? (int)items * CL : nsm * C::MINB;
     const Kv4Ws ws = kv4_ws_carve(workspace, nsm * C::MINB);
     static std::atomic<unsigned long long> allowed{0};

@@ -255,7 +255,7 @@ __device__ __forceinline__ Kv4Start kv4_start(const Kv4Att &a, int R, int RT) {
 
 // The sequence with `rank` longer ones before it (equal ones in their order), by all
 // NTH threads; len: shared memory for KV4_RANKED + 1 numbers.
-constexpr int KV4_RANKED = 512;
+constexpr int KV4_RANKED = 96;
 template <int NTH>
 __device__ __forceinline__ int kv4_ranked(const Kv4Att &a, int rank, int *len) {
     for (int b = threadIdx.x; b < a.B; b += NTH) len[b] = a.prefix[b] + (a.count ? a.count[b] : a.n);

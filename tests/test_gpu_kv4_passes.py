@@ -130,3 +130,23 @@ def test_the_rule_takes_two(A, B, groups, n, Hq, H, D, dtype, room, window, sink
         g = b // (B // groups)
         T._check({key: r[key][b:b + 1] for key in ("out", "lse")}, _f64(q)[b:b + 1], (K0[g:g + 1], V0[g:g + 1]), lens[g:g + 1],
                  (K[b:b + 1], V[b:b + 1]), P[b:b + 1], cnt[b:b + 1], dtype, D ** -0.5, mask, depth, window, sinks)
+
+
+@pytest.mark.parametrize("B", [64, 95, 96, 97, 160])
+def test_the_order_of_sequences(A, B):
+    """In more than one wave, longest first up to 96: of all lengths, equal ones, and some outside the cache."""
+    Hq, H, D, S = 8, 8, 64, 1040
+    rng = np.random.default_rng(B)
+    shared, K0, V0 = _filled(A, rng, 1, H, 50, D)
+    cache, K, V = _filled(A, rng, B, H, S, D)
+    P = rng.integers(0, S, B)
+    P[::7], P[5], P[B // 2] = 900, S, -1
+    q = _torch(rng.standard_normal((B, 1, Hq, D)), "bf16")
+    A.checked_shared_passes(2)
+    r = A.kv4_shared_attention(q, shared, _i32([50]), cache, 0, _i32(P))
+    assert A.checked_shared_passes(0) == 2 and A.checked_violation() is None
+    inside = (P >= 0) & (P < S)
+    np.testing.assert_array_equal(r["status"].cpu().numpy(), np.where(inside, 0, A.ROW_RANGE))
+    assert not r["out"][torch.from_numpy(~inside).cuda()].any()
+    for b in np.flatnonzero(inside):
+        T._check({key: r[key][b:b + 1] for key in ("out", "lse")}, _f64(q)[b:b + 1], (K0, V0), [50], (K[b:b + 1], V[b:b + 1]), [int(P[b])], [1], "bf16", D ** -0.5)
