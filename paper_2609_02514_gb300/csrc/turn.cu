@@ -32,6 +32,8 @@
 // warp that meets one is late by some 9 us, and has two or three tokens in all.  In
 // float64 those rows made it 48, one after another by their four lanes 94.
 #define ACES_FILE 10  // site numbers of the checked build
+#include <climits>
+
 #include "kv4_quant.cuh"
 #include "turn.cuh"
 #include "twofold.cuh"
@@ -875,8 +877,8 @@ static cudaError_t run_turn(const Turn &a, int nsm, cudaStream_t s) {
     const long long units = (long long)a.B * ((a.n + (1 << lt) - 1) >> lt);
     constexpr int RW = 512 / D;
     const int most = APPEND ? 1 + (a.Hq + RW - 1) / RW : (a.H + RW - 1) / RW + (a.Hq + RW - 1) / RW;
-    int slices = 1;
-    while (slices < most && units * slices < SLICE_WARPS * nsm) ++slices;
+    int slices = 1;  // (steps times slices is a 32-bit number in the kernel)
+    while (slices < most && units * slices < SLICE_WARPS * nsm && (long long)most * (slices + 1) <= INT_MAX) ++slices;
     const long long want = (units * slices + TW - 1) / TW;
     const unsigned grid = (unsigned)(want < (long long)TURN_CTAS * nsm ? want : (long long)TURN_CTAS * nsm);
     const size_t tables = (size_t)((TW << lt) + 2) * (D * 4) + (a.vec && !APPEND ? TW * Feed<D, F32, INTER, true>::RING : 0);
