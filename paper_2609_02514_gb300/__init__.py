@@ -609,7 +609,8 @@ def rotate_qk(q, k, inv_freq, start=None, depth=None, positions=None, axes=None,
     start[b] + i, or with tree_mask()'s depth at start[b] + depth[i]; or at positions [B, n], or
     [A, B, n] with up to four axes, of which pair j turns by axes[j] ([R / 2] int32).  scale multiplies
     the turned channels.  q and k may be strided views with a dense last dimension, and `out` may
-    hold q and k themselves (in place); anything else in it overlaps neither.
+    hold q and k themselves (in place); anything else in it overlaps neither.  No gradient goes through
+    it, nor through the other calls here: results of inputs that require one do not.
     """
     if not isinstance(q, torch.Tensor) or not q.is_cuda:
         raise ValueError("q must be a CUDA tensor")

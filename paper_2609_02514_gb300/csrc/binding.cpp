@@ -87,6 +87,15 @@ int integer(PyObject *o, const char *name) {
 }
 void *address(PyObject *o) { return reinterpret_cast<void *>((uintptr_t)whole(o)); }
 
+// A caller's tensor that the call has written: as an object once more.  Its version goes
+// up, so that autograd does not take what it saved of it before for its numbers.
+PyObject *written(PyObject *o) {
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    Py_INCREF(o);
+    return o;
+}
+
 // One output: the caller's object, or a tensor made here, which only becomes an object
 // on the way back to Python, so that what fails in between gives it back.
 struct Output {
@@ -102,9 +111,7 @@ struct Output {
         p = made.data_ptr();
     }
     PyObject *object() const {
-        if (!given) return THPVariable_Wrap(made);
-        Py_INCREF(given);
-        return given;
+        return given ? written(given) : THPVariable_Wrap(made);
     }
 };
 
@@ -292,9 +299,7 @@ struct Heads {
         for (int i = 0; i < 3; ++i) stride[i] = made.stride(i);
     }
     PyObject *object() const {
-        if (!given) return THPVariable_Wrap(made);
-        Py_INCREF(given);
-        return given;
+        return given ? written(given) : THPVariable_Wrap(made);
     }
 };
 const Tensor &queries(PyObject *o) {
