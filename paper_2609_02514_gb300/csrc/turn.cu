@@ -367,6 +367,13 @@ static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h
     const bool exact = !turns || a.scale == 1.0;
     auto close = [&](float off, Two x) { return fabsf(off) < 0x1p-40f * fabsf(x.h) && (a.norm || !exact || x.l != 0.0f); };
     bool unclear = t != 0.0f && (__float_as_uint(top.h) & 0x7FFFFu) == 0x40000u && close(top.l, top);
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+        // of the other sign, and as large or nearly: the step's sign is float64's (equal numbers are
+        // equal there too, but where a norm or a scale has rounded a turn's share away)
+        const float off = (z[e].h + top.h) + (z[e].l + top.l);
+        unclear |= t != 0.0f && fabsf(off) < 0x1p-40f * fabsf(top.h) && (off != 0.0f || (turns && (a.norm || a.scale != 1.0)));
+    }
     if (t != 0.0f && top.l != 0.0f && (__float_as_uint(top.h) & 0x7FFFFu) == 0x40000u) {
         const bool up = (top.l > 0.0f) == (top.h > 0.0f);
         const uint32_t u = __float_as_uint(top.h * -1.9073486328125e-06f) & ~0x7FFFFu;  // -2^-19

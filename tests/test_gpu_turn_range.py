@@ -143,3 +143,15 @@ def test_scaled_numbers_on_borders(A, dtype, D, inter):  # noqa: F811
     for scale in (1.2, 1.3, 0.7, 1.1, 0.9, 5.2):
         _check(A, k, _freq(D), np.zeros(n, int), dtype, inter, scale=scale)
         _check(A, k, _freq(D // 2), np.zeros(n, int), dtype, inter, scale=scale)
+
+
+@ROWS
+def test_equal_numbers_under_slow_turns(A, dtype, D, inter):  # noqa: F811
+    """Numbers of both signs that are equal but for what a turn of 2^-70 to 2^-30 adds: which of them is the
+    largest, and so the step's sign, hangs on what 64 bits keep of it."""
+    rng = np.random.default_rng(D + inter)
+    n, H = 500, 4
+    k = rng.choice([-1.0, 1.0], (n, H, D)) * rng.integers(5, 8, (n, H, D)) / 4
+    f = torch.from_numpy((2.0 ** rng.uniform(-70, -30, D // 2)).astype(np.float32)).cuda()
+    for turn in (dict(), dict(eps=1e-6), dict(scale=1.25), dict(scale=1.3)):
+        _check(A, k, f, rng.integers(0, 50, n), dtype, inter, **turn)
