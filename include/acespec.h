@@ -423,7 +423,7 @@ aces_status aces_kv4_read(const void *cache, int planes, int layer, int B, int H
  *   t = p * inv_freq[j] in 64 bits, p the token's position on the pair's axis
  * for the pairs j < rot_dim / 2 of channels (u, v): (j, j + rot_dim / 2), or
  * with interleaved (2 j, 2 j + 1).  Channels from rot_dim on stay y.
- *   inv_freq     [rot_dim / 2] float32, finite
+ *   inv_freq     [rot_dim / 2] float32; angles beyond 2^40 are not defined
  *   rot_dim      a multiple of D / 4, at most D
  *   axes         [rot_dim / 2] int32 or NULL: the pairs' axes (beyond 0 ..
  *                n_axes - 1 the nearest; needed with more than one)

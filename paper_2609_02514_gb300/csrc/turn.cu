@@ -15,7 +15,8 @@
 //   - of rows that go to the cache two whole groups, four lanes a row, to be quantised.
 //
 // The angle p f is taken as turns, a 64-bit fraction f / (2 pi) times p (a position of 2^20
-// has no fraction left in float32): whole turns fall off by themselves.
+// has no fraction left in float32): whole turns fall off by themselves.  Beyond 2^26 the
+// rounding of p f as a product in 64 bits comes to show, and is added.
 //
 // The cache's codes are those of z in 64 bits, so that they do not depend on how sums and
 // products were ordered here.  Float32's z is within E of that; where a quotient lies
@@ -199,6 +200,10 @@ __device__ __forceinline__ bool quantise_near(const float (&z)[G], float E, uint
     return finite && (none || (sure && far < 0.5f - fmaf(E, fabsf(inv), 1.0e-6f)));
 }
 
+// The angle p f of pair j as 64 bits round it
+__device__ __forceinline__ double turn_angle(const Turn &a, int p, int j) { return (double)p * (double)__ldg(a.freq + j); }
+constexpr float TURN_FAR = 67108864.0f;  // 2^26: beyond it that rounding shows
+
 // 1 / (2 pi) in two parts
 constexpr double INV_TURN = 0.15915494309189535, INV_TURN_LO = -9.839338337591493e-18;
 
@@ -234,7 +239,7 @@ static __device__ __noinline__ bool wide_row(const Turn &a, int b, int i, int h,
         z[e] = y[e];
         if (turns) {
             const int j = INTER ? (d0 + e) / 2 : second ? d0 - half + e : d0 + e;
-            const double angle = (double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j);
+            const double angle = turn_angle(a, turn_position(a, b, i, turn_axis(a, j)), j);
             const double hi = angle * INV_TURN, lo = fma(angle, INV_TURN, -hi) + angle * INV_TURN_LO;  // turns, in two parts
             double sn, cn;
             sincospi(2.0 * (hi - rint(hi) + lo), &sn, &cn);
@@ -318,7 +323,7 @@ static __device__ __noinline__ bool exact_row(const Turn &a, int b, int i, int h
         sn[x] = {0.0f, 0.0f}, cn[x] = {1.0f, 0.0f};
         if (!turns) continue;
         const int j = INTER ? d0 / 2 + x : second ? d0 - half + CH / 2 + x : d0 + x;
-        const double angle = (double)turn_position(a, b, i, turn_axis(a, j)) * (double)__ldg(a.freq + j);
+        const double angle = turn_angle(a, turn_position(a, b, i, turn_axis(a, j)), j);
         const double hi = angle * INV_TURN, lo = fma(angle, INV_TURN, -hi) + angle * INV_TURN_LO;  // turns, in two parts
         const double t = hi - rint(hi) + lo;
         const float th = (float)t;
@@ -665,8 +670,9 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     using My = Lane<D, F32, INTER, FULL, true>;
     constexpr int PC = My::PC;
     // weights of queries and keys [D], of each warp [token] cosines, sines [D / 2], and its ring
-    extern __shared__ __align__(16) float tables[];
+    extern __shared__ __align__(128) float tables[];
     __shared__ int sts[TW][TOKENS];
+    __shared__ uint32_t nears[TW];
     const int T = 1 << lt, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, R = FULL ? D : a.R;
     float *ws = tables, *cs = tables + 2 * D + warp * (T * D);
     int *st = sts[warp];
@@ -675,15 +681,20 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
     // The lane's pairs, lane and lane + 32: 2^64 f / (2 pi), whose whole turns do not count
     uint32_t fh[2] = {0u, 0u}, fl[2] = {0u, 0u};
     int axis[2] = {0, 0};
+    float fastest = 0.0f;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int j = lane + 32 * x;
         if (j >= R / 2) continue;
+        fastest = fmaxf(fastest, fabsf(__ldg(a.freq + j)));
         const double f = __ldg(a.freq + j), hi = f * INV_TURN, lo = fma(f, INV_TURN, -hi) + f * INV_TURN_LO;
         const unsigned long long u = __double2ull_rz((hi - floor(hi)) * 0x1p64) + (unsigned long long)__double2ll_rn(lo * 0x1p64);
         fh[x] = (uint32_t)(u >> 32), fl[x] = (uint32_t)u;
         axis[x] = turn_axis(a, j);
     }
+    // positions beyond which the angle's rounding to 64 bits shows, of the warp's fastest pair
+    fastest = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fastest)));
+    if (lane == 0) nears[warp] = fastest > TURN_FAR * 0x1p-31f ? (uint32_t)(TURN_FAR / fastest) : 0x80000000u;
     if (a.norm)  // weights that all heads share
         for (int y = 4 * threadIdx.x; y < 2 * D; y += 4 * TN) {
             const TurnWeight &w = y < D ? a.qw : a.kw;
@@ -734,6 +745,13 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
         };
         if (APPEND) fetch(0);
 
+        auto put_turn = [&](int tok, int j, uint32_t turns) {
+            float sn, cn;
+            // (to 24 bits, 2 pi 2^-26 of the angle: counted below)
+            sincospif((float)(int)turns * 0x1p-31f, &sn, &cn);
+            cs[tok * D + j] = cn * a.scale32, cs[tok * D + D / 2 + j] = sn * a.scale32;
+        };
+        uint32_t farthest = 0u;
         __syncwarp();  // the last unit's tables are read
 #pragma unroll 1
         for (int tok = 0; tok < tokens; ++tok)
@@ -742,10 +760,18 @@ __global__ void __launch_bounds__(TN, TURN_CTAS) k_turn(Turn a, int lt, int slic
                 const int j = lane + 32 * y;
                 if (j >= R / 2) continue;
                 const uint32_t p = (uint32_t)(tok == 0 ? p_next[y] : turn_position(a, b, i0 + tok, axis[y]));
-                const uint32_t turns = p * fh[y] + __umulhi(p, fl[y]) - (p >> 31 ? fl[y] : 0u);
-                float sn, cn;
-                sincospif((float)(int)turns * 0x1p-31f, &sn, &cn);
-                cs[tok * D + j] = cn * a.scale32, cs[tok * D + D / 2 + j] = sn * a.scale32;
+                farthest = max(farthest, p >> 31 ? 0u - p : p);
+                put_turn(tok, j, p * fh[y] + __umulhi(p, fl[y]) - (p >> 31 ? fl[y] : 0u));
+            }
+        if (farthest > nears[warp])  // those angles again, with their roundings
+#pragma unroll 1
+            for (int z = 0; z < 2 * tokens; ++z) {
+                const int tok = z >> 1, y = z & 1, j = lane + 32 * y;
+                if (j >= R / 2) continue;
+                const uint32_t p = (uint32_t)turn_position(a, b, i0 + tok, turn_axis(a, j));
+                const double at = (int)p, f = __ldg(a.freq + j);
+                put_turn(tok, j, p * (y ? fh[1] : fh[0]) + __umulhi(p, y ? fl[1] : fl[0]) - (p >> 31 ? (y ? fl[1] : fl[0]) : 0u) +
+                                     (uint32_t)__double2int_rn(fma(-at, f, at * f) * (INV_TURN * 0x1p32)));
             }
         ask(x + all.stride);
         if (APPEND && lane < TOKENS) st[lane] = 0;
