@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(FT, (Few<D, F32, NT>::MINB)) k_kv4_few(Kv4Att 
     auto q_info = [&](const Seg &sg, int to) {  // token and position of the rows
         if (tid >= R) return;
         const int r = sg.rt * R + tid, i = r / a.G;
-        const Kv4Token tk = r < a.n * a.G ? kv4_token<MODE>(a, sg.key, sg.b, i) : Kv4Token{false, 0};
+        const Kv4Token tk = kv4_token<MODE>(a, sg.key, r < a.n * a.G, sg.b, i);
         rowinfo[to][tid] = tk.live ? make_int2(i, tk.pos) : make_int2(-1, 0);
     };
     q_ask(cur);

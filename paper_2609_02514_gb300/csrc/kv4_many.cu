@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(MT, 1) k_kv4_many(Kv4Att a, Kv4Ws ws, int R, i
             const bool single = NR - rt * R <= 128;
             const int slot_row = single ? row : x * 128 + row;
             const int r0 = rt * R + slot_row, i = r0 / a.G, gq = r0 - i * a.G;
-            const Kv4Token tk = r0 < NR ? kv4_token<MODE>(a, key, b, i) : Kv4Token{false, 0};
+            const Kv4Token tk = kv4_token<MODE>(a, key, r0 < NR, b, i);
             const bool row_live = tk.live;
             const int pos = tk.pos, sinks = kv4_sinks<MODE>(a, key);
             const bool warp_live = __any_sync(0xffffffffu, row_live);

@@ -99,18 +99,19 @@ __device__ __forceinline__ int32_t kv4_status(const Kv4Att &a, int b) {
     return (kv4_seq_of<MODE>(a, b).ok ? 0 : ACES_ROW_RANGE) | (MODE == KV4_BEHIND ? a.part_status[b / a.per] : 0);
 }
 
-// A new token: whether there is one, its position, and the queries' place in q.
+// A new token of a row inside the item or not: whether there is one, its position, and the
+// queries' place in q.
 struct Kv4Token {
     bool live;
     int pos;
 };
 template <int MODE>
-__device__ __forceinline__ Kv4Token kv4_token(const Kv4Att &a, const Kv4Keys &k, int b, int i) {
+__device__ __forceinline__ Kv4Token kv4_token(const Kv4Att &a, const Kv4Keys &k, bool inside, int b, int i) {
     if (MODE != KV4_FIRST) {
-        const bool ok = k.live && i < k.cnt;
+        const bool ok = inside && k.live && i < k.cnt;
         return {ok, ok ? kv4_pos(k.P, a.mask ? a.depth + b * a.depth_b : nullptr, i) : 0};
     }
-    if (!k.live) return {false, 0};
+    if (!inside || !k.live) return {false, 0};
     const int s = i / a.own_n, own = b * a.per + s, t = i - s * a.own_n;  // the sequence and its token
     const Kv4Seq q = kv4_seq(a.own_prefix, a.own_count, own, a.own_n, a.own_S);
     if (!q.ok || t >= q.cnt) return {false, 0};
