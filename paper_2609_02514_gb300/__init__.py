@@ -605,7 +605,7 @@ def rotate_qk(q, k, inv_freq, start=None, depth=None, positions=None, axes=None,
     k_weight: [D], or [heads, D], or none) and turned by their positions; returns a dict of q, k.
 
     inv_freq [R / 2] float32: the first R channels turn (a multiple of D / 4), pairs j and j + R / 2,
-    or interleaved 2 j and 2 j + 1, by the angle position * inv_freq[j].  Token i of sequence b is at
+    or interleaved 2 j and 2 j + 1, by the angle position * inv_freq[j] (up to 2^40).  Token i of sequence b is at
     start[b] + i, or with tree_mask()'s depth at start[b] + depth[i]; or at positions [B, n], or
     [A, B, n] with up to four axes, of which pair j turns by axes[j] ([R / 2] int32).  scale multiplies
     the turned channels.  q and k may be strided views with a dense last dimension, and `out` may

@@ -147,6 +147,10 @@ TurnHeads heads(const void *p, const int64_t *s) { return {const_cast<void *>(p)
 // (18), of 4 behind 32000 121 / 129 (28), of 16 behind 8000 131 / 119 (39); 80 tokens of 8
 // behind 8000 191 / 189 (23), of 32 behind 2000 239 / 262 (23), of 16 behind 8000 347 / 326 (46).  Float32, 12 heads
 // over 4 of 64: one token of 32 behind 2000 26 / 27 (14), of 8 behind 16000 33 / 31 (26).
+// (The parts' way through memory, 1040 bytes a row of 128, is in the constants, though it grows with
+// the rows: the two cases at 23 differ by it.)  A prefix that leaves its cache nearly empty
+// pays for two passes all the same, 100 positions in a room of 16000 to 60000: one token of 16 sequences 12 / 22,
+// of 64 26 / 39; float32 11 / 22, 43 / 57; 80 tokens of 16 58 / 86, of 64 173 / 226.
 constexpr double FEW_EXTRA = 7.0, F32_EXTRA = 20.0, MANY_EXTRA = 33.0;
 bool two_passes(const Kv4Att &a, int groups, int nsm) {
     long long keys = a.shared_S;
