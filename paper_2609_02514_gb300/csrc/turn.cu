@@ -29,7 +29,7 @@
 // are what counts: through registers, which hold two steps, it was 66 whatever the number of
 // warps or instructions, and with a pipeline that ran dry behind every token; four steps of
 // 1 KB a warp through shared memory, across tokens, are enough (six: 59).
-// Into the cache, 80 tokens of 64 sequences: 45 us (111 MB), 35 when no row is done again: a
+// Into the cache, 80 tokens of 64 sequences: 43 us (111 MB), 35 when no row is done again: a
 // warp that meets one is late by some 9 us, and has two or three tokens in all.  In
 // float64 those rows made it 48, one after another by their four lanes 94.
 #define ACES_FILE 10  // site numbers of the checked build
