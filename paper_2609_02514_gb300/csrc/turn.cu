@@ -216,12 +216,19 @@ static __device__ __noinline__ bool wide_row(const Turn &a, int b, int i, int h,
     const int lane = threadIdx.x & 31, d0 = lane * CH, half = a.R / 2;
     const long long at = b * a.k.b + i * a.k.i + h * a.k.h + d0;
     double y[CH], ss = 0.0;
+    bool none = !a.norm;
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
         y[e] = F32 ? reinterpret_cast<const float *>(a.k.p)[at + e]
                    : __uint_as_float((uint32_t) reinterpret_cast<const unsigned short *>(a.k.p)[at + e] << 16);
+        none = a.norm ? none || !(fabs(y[e]) <= FLT_MAX) : none && y[e] != y[e];
         ss = fma(y[e], y[e], ss);
         if (a.norm) y[e] *= (double)weight_at(a.kw, h * a.kw.h + d0 + e);
+    }
+    if (a.norm ? __any_sync(ALL, none) : __all_sync(ALL, none)) {  // a norm that is none leaves zeros and NaN
+        if (d0 % 8 == 0) reinterpret_cast<uint32_t *>(row)[d0 / 8] = 0x88888888u;
+        if (d0 % G == 0) reinterpret_cast<unsigned short *>(row + D / 2)[d0 / G] = 0;
+        return true;
     }
     if (a.norm) {
         for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(ALL, ss, x);
